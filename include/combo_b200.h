@@ -304,6 +304,60 @@ combo_status combo_aggregation_divergence_noalloc(const void* models, const void
                                                   int64_t P, double* rho_out, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * The local step (Section 4.1 step (1)) for all workers at once: the operators
+ * that lead from a worker's samples to the gradient combo_segment_aggregate_sgd
+ * takes.  The paper trains with a framework's layers and states none of these;
+ * their formulas stand here.
+ * ---------------------------------------------------------------------------
+ *
+ * Gradient norms over many tensors, and clipping.  Worker w's gradient is a list
+ * of tensors; norm_w is taken over all of them together, and
+ *
+ *   norm_w = sqrt( sum g^2 ),   c_w = min(1, max_norm / (norm_w + 1e-6)),   out = c_w * g
+ *
+ * d_tensors: DEVICE array of n_tensors addresses, each aligned to its element
+ * (elem_bytes 4 = float, 2 = bfloat16), in the workers' order.  d_begin: device
+ * int64[n_tensors + 1], d_begin[t] = number of elements in the tensors before t
+ * (d_begin[0] = 0, d_begin[n_tensors] = total).  d_first: device int32[N + 1],
+ * worker w owns tensors d_first[w] .. d_first[w+1] - 1 (d_first[0] = 0,
+ * d_first[N] = n_tensors).  Tensors and workers may be empty.  The three arrays
+ * are trusted, like idx (see combo_check_tensors).  A row of an [N][P] array is
+ * one tensor; so is every layer's piece of it.
+ *
+ * combo_grad_norm writes norm_out and coef_out (device float[N]; either may be
+ * NULL); combo_grad_clip writes them and the clipped tensors to the addresses in
+ * d_out (as d_tensors; an output may be its input, and must not overlap any other
+ * input).  A tensor that is its own output and whose coefficient is 1 is not
+ * rewritten.  A norm that is infinite gives c = 0, one that is NaN gives NaN, and
+ * the outputs follow by the formula; a worker without elements has norm 0.
+ * max_norm >= 0.
+ *
+ * Arithmetic: squares are summed in binary32 over at most 16 elements and in
+ * binary64 beyond (wholly in binary64 where the squares leave binary32's range),
+ * in an order that depends on the sizes alone; out is the binary32 product,
+ * rounded once.  scratch: device memory of at least combo_grad_scratch_bytes(N)
+ * bytes, 8-byte aligned, contents undefined afterwards.  Two launches on
+ * `stream`.  total < 2^46.
+ */
+size_t combo_grad_scratch_bytes(int N);
+combo_status combo_grad_norm(const void* const* d_tensors, const int64_t* d_begin, const int32_t* d_first,
+                             int n_tensors, int N, int64_t total, int elem_bytes, float max_norm,
+                             float* norm_out, float* coef_out, void* scratch, size_t scratch_bytes,
+                             void* stream);
+combo_status combo_grad_clip(const void* const* d_tensors, void* const* d_out, const int64_t* d_begin,
+                             const int32_t* d_first, int n_tensors, int N, int64_t total, int elem_bytes,
+                             float max_norm, float* norm_out, float* coef_out, void* scratch,
+                             size_t scratch_bytes, void* stream);
+
+/* Debug helper for the two calls above: *dev_flag (device int32) becomes 0 when the
+ * table is as described (ascending, ends in place, non-empty tensors non-null and
+ * aligned), else 1 + a bad tensor, or 1 + n_tensors + a bad worker. */
+combo_status combo_check_tensors(const void* const* d_tensors, const int64_t* d_begin, const int32_t* d_first,
+                                 int n_tensors, int N, int64_t total, int elem_bytes, void* stream,
+                                 int32_t* dev_flag);
+
+/*
  * Reads and clears the device status word that kernels set when one of their
  * bounded waits gives up.  Synchronises the device.  Returns COMBO_OK or
  * COMBO_ERR_DEVICE_TIMEOUT (or COMBO_ERR_CUDA).

@@ -10,4 +10,5 @@ from .binding import (ComboError, combo_aggregation_divergence, combo_aggregatio
                       combo_select_peers_default_stream, combo_set_kernel_path, combo_set_launch_overlap,
                       combo_set_tuning,
                       combo_validate_idx, combo_version, load, combo_max_launch_columns,
-                      combo_set_launch_columns, combo_debug_dead_wait)
+                      combo_set_launch_columns, combo_debug_dead_wait,
+                      combo_grad_scratch_bytes, combo_grad_norm, combo_grad_clip, combo_check_tensors)

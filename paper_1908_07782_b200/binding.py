@@ -55,6 +55,9 @@ def load():
                              vp, vp, vp, vp],
         "combo_aggregation_divergence": [vp, vp, i32, vp, i32, i64, vp, vp, ctypes.c_size_t, vp],
         "combo_aggregation_divergence_noalloc": [vp, vp, i32, vp, i32, i64, vp, vp],
+        "combo_grad_norm": [vp, vp, vp, i32, i32, i64, i32, f32, vp, vp, vp, ctypes.c_size_t, vp],
+        "combo_grad_clip": [vp, vp, vp, vp, i32, i32, i64, i32, f32, vp, vp, vp, ctypes.c_size_t, vp],
+        "combo_check_tensors": [vp, vp, vp, i32, i32, i64, i32, vp, vp],
         "combo_debug_dead_wait": [vp],
         "combo_device_status": [],
         "combo_last_kernel_path": [],
@@ -66,6 +69,8 @@ def load():
         fn.restype = ctypes.c_int
     lib.combo_divergence_scratch_bytes.argtypes = [i32]
     lib.combo_divergence_scratch_bytes.restype = ctypes.c_size_t
+    lib.combo_grad_scratch_bytes.argtypes = [i32]
+    lib.combo_grad_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_set_kernel_path.argtypes = [i32]
     lib.combo_set_kernel_path.restype = None
     lib.combo_set_tuning.argtypes = [i32, i32]
@@ -228,6 +233,44 @@ def combo_aggregation_divergence_noalloc(models, mean_of, elem_bytes, weights, N
                                                        P, _ptr(rho_out), _stream(stream)),
            "combo_aggregation_divergence_noalloc")
     return rho_out
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def combo_grad_scratch_bytes(N: int) -> int:
+    return int(load().combo_grad_scratch_bytes(N))
+
+
+def combo_grad_norm(tensors, begin, first, n_tensors, N, total, elem_bytes, max_norm, norm_out, coef_out, scratch,
+                    stream=None):
+    """Norm of every worker's gradient over its tensors, and the coefficient that clips it
+    to ``max_norm`` (float32 [N] each, device).  ``tensors``: device int64 addresses;
+    ``begin``: device int64 [n_tensors + 1] positions; ``first``: device int32 [N + 1]."""
+    _check(load().combo_grad_norm(_ptr(tensors), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes, max_norm,
+                                  _ptr(norm_out), _ptr(coef_out), _ptr(scratch), _bytes(scratch), _stream(stream)),
+           "combo_grad_norm")
+    return norm_out
+
+
+def combo_grad_clip(tensors, out, begin, first, n_tensors, N, total, elem_bytes, max_norm, norm_out, coef_out, scratch,
+                    stream=None):
+    """combo_grad_norm, and every tensor times its worker's coefficient, written to the
+    addresses in ``out`` (device int64; may be ``tensors``)."""
+    _check(load().combo_grad_clip(_ptr(tensors), _ptr(out), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes,
+                                  max_norm, _ptr(norm_out), _ptr(coef_out), _ptr(scratch), _bytes(scratch),
+                                  _stream(stream)), "combo_grad_clip")
+    return norm_out
+
+
+def combo_check_tensors(tensors, begin, first, n_tensors, N, total, elem_bytes, stream=None) -> int:
+    """0 when the table is as combo_grad_norm wants it, else 1 + a bad tensor, or
+    1 + n_tensors + a bad worker."""
+    flag = torch.zeros(1, dtype=torch.int32, device=begin.device)
+    _check(load().combo_check_tensors(_ptr(tensors), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes,
+                                      _stream(stream), _ptr(flag)), "combo_check_tensors")
+    return int(flag.item())
 
 
 def combo_device_status():

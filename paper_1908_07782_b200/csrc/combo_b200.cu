@@ -8,6 +8,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "host_common.h"
 #include "segment_aggregate.cuh"
 #include "divergence.cuh"
 #include "select_peers.cuh"
@@ -858,6 +859,21 @@ combo_status select_peers_impl(uint64_t seed, uint32_t round, int N, int S, int 
 }
 
 }  // namespace
+
+namespace combo_host {
+
+combo_status fail(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+
+combo_status device(int* sms, int* smem_optin) {
+    DeviceInfo* dev = nullptr;
+    combo_status rc = device_info(&dev);
+    if (rc != COMBO_OK) return rc;
+    *sms = dev->sms;
+    *smem_optin = dev->smem_optin;
+    return COMBO_OK;
+}
+
+}  // namespace combo_host
 
 extern "C" {
 

@@ -1,0 +1,42 @@
+// What the translation units of libcombo_b200.so share on the host side.  Defined in combo_b200.cu.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/combo_b200.h"
+
+namespace combo_host {
+
+#pragma GCC visibility push(hidden)
+// Records a failed CUDA call for combo_last_cuda_error() and returns COMBO_ERR_CUDA.
+combo_status fail(cudaError_t e, const char* what);
+// The current device's SM count and largest shared memory of a block; COMBO_ERR_UNSUPPORTED unless it is 10.x.
+combo_status device(int* sms, int* smem_optin);
+#pragma GCC visibility pop
+
+inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Whether [a, a + na) and [b, b + nb) share a byte.
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na && nb && x < y + nb && y < x + na;
+}
+
+// Launches `kern` so that it may become resident while the stream's preceding kernel drains; the kernel
+// itself waits for that one (pdl_wait) before it touches anything that one writes.
+template <typename... P, typename... A>
+inline cudaError_t launch_after(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
+}  // namespace combo_host
