@@ -358,6 +358,54 @@ combo_status combo_check_tensors(const void* const* d_tensors, const int64_t* d_
                                  int32_t* dev_flag);
 
 /*
+ * Group norm with an activation, channels last, for samples of all workers.  x is
+ * [B][L][C] (B samples of L positions), `groups` groups of C / groups neighbouring
+ * channels; w is the worker a sample belongs to:
+ *
+ *   mean, rstd = 1 / sqrt(var + eps) over a (sample, group),  var biased
+ *   h = (x - mean) * rstd,   z = h * gamma_w + beta_w,   y = act(z)
+ *
+ * and backward, from dy and the mean and rstd the forward call wrote:
+ *
+ *   dz = dy * act'(z),   dgamma_w = sum dz * h,   dbeta_w = sum dz     (w's samples)
+ *   t = dz * gamma_w,    dx = rstd * (t - mean(t) - h * mean(t * h))
+ *
+ * x, y, dy, dx: elem_bytes 4 = float or 2 = bfloat16, aligned to it; positions lie
+ * `..._pitch` >= C elements apart, samples L pitches.  y may be x, and dx may be x or
+ * dy, with the same pitch; other overlaps are refused.  gamma, beta: param_bytes 4 or
+ * 2, worker w's at + w * param_pitch elements -- a flat [N][P] array is given by its
+ * first vector's place and pitch P --; both NULL for 1 and 0.  d_begin: device
+ * int64[N + 1], worker w's samples are d_begin[w] .. d_begin[w+1] - 1 (ascending,
+ * d_begin[0] = 0, d_begin[N] = B; trusted, like idx); NULL if N == 1.  A worker may
+ * have no sample.  mean, rstd: float [B][groups], NULL in the forward call if not
+ * wanted.  dgamma, dbeta: float, worker w's at + w * grad_pitch, written (not added
+ * to), zeros for a worker without samples; both NULL if not wanted.
+ *
+ * Arithmetic: binary32, rounded once to bfloat16 at the end.  Statistics by merging
+ * (count, mean, sum of squared deviations), so a large mean costs nothing.  z is formed
+ * in the order written, without fused operations, in both calls: where ReLU clipped
+ * (z <= 0), dz is 0 whatever dy holds.  ReLU keeps NaN; NaN and infinity stay in their
+ * (sample, group).  Results do not change from run to run.
+ *
+ * scratch (backward): combo_group_norm_scratch_bytes bytes, 8-byte aligned.
+ * C / groups <= COMBO_NORM_MAX_CHANNELS, B * L * C <= 2^40.
+ */
+enum { COMBO_ACT_NONE = 0, COMBO_ACT_RELU = 1, COMBO_ACT_SILU = 2 /* z / (1 + exp(-z)) */ };
+#define COMBO_NORM_MAX_CHANNELS 4096
+combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y_pitch, int elem_bytes,
+                              const void* gamma, const void* beta, int param_bytes, int64_t param_pitch,
+                              const int64_t* d_begin, int N, int64_t B, int64_t L, int64_t C, int groups,
+                              float eps, int act, float* mean_out, float* rstd_out, void* stream);
+size_t combo_group_norm_scratch_bytes(int64_t B, int64_t L, int64_t C);
+combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch,
+                                       void* dx, int64_t dx_pitch, int elem_bytes, const void* gamma,
+                                       const void* beta, int param_bytes, int64_t param_pitch,
+                                       const int64_t* d_begin, int N, int64_t B, int64_t L, int64_t C,
+                                       int groups, int act, const float* mean, const float* rstd,
+                                       float* dgamma, float* dbeta, int64_t grad_pitch, void* scratch,
+                                       size_t scratch_bytes, void* stream);
+
+/*
  * Reads and clears the device status word that kernels set when one of their
  * bounded waits gives up.  Synchronises the device.  Returns COMBO_OK or
  * COMBO_ERR_DEVICE_TIMEOUT (or COMBO_ERR_CUDA).

@@ -14,6 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libcombo_b200.so")
 _lib = None
 
 COMBO_OK = 0
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 PATH_AUTO, PATH_DIRECT, PATH_STAGED, PATH_TILE, PATH_DIRECT_NAIVE = 0, 1, 2, 5, 6
 
 
@@ -58,6 +59,9 @@ def load():
         "combo_grad_norm": [vp, vp, vp, i32, i32, i64, i32, f32, vp, vp, vp, ctypes.c_size_t, vp],
         "combo_grad_clip": [vp, vp, vp, vp, i32, i32, i64, i32, f32, vp, vp, vp, ctypes.c_size_t, vp],
         "combo_check_tensors": [vp, vp, vp, i32, i32, i64, i32, vp, vp],
+        "combo_group_norm": [vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, vp, vp],
+        "combo_group_norm_backward": [vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, i32,
+                                      vp, vp, vp, vp, i64, vp, ctypes.c_size_t, vp],
         "combo_debug_dead_wait": [vp],
         "combo_device_status": [],
         "combo_last_kernel_path": [],
@@ -71,6 +75,8 @@ def load():
     lib.combo_divergence_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_grad_scratch_bytes.argtypes = [i32]
     lib.combo_grad_scratch_bytes.restype = ctypes.c_size_t
+    lib.combo_group_norm_scratch_bytes.argtypes = [i64, i64, i64]
+    lib.combo_group_norm_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_set_kernel_path.argtypes = [i32]
     lib.combo_set_kernel_path.restype = None
     lib.combo_set_tuning.argtypes = [i32, i32]
@@ -271,6 +277,86 @@ def combo_check_tensors(tensors, begin, first, n_tensors, N, total, elem_bytes, 
     _check(load().combo_check_tensors(_ptr(tensors), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes,
                                       _stream(stream), _ptr(flag)), "combo_check_tensors")
     return int(flag.item())
+
+
+def _same(name: str, what: str, ok: bool) -> None:
+    if not ok:
+        raise ValueError("%s: %s" % (name, what))
+
+
+def _pitch(t, name, arg) -> int:
+    """Elements between the positions of a channels-last [B, L, C] tensor."""
+    B, L, C = t.shape
+    pitch = t.stride(1) if L > 1 else t.stride(0) if B > 1 else C
+    _same(name, "%s: channels must be neighbours, samples L positions apart" % arg,
+          (C == 1 or t.stride(2) == 1) and (B <= 1 or L <= 1 or t.stride(0) == L * pitch))
+    return pitch
+
+
+def _rows(t, name, arg) -> int:
+    """Elements between the rows of an [N, C] tensor."""
+    _same(name, "%s: a row's elements must be neighbours" % arg, t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1))
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _norm_args(name, x, gamma, beta, begin):
+    """What the two group norm calls check and pass alike: parameters, their size and pitch, workers."""
+    _same(name, "x must be [B, L, C]", x.dim() == 3)
+    N = 1 if begin is None else begin.numel() - 1
+    _same(name, "begin must be int64", begin is None or (begin.dtype == torch.int64 and begin.is_contiguous()))
+    if gamma is None or beta is None:
+        return N, 4, 0
+    _same(name, "gamma and beta must be [N, C] of one type and one pitch", gamma.shape == beta.shape == (N, x.shape[2])
+          and gamma.dtype == beta.dtype and gamma.dtype in (torch.float32, torch.bfloat16)
+          and _rows(gamma, name, "gamma") == _rows(beta, name, "beta"))
+    return N, gamma.element_size(), _rows(gamma, name, "gamma")
+
+
+def combo_group_norm(x, y, gamma, beta, begin, groups, eps, act, mean=None, rstd=None, scratch=None, stream=None):
+    """y = act(group norm of x), channels last: x, y [B, L, C]; gamma, beta [N, C] (views of flat
+    parameter vectors, or None); begin: device int64 [N + 1], the workers' samples, or None for one
+    worker; mean, rstd: float32 [B, groups] or None.  The forward pass needs no scratch: it is
+    taken so that one set of arguments serves both directions."""
+    name = "combo_group_norm"
+    N, pb, pp = _norm_args(name, x, gamma, beta, begin)
+    _same(name, "y must be like x", y.shape == x.shape and y.dtype == x.dtype and x.dtype in (torch.float32, torch.bfloat16))
+    for t in (mean, rstd):
+        _same(name, "mean and rstd must be float32 [B, groups]",
+              t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == x.shape[0] * groups))
+    B, L, C = x.shape
+    _check(load().combo_group_norm(_ptr(x), _pitch(x, name, "x"), _ptr(y), _pitch(y, name, "y"), x.element_size(),
+                                   _ptr(gamma), _ptr(beta), pb, pp, _ptr(begin), N, B, L, C, groups, eps, act,
+                                   _ptr(mean), _ptr(rstd), _stream(stream)), name)
+    return y
+
+
+def combo_group_norm_scratch_bytes(B: int, L: int, C: int, groups: int = 1) -> int:
+    """Bytes the backward pass wants (the same for any number of groups)."""
+    return int(load().combo_group_norm_scratch_bytes(B, L, C))
+
+
+def combo_group_norm_backward(dy, x, dx, gamma, beta, begin, groups, act, mean, rstd, dgamma, dbeta, scratch,
+                              stream=None):
+    """Gradients of combo_group_norm: dx [B, L, C] and, per worker, dgamma and dbeta (float32
+    [N, C], views of flat gradient vectors, or None), from the forward call's mean and rstd."""
+    name = "combo_group_norm_backward"
+    N, pb, pp = _norm_args(name, x, gamma, beta, begin)
+    _same(name, "dy and dx must be like x", dy.shape == dx.shape == x.shape and dy.dtype == dx.dtype == x.dtype
+          and x.dtype in (torch.float32, torch.bfloat16))
+    for t in (mean, rstd):
+        _same(name, "mean and rstd must be float32 [B, groups]",
+              t.dtype == torch.float32 and t.is_contiguous() and t.numel() == x.shape[0] * groups)
+    gp = 0
+    if dgamma is not None and dbeta is not None:
+        gp = _rows(dgamma, name, "dgamma")
+        _same(name, "dgamma and dbeta must be float32 [N, C] of one pitch", dgamma.shape == dbeta.shape == (N, x.shape[2])
+              and dgamma.dtype == dbeta.dtype == torch.float32 and gp == _rows(dbeta, name, "dbeta"))
+    B, L, C = x.shape
+    _check(load().combo_group_norm_backward(
+        _ptr(dy), _pitch(dy, name, "dy"), _ptr(x), _pitch(x, name, "x"), _ptr(dx), _pitch(dx, name, "dx"),
+        x.element_size(), _ptr(gamma), _ptr(beta), pb, pp, _ptr(begin), N, B, L, C, groups, act, _ptr(mean), _ptr(rstd),
+        _ptr(dgamma), _ptr(dbeta), gp, _ptr(scratch), _bytes(scratch), _stream(stream)), name)
+    return dx
 
 
 def combo_device_status():
