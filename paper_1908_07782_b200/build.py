@@ -60,6 +60,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
                 [nvcc_path()] + arch + ["-lineinfo", "-O3", "-std=c++17", "-Xptxas", "-v" if verbose else "-warn-spills",
                                         "-Xcompiler", "-fPIC", "-c", "-o", part, src]))
     if any([p.wait() for p in running]):
+        for part, _ in spare:
+            if os.path.exists(part):
+                os.remove(part)
         raise RuntimeError("nvcc failed")
     for part, obj in spare:
         os.replace(part, obj)
