@@ -406,6 +406,43 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
                                        size_t scratch_bytes, void* stream);
 
 /*
+ * Products grouped by worker: every worker's rows (samples) times its own weights,
+ * a layer without bias in one call for all workers, however many rows each has.
+ *
+ *   combo_grouped_linear              y[m][n]    = sum_k x[m][k] W_w[n][k]
+ *   combo_grouped_linear_grad_input   dx[m][k]   = sum_n dy[m][n] W_w[n][k]
+ *   combo_grouped_linear_grad_weight  dW_w[n][k] = sum_m dy[m][n] x[m][k]
+ *
+ * m runs over the M rows, worker w's being d_begin[w] .. d_begin[w+1] - 1 (device
+ * int64[N + 1], ascending, within 0 .. M; trusted, like idx; rows of no worker are
+ * neither read into a result nor written), k over n_in, n over n_out.  Rows of x, y,
+ * dx, dy lie `..._pitch` elements apart.  W_w is at w + v * w_stride elements for
+ * worker v, its rows w_pitch >= n_in apart: a layer inside a flat [N][P] array is given
+ * by its first weight's place, pitch n_in and stride P.  The same holds for dW, which
+ * is written (not added to), zeros for a worker without rows.
+ *
+ * elem_bytes (of the inputs) / out_bytes: 4 / 4 float; 2 / 2 and 2 / 4 bfloat16 in,
+ * bfloat16 or float out.  Products are exact to binary32 or better and accumulated in
+ * binary32, the result is rounded once.  Outputs must not overlap inputs.  A NaN or
+ * infinity reaches the results that its row and its worker's weights enter, no others.
+ * Fastest where all bases, pitches and strides are multiples of 16 bytes.
+ */
+#define COMBO_LINEAR_MAX_WIDTH (1 << 20)   /* n_in, n_out */
+#define COMBO_LINEAR_MAX_ROWS (1 << 22)    /* M */
+combo_status combo_grouped_linear(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch,
+                                  int64_t w_stride, void* y, int64_t y_pitch, int elem_bytes, int out_bytes,
+                                  const int64_t* d_begin, int N, int64_t M, int64_t n_in, int64_t n_out,
+                                  void* stream);
+combo_status combo_grouped_linear_grad_input(const void* dy, int64_t dy_pitch, const void* w, int64_t w_pitch,
+                                             int64_t w_stride, void* dx, int64_t dx_pitch, int elem_bytes,
+                                             int out_bytes, const int64_t* d_begin, int N, int64_t M,
+                                             int64_t n_in, int64_t n_out, void* stream);
+combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch,
+                                              void* dw, int64_t dw_pitch, int64_t dw_stride, int elem_bytes,
+                                              int out_bytes, const int64_t* d_begin, int N, int64_t M,
+                                              int64_t n_in, int64_t n_out, void* stream);
+
+/*
  * Reads and clears the device status word that kernels set when one of their
  * bounded waits gives up.  Synchronises the device.  Returns COMBO_OK or
  * COMBO_ERR_DEVICE_TIMEOUT (or COMBO_ERR_CUDA).

@@ -13,4 +13,5 @@ from .binding import (ComboError, combo_aggregation_divergence, combo_aggregatio
                       combo_set_launch_columns, combo_debug_dead_wait,
                       combo_grad_scratch_bytes, combo_grad_norm, combo_grad_clip, combo_check_tensors,
                       combo_group_norm, combo_group_norm_scratch_bytes, combo_group_norm_backward,
-                      ACT_NONE, ACT_RELU, ACT_SILU)
+                      ACT_NONE, ACT_RELU, ACT_SILU,
+                      combo_grouped_linear, combo_grouped_linear_grad_input, combo_grouped_linear_grad_weight)

@@ -62,6 +62,9 @@ def load():
         "combo_group_norm": [vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, vp, vp],
         "combo_group_norm_backward": [vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, i32,
                                       vp, vp, vp, vp, i64, vp, ctypes.c_size_t, vp],
+        "combo_grouped_linear": [vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, i32, i64, i64, i64, vp],
+        "combo_grouped_linear_grad_input": [vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, i32, i64, i64, i64, vp],
+        "combo_grouped_linear_grad_weight": [vp, i64, vp, i64, vp, i64, i64, i32, i32, vp, i32, i64, i64, i64, vp],
         "combo_debug_dead_wait": [vp],
         "combo_device_status": [],
         "combo_last_kernel_path": [],
@@ -299,6 +302,11 @@ def _rows(t, name, arg) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _size(t, name) -> int:
+    _same(name, "types are float32 and bfloat16", t.dtype in (torch.float32, torch.bfloat16))
+    return t.element_size()
+
+
 def _norm_args(name, x, gamma, beta, begin):
     """What the two group norm calls check and pass alike: parameters, their size and pitch, workers."""
     _same(name, "x must be [B, L, C]", x.dim() == 3)
@@ -357,6 +365,53 @@ def combo_group_norm_backward(dy, x, dx, gamma, beta, begin, groups, act, mean, 
         x.element_size(), _ptr(gamma), _ptr(beta), pb, pp, _ptr(begin), N, B, L, C, groups, act, _ptr(mean), _ptr(rstd),
         _ptr(dgamma), _ptr(dbeta), gp, _ptr(scratch), _bytes(scratch), _stream(stream)), name)
     return dx
+
+
+def _product_args(name, rows, weights, begin, row_widths):
+    """Shapes and pitches of a grouped product: row operands [M, width], weights [N, n_out, n_in]."""
+    N, n_out, n_in = weights.shape
+    _same(name, "begin must be int64 [N + 1]", begin.dtype == torch.int64 and begin.shape == (N + 1,) and begin.is_contiguous())
+    _same(name, "weights: a row's elements must be neighbours", n_in == 1 or weights.stride(2) == 1)
+    M = rows[0].shape[0]
+    for t, width in zip(rows, row_widths):
+        _same(name, "rows must be [M, %d]" % width, t.shape == (M, width))
+    w_pitch = weights.stride(1) if n_out > 1 else n_in
+    return N, M, n_in, n_out, w_pitch, weights.stride(0) if N > 1 else 0
+
+
+def combo_grouped_linear(x, w, y, begin, stream=None):
+    """y[m] = x[m] W_w^T for every worker w's rows m (``begin``: device int64 [N + 1]).  x [M, n_in],
+    w [N, n_out, n_in] (a view of flat parameter vectors, strides as they are), y [M, n_out] of x's
+    type or, for bfloat16, float32."""
+    name = "combo_grouped_linear"
+    N, M, n_in, n_out, wp, ws = _product_args(name, (x, y), w, begin, (w.shape[2], w.shape[1]))
+    _same(name, "x and w must have one type", x.dtype == w.dtype)
+    _check(load().combo_grouped_linear(_ptr(x), _rows(x, name, "x"), _ptr(w), wp, ws, _ptr(y), _rows(y, name, "y"),
+                                       _size(x, name), _size(y, name), _ptr(begin), N, M, n_in, n_out, _stream(stream)), name)
+    return y
+
+
+def combo_grouped_linear_grad_input(dy, w, dx, begin, stream=None):
+    """dx[m] = dy[m] W_w: the gradient of combo_grouped_linear for its rows."""
+    name = "combo_grouped_linear_grad_input"
+    N, M, n_in, n_out, wp, ws = _product_args(name, (dy, dx), w, begin, (w.shape[1], w.shape[2]))
+    _same(name, "dy and w must have one type", dy.dtype == w.dtype)
+    _check(load().combo_grouped_linear_grad_input(_ptr(dy), _rows(dy, name, "dy"), _ptr(w), wp, ws, _ptr(dx),
+                                                  _rows(dx, name, "dx"), _size(dy, name), _size(dx, name), _ptr(begin), N, M,
+                                                  n_in, n_out, _stream(stream)), name)
+    return dx
+
+
+def combo_grouped_linear_grad_weight(dy, x, dw, begin, stream=None):
+    """dw[w] = sum over worker w's rows of dy[m]^T x[m]: the gradient for the weights, [N, n_out, n_in]
+    (a view of flat gradient vectors), of dy's type or float32."""
+    name = "combo_grouped_linear_grad_weight"
+    N, M, n_in, n_out, wp, ws = _product_args(name, (dy, x), dw, begin, (dw.shape[1], dw.shape[2]))
+    _same(name, "dy and x must have one type", dy.dtype == x.dtype)
+    _check(load().combo_grouped_linear_grad_weight(_ptr(dy), _rows(dy, name, "dy"), _ptr(x), _rows(x, name, "x"), _ptr(dw),
+                                                   wp, ws, _size(dy, name), _size(dw, name), _ptr(begin), N, M, n_in, n_out,
+                                                   _stream(stream)), name)
+    return dw
 
 
 def combo_device_status():
