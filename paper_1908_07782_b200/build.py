@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "build")
 HEADERS = {
     "combo_b200.cu": ("segment_aggregate.cuh", "select_peers.cuh", "divergence.cuh", "pull_aggregate.cuh", "host_common.h"),
     "group_norm.cu": ("host_common.h", "step_common.cuh"),
-    "grouped_linear.cu": ("host_common.h", "step_common.cuh"),
+    "grouped_linear.cu": ("host_common.h", "step_common.cuh", "tensor_core.cuh"),
     "grad_clip.cu": ("host_common.h", "step_common.cuh"),
 }
 SOURCES = [os.path.join(CSRC, f) for f in HEADERS]

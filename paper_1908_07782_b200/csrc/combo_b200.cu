@@ -873,6 +873,16 @@ combo_status device(int* sms, int* smem_optin) {
     return COMBO_OK;
 }
 
+bool encode_tiled(CUtensorMap* map, CUtensorMapDataType type, int rank, void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+                  const cuuint32_t* box, const cuuint32_t* elem_strides, CUtensorMapSwizzle swizzle) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    const CUresult r = enc ? enc(map, type, (cuuint32_t)rank, base, dims, strides, box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE)
+                           : CUDA_ERROR_NOT_FOUND;
+    if (r != CUDA_SUCCESS) snprintf(t_cuda_err, sizeof(t_cuda_err), "cuTensorMapEncodeTiled failed with %d", (int)r);
+    return r == CUDA_SUCCESS;
+}
+
 }  // namespace combo_host
 
 extern "C" {
@@ -1211,6 +1221,11 @@ combo_status combo_device_status(void) {
         // (the device is idle here), so that the launch that next takes that slot starts clean
         static const combo::TileSlot clean[combo::kTileSlots] = {};
         cudaMemcpyToSymbol(combo::g_tile_slots, clean, sizeof(clean));
+        snprintf(t_cuda_err, sizeof(t_cuda_err), "bounded wait gave up at site %d", v);
+        return COMBO_ERR_DEVICE_TIMEOUT;
+    }
+    if ((e = combo_host::grouped_linear_status(&v)) != cudaSuccess) return cuda_fail(e, "grouped product status");
+    if (v != 0) {
         snprintf(t_cuda_err, sizeof(t_cuda_err), "bounded wait gave up at site %d", v);
         return COMBO_ERR_DEVICE_TIMEOUT;
     }

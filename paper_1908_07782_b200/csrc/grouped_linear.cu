@@ -12,6 +12,7 @@
 //   gradient, weights n            k           m (ragged)   both along i / j
 #include "host_common.h"
 #include "step_common.cuh"
+#include "tensor_core.cuh"
 
 namespace {
 
@@ -189,6 +190,345 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
     }
 }
 
+// ---------------------------------------------------------------- tensor cores
+// bfloat16 operands on 16-byte boundaries.  The weights' index is the height of the product (128 CG outputs), the
+// ragged rows its width: a worker's rows are cut evenly into tiles of at most p.width, and the width of a product can
+// be any multiple of 16 CG, so that ragged rows cost at most 16 CG - 1 idle columns a worker, not half a tile.
+//
+//              height i                       width j                    summed r
+//   forward    n: W, along r                  rows: X, along r           k
+//   grad rows  k: W, along i                  rows: dY, along r          n
+//   grad w.    n: dY, along i                 k: X, along j              rows (ragged)
+//
+// Persistent CTAs; a warp that issues TMA loads into a ring of stages of 64 values of r, a warp that issues the
+// products, four warps that take finished accumulators out of TMEM (two of them there, 256 columns each, so that the
+// next tile's products run meanwhile), turn them through shared memory and store them.  The last rows of a worker in
+// the gradient of the weights: what the load brought beyond them is zeroed in shared memory before the products see
+// it (another worker's NaN would not vanish by being multiplied with zero).
+using namespace combo_tc;
+
+__device__ int g_linear_status;              // 0, or the site of the first wait that gave up
+__device__ __forceinline__ bool give_up(int site) {
+    atomicCAS(&g_linear_status, 0, site);
+    return false;
+}
+
+constexpr int kTcThreads = 192;
+constexpr int kStep = 64;                    // values of r in a stage
+constexpr int kOperandA = 128 * kStep * 2;   // bytes of the height's operand in a stage
+constexpr int kRowBox = 32;                  // rows in a box of X or dY
+constexpr int kMaxStages = 8;
+constexpr int kTurn = 32 * 33 * 4;           // bytes in which an epilogue warp turns 32 x 32 outputs
+constexpr int kTmemColumns = 512;
+
+struct TcParams {
+    Product p;
+    int width;                               // widest tile along j
+    int stages, stage_bytes;
+};
+
+// One tile of the grid's work, and how far the ring has gone.
+struct Tile {
+    int w;                                   // worker
+    long long row0, row1;                    // its rows: of the tile (forward, rows' gradient), or all that are summed
+    int i0, j0, n;                           // outputs; n = the product's width
+    int steps;                               // stages of r
+};
+
+// Walks the tiles t, t + stride, ... in order, workers 32 at a time.  The whole warp.
+template <int CG, int MODE> struct Tiles {
+    const TcParams& q;
+    int t, lane, w0, mt, jt;
+    int incl, total, before;                 // tiles of the lane's worker and those before it in the lot; of the lot; before the lot
+    __device__ __forceinline__ Tiles(const TcParams& q_, int first) : q(q_), t(first) {
+        lane = threadIdx.x & 31;
+        mt = (q.p.I + 128 * CG - 1) / (128 * CG);
+        jt = (q.p.J + q.width - 1) / q.width;
+        w0 = before = total = incl = 0;
+        if (MODE != kGradWeight) lot();
+    }
+    __device__ __forceinline__ void lot() {
+        long long a = 0, b = 0;
+        if (w0 + lane < q.p.N) rows_of(q.p, w0 + lane, a, b);
+        incl = (int)((b - a + q.width - 1) / q.width) * mt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        total = __shfl_sync(0xffffffffu, incl, 31);
+    }
+    __device__ __forceinline__ bool next(Tile& x, int stride) {
+        if (MODE == kGradWeight) {
+            const int per = mt * jt;
+            if (t >= per * q.p.N) return false;
+            x.w = t / per;
+            const int k = t - x.w * per;
+            x.i0 = (k % mt) * 128 * CG;
+            x.j0 = (k / mt) * q.width;
+            x.n = q.width;
+            rows_of(q.p, x.w, x.row0, x.row1);
+            x.steps = (int)((x.row1 - x.row0 + kStep - 1) / kStep);
+        } else {
+            while (t >= before + total) {
+                before += total;
+                w0 += 32;
+                if (w0 >= q.p.N) return false;
+                lot();
+            }
+            const unsigned m = __ballot_sync(0xffffffffu, incl > t - before);
+            const int k = __ffs(m) - 1;
+            const int end = __shfl_sync(0xffffffffu, incl, k), prev = __shfl_sync(0xffffffffu, incl, k > 0 ? k - 1 : 0);
+            const int start = k > 0 ? prev : 0, at = t - before - start, tiles = (end - start) / mt;
+            x.w = w0 + k;
+            long long a, b;
+            rows_of(q.p, x.w, a, b);
+            const int even = (int)((b - a + tiles - 1) / tiles);
+            x.n = (even + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            x.i0 = (at % mt) * 128 * CG;
+            x.j0 = (at / mt) * x.n;
+            x.row0 = a + x.j0;
+            x.row1 = min(x.row0 + x.n, b);
+            x.steps = (q.p.R + kStep - 1) / kStep;
+        }
+        t += stride;
+        return true;
+    }
+};
+
+template <int CG, int MODE, int OB>
+__global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __grid_constant__ CUtensorMap map_a,
+                                                      const __grid_constant__ CUtensorMap map_b) {
+    constexpr bool A_R = MODE == kForward, B_R = MODE != kGradWeight;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 5];
+    __shared__ uint32_t tmem_at;
+    __shared__ int dead;                     // a wait of this CTA gave up: every role leaves its loop
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CG == 1 ? 0 : (int)(blockIdx.x & 1);
+    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 8 * s; };
+    const auto empty = [&](int s) { return bar0 + 8 * (kMaxStages + s); };
+    const auto acc_full = [&](int b) { return bar0 + 8 * (2 * kMaxStages + b); };
+    const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * kMaxStages + 2 + b); };
+    const uint32_t tail_bar = bar0 + 8 * (2 * kMaxStages + 4);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < q.stages; ++s) {
+            mbar_init(full(s), CG);          // one arrival from each CTA, and the bytes of both
+            mbar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), 4 * CG);
+        }
+        mbar_init(tail_bar, 1);
+        mbar_init_fence();
+        dead = 0;
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_at), kTmemColumns);
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+    volatile int* dead_v = &dead;
+    const int first = (int)blockIdx.x / CG, stride = (int)gridDim.x / CG;
+    Tile x;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ loads
+        Tiles<CG, MODE> tiles(q, first);
+        int s = 0, used = 0;
+        uint32_t ph = 0, tail_ph = 0;
+        bool ok = true;
+        while (ok && tiles.next(x, stride)) {
+            const int half = x.n / CG;       // of the width: this CTA's share
+            const int boxes = MODE == kGradWeight ? half / 64 : (half + kRowBox - 1) / kRowBox;
+            const uint32_t bytes = kOperandA + boxes * (MODE == kGradWeight ? 64 * kStep * 2 : kRowBox * kStep * 2);
+            const int i = x.i0 + rank * 128, j = MODE == kGradWeight ? x.j0 + rank * half : (int)x.row0 + rank * half;
+            for (int k = 0; k < x.steps; ++k) {
+                ok = !*dead_v && (mbar_wait(empty(s), ph ^ 1u) || give_up(40));
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                const uint32_t a = smem + s * q.stage_bytes, b = a + kOperandA;
+                const int left = MODE == kGradWeight ? (int)min(x.row1 - x.row0 - (long long)k * kStep, (long long)kStep) : kStep;
+                // rows to be zeroed: the load counts on this CTA's own barrier, and arrives for the products afterwards
+                const bool tail = MODE == kGradWeight && left % 16 != 0;
+                const uint32_t bar = tail ? tail_bar : CG == 1 ? full(s) : at_leader(full(s));
+                if (lane == 0) {
+                    mbar_arrive_expect(bar, bytes);
+                    const int r = k * kStep;
+                    if (MODE == kForward) {
+                        tma_3d<CG>(a, &map_a, r, i, x.w, bar);
+                    } else if (MODE == kGradInput) {
+                        tma_3d<CG>(a, &map_a, i, r, x.w, bar);
+                        tma_3d<CG>(a + 64 * kStep * 2, &map_a, i + 64, r, x.w, bar);
+                    } else {
+                        tma_2d<CG>(a, &map_a, i, (int)x.row0 + r, bar);
+                        tma_2d<CG>(a + 64 * kStep * 2, &map_a, i + 64, (int)x.row0 + r, bar);
+                    }
+                    for (int c = 0; c < boxes; ++c) {
+                        if (MODE == kGradWeight) tma_2d<CG>(b + c * 64 * kStep * 2, &map_b, j + c * 64, (int)x.row0 + r, bar);
+                        else tma_2d<CG>(b + c * kRowBox * kStep * 2, &map_b, r, j + c * kRowBox, bar);
+                    }
+                }
+                __syncwarp();
+                if (tail) {
+                    ok = mbar_wait(tail_bar, tail_ph) || give_up(41);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    tail_ph ^= 1u;
+                    const int lines = (left + 15) / 16 * 16 - left;
+                    for (int e = lane; e < (2 + boxes) * lines * 8; e += 32) {
+                        const int box = e / (lines * 8), o = e - box * lines * 8;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a + box * 64 * kStep * 2 + left * 128 + o * 16), "r"(0u) : "memory");
+                    }
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(CG == 1 ? full(s) : at_leader(full(s)));
+                    __syncwarp();
+                }
+                if (used < q.stages) ++used;
+                if (++s == q.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+        if (!ok) {
+            // after a wait that gave up nothing tells when the copies under way have landed: far longer than they take
+            *dead_v = 1;
+            for (int k = 0; k < 2000; ++k) __nanosleep(1000);
+        }
+        // No copy may be under way when the CTA leaves: the products of the last `used` stages have freed them.
+        for (int k = 0; k < used && ok; ++k) {
+            if (--s < 0) { s = q.stages - 1; ph ^= 1u; }
+            ok = mbar_wait(empty(s), ph) || give_up(42);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ products
+        if (rank == 0) {
+            Tiles<CG, MODE> tiles(q, first);
+            int s = 0, buf = 0;
+            uint32_t ph = 0, acc_ph = 0;
+            bool ok = true;
+            while (ok && tiles.next(x, stride)) {
+                if (x.steps == 0) continue;
+                ok = mbar_wait(acc_empty(buf), acc_ph ^ 1u) || give_up(43);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t d = tmem + buf * 256, kind = product_kind(128 * CG, x.n, A_R, B_R);
+                for (int k = 0; k < x.steps; ++k) {
+                    ok = !*dead_v && (mbar_wait(full(s), ph) || give_up(44));
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    tc_fence_after();
+                    if (lane == 0) {
+                        const uint32_t a = smem + s * q.stage_bytes, b = a + kOperandA;
+                        const uint64_t da = operand(a, A_R, 64 * kStep * 2), db = operand(b, B_R, 64 * kStep * 2);
+                        const int left = MODE == kGradWeight ? (int)min(x.row1 - x.row0 - (long long)k * kStep, (long long)kStep) : kStep;
+                        for (int c = 0; c * 16 < left; ++c)
+                            mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, k + c > 0);
+                        mma_commit<CG>(empty(s));
+                        if (k + 1 == x.steps) mma_commit<CG>(acc_full(buf));
+                    }
+                    __syncwarp();
+                    if (++s == q.stages) { s = 0; ph ^= 1u; }
+                }
+                if (++buf == 2) { buf = 0; acc_ph ^= 1u; }
+            }
+            if (!ok) *dead_v = 1;
+        }
+    } else {
+        // ------------------------------------------------------------ results
+        Tiles<CG, MODE> tiles(q, first);
+        const int quarter = warp & 3;        // a warp reads the 32 lanes of TMEM that its number allows
+        float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + q.stages * q.stage_bytes + quarter * kTurn);
+        int buf = 0;
+        uint32_t acc_ph = 0;
+        bool ok = true;
+        while (ok && tiles.next(x, stride)) {
+            const int i = x.i0 + rank * 128 + quarter * 32;
+            const bool any = x.steps > 0;
+            if (any) {
+                ok = !*dead_v && (mbar_wait(acc_full(buf), acc_ph) || give_up(45));
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc_fence_after();
+            }
+            unsigned char* c = MODE == kGradWeight ? q.p.c + x.w * q.p.stride * OB : q.p.c;
+            const int wide = MODE == kGradWeight ? min(x.n, q.p.J - x.j0) : (int)(x.row1 - x.row0);
+            if (i < q.p.I) {
+                for (int c0 = 0; c0 < wide; c0 += 32) {
+                    uint32_t v[32];
+                    if (any) {
+                        tmem_load32(tmem + buf * 256 + c0 + ((uint32_t)(quarter * 32) << 16), v);
+                        tmem_load_wait();
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0u;
+                    }
+                    // 33 floats to a line: neither the writes nor the reads meet on a bank
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) turn[MODE == kGradWeight ? lane * 33 + e : e * 33 + lane] = __uint_as_float(v[e]);
+                    __syncwarp();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int line = e * 8 + (lane >> 2), col = (lane & 3) * 8;
+                        float o[8];
+#pragma unroll
+                        for (int f = 0; f < 8; ++f) o[f] = turn[line * 33 + col + f];
+                        long long row;
+                        int at, end;
+                        bool in;
+                        if (MODE == kGradWeight) {
+                            row = i + line;
+                            in = row < q.p.I;
+                            at = x.j0 + c0 + col;
+                            end = q.p.J;
+                        } else {
+                            row = x.row0 + c0 + line;
+                            in = row < x.row1;
+                            at = i + col;
+                            end = q.p.I;
+                        }
+                        if (in) {
+                            unsigned char* to = c + (row * q.p.c_pitch + at) * OB;
+                            if (q.p.c_vec && at + 8 <= end) {
+                                if constexpr (OB == 2) {
+                                    *reinterpret_cast<uint4*>(to) = Elem<2>::pack(o);
+                                } else {
+                                    *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+                                    *reinterpret_cast<float4*>(to + 16) = make_float4(o[4], o[5], o[6], o[7]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int f = 0; f < 8; ++f)
+                                    if (at + f < end) Elem<OB>::put(to + f * OB, o[f]);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            if (any) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(CG == 1 ? acc_empty(buf) : at_leader(acc_empty(buf)));
+                if (++buf == 2) { buf = 0; acc_ph ^= 1u; }
+            }
+        }
+        if (!ok) *dead_v = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
+    tc_fence_after();
+    if (warp == 1) tmem_release<CG>(tmem, kTmemColumns);
+}
+
 // ---------------------------------------------------------------- host
 template <int EB, int OB> cudaError_t launch_fma(const Product& p, int mode, cudaStream_t st) {
     const unsigned cols = (unsigned)((p.J + kFT - 1) / kFT);
@@ -203,6 +543,76 @@ template <int EB, int OB> cudaError_t launch_fma(const Product& p, int mode, cud
         else k_fma<EB, OB, kGradInput><<<grid, kFThreads, 0, st>>>(p);
     }
     return cudaGetLastError();
+}
+
+// Tensor map of bfloat16 rows, boxes of 64 elements x `box` rows; layers = 0: rows alone, else that many, `stride` apart.
+bool encode(CUtensorMap* map, const void* base, long long width, long long rows, long long pitch, int layers, long long stride, int box) {
+    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)layers};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(stride ? stride : 8) * 2};
+    const cuuint32_t boxes[3] = {kStep, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+    return combo_host::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, layers ? 3 : 2, const_cast<void*>(base), dims, strides, boxes,
+                                    ones, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int CG, int MODE> cudaError_t launch_tc_inst(const TcParams& q, const CUtensorMap& a, const CUtensorMap& b, int out_bytes, int grid,
+                                                       cudaStream_t st) {
+    auto kern = out_bytes == 2 ? k_tc<CG, MODE, 2> : k_tc<CG, MODE, 4>;
+    const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + 4 * kTurn;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, q, a, b);
+}
+
+template <int CG> combo_status launch_tc(const Product& p, int mode, int out_bytes, int sms, int smem_optin, cudaStream_t st) {
+    TcParams q = {p, 256, 0, 0};
+    // the height is W's (forward: n_out, rows' gradient: n_in) or n_out; see the table above
+    const long long mt = (p.I + 128 * CG - 1) / (128 * CG);
+    long long tiles;
+    if (mode == kGradWeight) {
+        const int least = 64 * CG;
+        while (q.width > least && (q.width / 2 >= p.J || mt * ((p.J + q.width - 1) / q.width) * p.N * CG < sms)) q.width /= 2;
+        tiles = mt * ((p.J + q.width - 1) / q.width) * p.N;
+    } else {
+        // the host knows the workers' rows on average only
+        const long long mean = (p.M + p.N - 1) / p.N;
+        const auto count = [&](int width) { return mt * p.N * ((mean + width - 1) / width); };
+        while (q.width > 32 * CG && (q.width >= 4 * mean || count(q.width) * CG < sms)) q.width /= 2;
+        tiles = mt * (p.M / q.width + (p.N < p.M ? p.N : p.M));
+    }
+    if (tiles > 0x40000000LL) return COMBO_ERR_INVALID_ARG;
+    const int half = q.width / CG;
+    q.stage_bytes = kOperandA + (half > kRowBox ? half : kRowBox) * kStep * 2;
+    q.stages = (smem_optin - 2048 - 4 * kTurn) / q.stage_bytes;
+    if (q.stages > kMaxStages) q.stages = kMaxStages;
+    int grid = sms / CG * CG;
+    if (tiles * CG < grid) grid = (int)tiles * CG;
+    if (grid < CG) grid = CG;
+    CUtensorMap a, b;
+    bool fine;
+    // p.a: the rows' operand of the first kind (X, dY, dY), p.b: W, W, X
+    if (mode == kForward)
+        fine = encode(&a, p.b, p.R, p.I, p.b_pitch, p.N, p.stride, 128) && encode(&b, p.a, p.R, p.M, p.a_pitch, 0, 0, kRowBox);
+    else if (mode == kGradInput)
+        fine = encode(&a, p.b, p.I, p.R, p.b_pitch, p.N, p.stride, 64) && encode(&b, p.a, p.R, p.M, p.a_pitch, 0, 0, kRowBox);
+    else
+        fine = encode(&a, p.a, p.I, p.M, p.a_pitch, 0, 0, 64) && encode(&b, p.b, p.J, p.M, p.b_pitch, 0, 0, 64);
+    if (!fine) return COMBO_ERR_CUDA;
+    cudaError_t e;
+    if (mode == kForward) e = launch_tc_inst<CG, kForward>(q, a, b, out_bytes, grid, st);
+    else if (mode == kGradInput) e = launch_tc_inst<CG, kGradInput>(q, a, b, out_bytes, grid, st);
+    else e = launch_tc_inst<CG, kGradWeight>(q, a, b, out_bytes, grid, st);
+    return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "grouped product launch");
 }
 
 bool vec_ok(const void* p, int64_t pitch, int64_t stride, int eb) {
@@ -273,6 +683,11 @@ combo_status product(int mode, const void* rows1, int64_t pitch1, const void* ro
         p.R = (int)width1;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (elem_bytes == 2 && p.a_vec && p.b_vec && (mode == kGradWeight ? M > 0 : true)) {
+        Product t = p;
+        if (mode != kGradWeight) t.I = p.J;      // the weights' index is the height there
+        return launch_tc<1>(t, mode, out_bytes, sms, smem, st);
+    }
     cudaError_t e;
     if (elem_bytes == 4) e = launch_fma<4, 4>(p, mode, st);
     else if (out_bytes == 2) e = launch_fma<2, 2>(p, mode, st);
@@ -281,6 +696,17 @@ combo_status product(int mode, const void* rows1, int64_t pitch1, const void* ro
 }
 
 }  // namespace
+
+namespace combo_host {
+
+cudaError_t grouped_linear_status(int* code) {
+    const int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(code, g_linear_status, sizeof(int));
+    if (e == cudaSuccess && *code != 0) e = cudaMemcpyToSymbol(g_linear_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace combo_host
 
 extern "C" {
 

@@ -1,5 +1,6 @@
 // What the translation units of libcombo_b200.so share on the host side.  Defined in combo_b200.cu.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -12,6 +13,12 @@ namespace combo_host {
 combo_status fail(cudaError_t e, const char* what);
 // The current device's SM count and largest shared memory of a block; COMBO_ERR_UNSUPPORTED unless it is 10.x.
 combo_status device(int* sms, int* smem_optin);
+// Status word of the grouped products' kernels (see combo_device_status): reads it, and clears it if it is set.
+cudaError_t grouped_linear_status(int* code);
+// cuTensorMapEncodeTiled without interleaving, out-of-bounds elements read as zero; false (and a text for
+// combo_last_cuda_error()) if it is missing or refuses.
+bool encode_tiled(CUtensorMap* map, CUtensorMapDataType type, int rank, void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+                  const cuuint32_t* box, const cuuint32_t* elem_strides, CUtensorMapSwizzle swizzle);
 #pragma GCC visibility pop
 
 inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
