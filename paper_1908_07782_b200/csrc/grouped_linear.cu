@@ -10,6 +10,8 @@
 //   forward           m (ragged)   n           k        both operands contiguous along r
 //   gradient, rows    m (ragged)   k           n        A along r, B along j
 //   gradient, weights n            k           m (ragged)   both along i / j
+#include <string.h>
+
 #include "host_common.h"
 #include "step_common.cuh"
 #include "tensor_core.cuh"
@@ -200,11 +202,11 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
 //   grad rows  k: W, along i                  rows: dY, along r          n
 //   grad w.    n: dY, along i                 k: X, along j              rows (ragged)
 //
-// Persistent CTAs; a warp that issues TMA loads into a ring of stages of 64 values of r, a warp that issues the
-// products, four warps that take finished accumulators out of TMEM (two of them there, 256 columns each, so that the
-// next tile's products run meanwhile), turn them through shared memory and store them.  The last rows of a worker in
-// the gradient of the weights: what the load brought beyond them is zeroed in shared memory before the products see
-// it (another worker's NaN would not vanish by being multiplied with zero).
+// Persistent CTAs; two warps that issue TMA loads, one for either operand, into a ring of stages of 64 values of r, a
+// warp that issues the products, four warps that take finished accumulators out of TMEM (two of them there, 256 columns
+// each, so that the next tile's products run meanwhile), turn them through shared memory and store them.  The last rows
+// of a worker in the gradient of the weights: what the load brought beyond them is zeroed in shared memory before the
+// products see it, by a warp of its own (another worker's NaN would not vanish by being multiplied with zero).
 using namespace combo_tc;
 
 __device__ int g_linear_status;              // 0, or the site of the first wait that gave up
@@ -213,10 +215,12 @@ __device__ __forceinline__ bool give_up(int site) {
     return false;
 }
 
-constexpr int kTcThreads = 192;
+constexpr int kOutWarps = 4;                 // one for each quarter of TMEM's lanes (eight were no faster)
+constexpr int kFirstOutWarp = 4;
+constexpr int kTcThreads = 32 * (kFirstOutWarp + kOutWarps);
 constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kOperandA = 128 * kStep * 2;   // bytes of the height's operand in a stage
-constexpr int kRowBox = 32;                  // rows in a box of X or dY
+constexpr int kRowBoxes = 4;                 // boxes of 32, 64, 128 or 256 rows of X or dY
 constexpr int kMaxStages = 8;
 constexpr int kTurn = 32 * 33 * 4;           // bytes in which an epilogue warp turns 32 x 32 outputs
 constexpr int kTmemColumns = 512;
@@ -225,6 +229,11 @@ struct TcParams {
     Product p;
     int width;                               // widest tile along j
     int stages, stage_bytes;
+    int a_blocks, b_blocks;                  // whether an operand along i or j comes by a map of blocks of 64, in one copy; else a copy a block
+};
+// Tensor maps: the height's operand; the width's, by the rows of a box (one map in the gradient of the weights)
+struct alignas(64) TcMaps {
+    CUtensorMap a, b[kRowBoxes];
 };
 
 // One tile of the grid's work, and how far the ring has gone.
@@ -296,37 +305,48 @@ template <int CG, int MODE> struct Tiles {
     }
 };
 
+// Zeroes lines [left, next multiple of 16) of `blocks` blocks of 64 lines of 128 bytes; a warp.
+__device__ __forceinline__ void zero_tail(uint32_t at, int blocks, int left, int lane) {
+    const int words = ((left + 15) / 16 * 16 - left) * 8;
+    for (int e = lane; e < blocks * words; e += 32) {
+        const int block = e / words, o = e - block * words;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + block * 64 * kStep * 2 + left * 128 + o * 16), "r"(0u) : "memory");
+    }
+    fence_async();
+    __syncwarp();
+}
+
 template <int CG, int MODE, int OB>
-__global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __grid_constant__ CUtensorMap map_a,
-                                                      const __grid_constant__ CUtensorMap map_b) {
+__global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __grid_constant__ TcMaps maps) {
     constexpr bool A_R = MODE == kForward, B_R = MODE != kGradWeight;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 5];
+    __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 4];
     __shared__ uint32_t tmem_at;
     __shared__ int dead;                     // a wait of this CTA gave up: every role leaves its loop
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x & 1);
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8 * s; };
     const auto empty = [&](int s) { return bar0 + 8 * (kMaxStages + s); };
-    const auto acc_full = [&](int b) { return bar0 + 8 * (2 * kMaxStages + b); };
-    const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * kMaxStages + 2 + b); };
-    const uint32_t tail_bar = bar0 + 8 * (2 * kMaxStages + 4);
+    const auto tail = [&](int s) { return bar0 + 8 * (2 * kMaxStages + s); };
+    const auto peer_zeroed = [&](int s) { return bar0 + 8 * (3 * kMaxStages + s); };
+    const auto acc_full = [&](int b) { return bar0 + 8 * (4 * kMaxStages + b); };
+    const auto acc_empty = [&](int b) { return bar0 + 8 * (4 * kMaxStages + 2 + b); };
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.stages; ++s) {
-            mbar_init(full(s), CG);          // one arrival from each CTA, and the bytes of both
+            mbar_init(full(s), 2);           // one arrival for either operand, and the bytes of all CTAs
             mbar_init(empty(s), 1);
+            mbar_init(tail(s), 2);
+            mbar_init(peer_zeroed(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
-            mbar_init(acc_empty(b), 4 * CG);
+            mbar_init(acc_empty(b), kOutWarps * CG);
         }
-        mbar_init(tail_bar, 1);
         mbar_init_fence();
         dead = 0;
-        prefetch_map(&map_a);
-        prefetch_map(&map_b);
+        prefetch_map(&maps.a);
     }
     if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_at), kTmemColumns);
     tc_fence_before();
@@ -341,168 +361,195 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
     const int first = (int)blockIdx.x / CG, stride = (int)gridDim.x / CG;
     Tile x;
 
-    if (warp == 0) {
-        // ------------------------------------------------------------ loads
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------ loads: warp 0 the height's operand, warp 2 the width's
+        const int operand = warp == 0 ? 0 : 1;
         Tiles<CG, MODE> tiles(q, first);
-        int s = 0, used = 0;
-        uint32_t ph = 0, tail_ph = 0;
+        uint32_t done = 0;                   // stages issued
         bool ok = true;
-        while (ok && tiles.next(x, stride)) {
+        while (tiles.next(x, stride)) {
             const int half = x.n / CG;       // of the width: this CTA's share
-            const int boxes = MODE == kGradWeight ? half / 64 : (half + kRowBox - 1) / kRowBox;
-            const uint32_t bytes = kOperandA + boxes * (MODE == kGradWeight ? 64 * kStep * 2 : kRowBox * kStep * 2);
-            const int i = x.i0 + rank * 128, j = MODE == kGradWeight ? x.j0 + rank * half : (int)x.row0 + rank * half;
-            for (int k = 0; k < x.steps; ++k) {
-                ok = !*dead_v && (mbar_wait(empty(s), ph ^ 1u) || give_up(40));
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                const uint32_t a = smem + s * q.stage_bytes, b = a + kOperandA;
-                const int left = MODE == kGradWeight ? (int)min(x.row1 - x.row0 - (long long)k * kStep, (long long)kStep) : kStep;
-                // rows to be zeroed: the load counts on this CTA's own barrier, and arrives for the products afterwards
-                const bool tail = MODE == kGradWeight && left % 16 != 0;
-                const uint32_t bar = tail ? tail_bar : CG == 1 ? full(s) : at_leader(full(s));
-                if (lane == 0) {
-                    mbar_arrive_expect(bar, bytes);
-                    const int r = k * kStep;
-                    if (MODE == kForward) {
-                        tma_3d<CG>(a, &map_a, r, i, x.w, bar);
-                    } else if (MODE == kGradInput) {
-                        tma_3d<CG>(a, &map_a, i, r, x.w, bar);
-                        tma_3d<CG>(a + 64 * kStep * 2, &map_a, i + 64, r, x.w, bar);
-                    } else {
-                        tma_2d<CG>(a, &map_a, i, (int)x.row0 + r, bar);
-                        tma_2d<CG>(a + 64 * kStep * 2, &map_a, i + 64, (int)x.row0 + r, bar);
-                    }
-                    for (int c = 0; c < boxes; ++c) {
-                        if (MODE == kGradWeight) tma_2d<CG>(b + c * 64 * kStep * 2, &map_b, j + c * 64, (int)x.row0 + r, bar);
-                        else tma_2d<CG>(b + c * kRowBox * kStep * 2, &map_b, r, j + c * kRowBox, bar);
-                    }
-                }
-                __syncwarp();
-                if (tail) {
-                    ok = mbar_wait(tail_bar, tail_ph) || give_up(41);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    tail_ph ^= 1u;
-                    const int lines = (left + 15) / 16 * 16 - left;
-                    for (int e = lane; e < (2 + boxes) * lines * 8; e += 32) {
-                        const int box = e / (lines * 8), o = e - box * lines * 8;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a + box * 64 * kStep * 2 + left * 128 + o * 16), "r"(0u) : "memory");
-                    }
-                    fence_async();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(CG == 1 ? full(s) : at_leader(full(s)));
-                    __syncwarp();
-                }
-                if (used < q.stages) ++used;
-                if (++s == q.stages) { s = 0; ph ^= 1u; }
+            int bytes = kOperandA;           // of a stage
+            const CUtensorMap* map = &maps.a;
+            const bool blocks = operand == 0 ? q.a_blocks : q.b_blocks;
+            if (operand == 1 && MODE == kGradWeight) {
+                bytes = half * kStep * 2;
+                map = &maps.b[0];
+            } else if (operand == 1) {
+                const int m = half <= 32 ? 0 : half <= 64 ? 1 : half <= 128 ? 2 : 3;
+                bytes = (32 << m) * kStep * 2;
+                map = &maps.b[m];
             }
+            const int at = operand == 0 ? x.i0 + rank * 128 : MODE == kGradWeight ? x.j0 + rank * half : (int)x.row0 + rank * half;
+            // the last rows, if some of a 16 are another's: that load counts on a barrier of this CTA alone, and the warp
+            // that zeroes the others arrives for it
+            const int rest = MODE == kGradWeight ? (int)((x.row1 - x.row0) % kStep) : 0;
+            const int plain = rest % 16 != 0 ? x.steps - 1 : x.steps;
+            uint32_t s = done % q.stages, ph = done / q.stages & 1u;
+            const auto load = [&](int k, uint32_t bar) {
+                const int r = MODE == kGradWeight ? (int)x.row0 + k * kStep : k * kStep;
+                const uint32_t to = smem + s * q.stage_bytes + operand * kOperandA;
+                if (operand == 0 && MODE == kForward) tma_3d<CG>(to, map, r, at, x.w, bar);
+                else if (operand == 1 && MODE != kGradWeight) tma_2d<CG>(to, map, r, at, bar);
+                else if (blocks && MODE == kGradInput) tma_4d<CG>(to, map, 0, r, at / 64, x.w, bar);
+                else if (blocks) tma_3d<CG>(to, map, 0, r, at / 64, bar);
+                else
+                    for (int c = 0; c * 64 * kStep * 2 < bytes; ++c) {
+                        if (MODE == kGradInput) tma_3d<CG>(to + c * 64 * kStep * 2, map, at + c * 64, r, x.w, bar);
+                        else tma_2d<CG>(to + c * 64 * kStep * 2, map, at + c * 64, r, bar);
+                    }
+            };
+            if (elect()) {
+                for (int k = 0; k < x.steps; ++k) {
+                    if (!mbar_wait(empty(s), ph ^ 1u, dead_v)) { ok = give_up(40); break; }
+                    if (k == plain) {
+                        mbar_arrive_expect(tail(s), bytes);
+                        load(k, tail(s));
+                    } else {
+                        // the leader expects the bytes of both CTAs; the other one's may come before
+                        if (rank == 0) mbar_arrive_expect(full(s), bytes * CG);
+                        load(k, CG == 1 ? full(s) : at_leader(full(s)));
+                    }
+                    if (++s == q.stages) { s = 0; ph ^= 1u; }
+                }
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            done += x.steps;
         }
         if (!ok) {
             // after a wait that gave up nothing tells when the copies under way have landed: far longer than they take
             *dead_v = 1;
             for (int k = 0; k < 2000; ++k) __nanosleep(1000);
         }
-        // No copy may be under way when the CTA leaves: the products of the last `used` stages have freed them.
-        for (int k = 0; k < used && ok; ++k) {
-            if (--s < 0) { s = q.stages - 1; ph ^= 1u; }
-            ok = mbar_wait(empty(s), ph) || give_up(42);
-        }
+        // No copy may be under way when the CTA leaves: the products have freed the last stages.
+        for (uint32_t k = 1; k <= done && k <= (uint32_t)q.stages && ok; ++k)
+            ok = mbar_wait(empty((done - k) % q.stages), (done - k) / q.stages & 1u, dead_v) || give_up(43);
     } else if (warp == 1) {
-        // ------------------------------------------------------------ products
+        // ------------------------------------------------------------ products, by one thread of the leader
         if (rank == 0) {
             Tiles<CG, MODE> tiles(q, first);
-            int s = 0, buf = 0;
-            uint32_t ph = 0, acc_ph = 0;
+            uint32_t done = 0, accs = 0, zeroed = 0;     // `zeroed`: parities of peer_zeroed, of the issuing thread
             bool ok = true;
-            while (ok && tiles.next(x, stride)) {
+            while (tiles.next(x, stride)) {
                 if (x.steps == 0) continue;
-                ok = mbar_wait(acc_empty(buf), acc_ph ^ 1u) || give_up(43);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t d = tmem + buf * 256, kind = product_kind(128 * CG, x.n, A_R, B_R);
-                for (int k = 0; k < x.steps; ++k) {
-                    ok = !*dead_v && (mbar_wait(full(s), ph) || give_up(44));
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                const uint32_t buf = accs & 1u;
+                const int rest = MODE == kGradWeight ? (int)((x.row1 - x.row0) % kStep) : 0;
+                if (elect()) {
+                    const uint32_t d = tmem + buf * 256, kind = product_kind(128 * CG, x.n, A_R, B_R);
+                    uint32_t s = done % q.stages, ph = done / q.stages & 1u;
+                    ok = mbar_wait(acc_empty(buf), (accs >> 1 & 1u) ^ 1u, dead_v) || give_up(44);
                     tc_fence_after();
-                    if (lane == 0) {
-                        const uint32_t a = smem + s * q.stage_bytes, b = a + kOperandA;
-                        const uint64_t da = operand(a, A_R, 64 * kStep * 2), db = operand(b, B_R, 64 * kStep * 2);
-                        const int left = MODE == kGradWeight ? (int)min(x.row1 - x.row0 - (long long)k * kStep, (long long)kStep) : kStep;
-                        for (int c = 0; c * 16 < left; ++c)
-                            mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, k + c > 0);
+                    for (int k = 0; k < x.steps && ok; ++k) {
+                        if (!mbar_wait(full(s), ph, dead_v)) { ok = give_up(45); break; }
+                        const bool last = k + 1 == x.steps;
+                        if (MODE == kGradWeight && last && rest % 16 != 0) {
+                            if (CG == 2 && !mbar_wait(peer_zeroed(s), zeroed >> s & 1u, dead_v)) { ok = give_up(46); break; }
+                            zeroed ^= 1u << s;
+                            fence_cluster();         // threads of both CTAs have written zeros
+                        }
+                        tc_fence_after();
+                        const uint32_t a = smem + s * q.stage_bytes;
+                        const uint64_t da = operand(a, A_R, 64 * kStep * 2), db = operand(a + kOperandA, B_R, 64 * kStep * 2);
+                        if (MODE == kGradWeight && last && rest != 0) {
+                            for (int c = 0; c * 16 < rest; ++c)
+                                mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, k + c > 0);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < kStep / 16; ++c)
+                                mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, k + c > 0);
+                        }
                         mma_commit<CG>(empty(s));
-                        if (k + 1 == x.steps) mma_commit<CG>(acc_full(buf));
+                        if (++s == q.stages) { s = 0; ph ^= 1u; }
                     }
-                    __syncwarp();
-                    if (++s == q.stages) { s = 0; ph ^= 1u; }
+                    if (ok) mma_commit<CG>(acc_full(buf));
                 }
-                if (++buf == 2) { buf = 0; acc_ph ^= 1u; }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                done += x.steps;
+                ++accs;
             }
             if (!ok) *dead_v = 1;
         }
-    } else {
+    } else if (warp == 3) {
+        // ------------------------------------------------------------ rows of others, zeroed
+        if (MODE == kGradWeight) {
+            Tiles<CG, MODE> tiles(q, first);
+            uint32_t done = 0, parity = 0;
+            bool ok = true;
+            while (tiles.next(x, stride)) {
+                const int rest = (int)((x.row1 - x.row0) % kStep);
+                done += x.steps;
+                if (rest % 16 == 0) continue;
+                const uint32_t s = (done - 1) % q.stages;
+                ok = mbar_wait(tail(s), parity >> s & 1u, dead_v) || give_up(41);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                parity ^= 1u << s;
+                zero_tail(smem + s * q.stage_bytes, 2 + x.n / CG / 64, rest, lane);
+                if (elect()) {
+                    if (rank == 0) {
+                        mbar_arrive(full(s));
+                        mbar_arrive(full(s));
+                    } else {
+                        mbar_arrive_release(at_leader(peer_zeroed(s)));
+                    }
+                }
+                __syncwarp();
+            }
+            if (!ok) *dead_v = 1;
+        }
+    } else if (warp >= kFirstOutWarp) {
         // ------------------------------------------------------------ results
         Tiles<CG, MODE> tiles(q, first);
         const int quarter = warp & 3;        // a warp reads the 32 lanes of TMEM that its number allows
         float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + q.stages * q.stage_bytes + quarter * kTurn);
-        int buf = 0;
-        uint32_t acc_ph = 0;
+        uint32_t accs = 0;
         bool ok = true;
-        while (ok && tiles.next(x, stride)) {
+        while (tiles.next(x, stride)) {
+            const uint32_t buf = accs & 1u;
             const int i = x.i0 + rank * 128 + quarter * 32;
             const bool any = x.steps > 0;
             if (any) {
-                ok = !*dead_v && (mbar_wait(acc_full(buf), acc_ph) || give_up(45));
+                ok = mbar_wait(acc_full(buf), accs >> 1 & 1u, dead_v) || give_up(47);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_fence_after();
             }
             unsigned char* c = MODE == kGradWeight ? q.p.c + x.w * q.p.stride * OB : q.p.c;
             const int wide = MODE == kGradWeight ? min(x.n, q.p.J - x.j0) : (int)(x.row1 - x.row0);
             if (i < q.p.I) {
+                // lots of 32 columns; the next lot's load is under way while this one is stored
+                const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16);
+                uint32_t next[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) next[e] = 0u;
+                if (any) tmem_load32(acc, next);
                 for (int c0 = 0; c0 < wide; c0 += 32) {
                     uint32_t v[32];
-                    if (any) {
-                        tmem_load32(tmem + buf * 256 + c0 + ((uint32_t)(quarter * 32) << 16), v);
-                        tmem_load_wait();
-                    } else {
+                    if (any) tmem_load_wait(next);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = 0u;
-                    }
+                    for (int e = 0; e < 32; ++e) v[e] = next[e];
+                    if (any && c0 + 32 < wide) tmem_load32(acc + c0 + 32, next);
                     // 33 floats to a line: neither the writes nor the reads meet on a bank
 #pragma unroll
                     for (int e = 0; e < 32; ++e) turn[MODE == kGradWeight ? lane * 33 + e : e * 33 + lane] = __uint_as_float(v[e]);
                     __syncwarp();
+                    // a lane stores 16 bytes, neighbours what lies beside it
+                    constexpr int kLane = 16 / OB, kPerLine = 32 / kLane;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int line = e * 8 + (lane >> 2), col = (lane & 3) * 8;
-                        float o[8];
+                    for (int e = 0; e < kPerLine; ++e) {
+                        const int line = e * (32 / kPerLine) + lane / kPerLine, col = lane % kPerLine * kLane;
+                        float o[kLane];
 #pragma unroll
-                        for (int f = 0; f < 8; ++f) o[f] = turn[line * 33 + col + f];
-                        long long row;
-                        int at, end;
-                        bool in;
-                        if (MODE == kGradWeight) {
-                            row = i + line;
-                            in = row < q.p.I;
-                            at = x.j0 + c0 + col;
-                            end = q.p.J;
-                        } else {
-                            row = x.row0 + c0 + line;
-                            in = row < x.row1;
-                            at = i + col;
-                            end = q.p.I;
-                        }
-                        if (in) {
+                        for (int f = 0; f < kLane; ++f) o[f] = turn[line * 33 + col + f];
+                        const long long row = MODE == kGradWeight ? i + line : x.row0 + c0 + line;
+                        const int at = MODE == kGradWeight ? x.j0 + c0 + col : i + col, end = MODE == kGradWeight ? q.p.J : q.p.I;
+                        if (row < (MODE == kGradWeight ? (long long)q.p.I : x.row1)) {
                             unsigned char* to = c + (row * q.p.c_pitch + at) * OB;
-                            if (q.p.c_vec && at + 8 <= end) {
-                                if constexpr (OB == 2) {
-                                    *reinterpret_cast<uint4*>(to) = Elem<2>::pack(o);
-                                } else {
-                                    *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
-                                    *reinterpret_cast<float4*>(to + 16) = make_float4(o[4], o[5], o[6], o[7]);
-                                }
+                            if (q.p.c_vec && at + kLane <= end) {
+                                *reinterpret_cast<uint4*>(to) = Elem<OB>::pack(o);
                             } else {
 #pragma unroll
-                                for (int f = 0; f < 8; ++f)
+                                for (int f = 0; f < kLane; ++f)
                                     if (at + f < end) Elem<OB>::put(to + f * OB, o[f]);
                             }
                         }
@@ -514,7 +561,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(CG == 1 ? acc_empty(buf) : at_leader(acc_empty(buf)));
-                if (++buf == 2) { buf = 0; acc_ph ^= 1u; }
+                ++accs;
             }
         }
         if (!ok) *dead_v = 1;
@@ -545,19 +592,29 @@ template <int EB, int OB> cudaError_t launch_fma(const Product& p, int mode, cud
     return cudaGetLastError();
 }
 
-// Tensor map of bfloat16 rows, boxes of 64 elements x `box` rows; layers = 0: rows alone, else that many, `stride` apart.
-bool encode(CUtensorMap* map, const void* base, long long width, long long rows, long long pitch, int layers, long long stride, int box) {
-    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)layers};
-    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(stride ? stride : 8) * 2};
-    const cuuint32_t boxes[3] = {kStep, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
-    return combo_host::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, layers ? 3 : 2, const_cast<void*>(base), dims, strides, boxes,
-                                    ones, CU_TENSOR_MAP_SWIZZLE_128B);
+// Tensor map of bfloat16 rows, `pitch` apart, in `layers` lots `stride` apart (0: none); boxes of 64 elements by `rows_box`
+// rows.  blocks > 0: boxes of that many times 64 elements, laid out block after block (width a multiple of 64).
+bool encode(CUtensorMap* map, const void* base, long long width, long long rows, long long pitch, int layers, long long stride,
+            int rows_box, int blocks) {
+    cuuint64_t dims[4], strides[3];
+    cuuint32_t box[4], ones[4] = {1, 1, 1, 1};
+    int n = 0;
+    const auto add = [&](long long dim, long long step, int b) {
+        dims[n] = (cuuint64_t)dim;
+        if (n > 0) strides[n - 1] = (cuuint64_t)step * 2;
+        box[n++] = (cuuint32_t)b;
+    };
+    add(blocks ? kStep : width, 1, kStep);
+    add(rows, pitch, rows_box);
+    if (blocks) add(width / kStep, kStep, blocks);
+    if (layers) add(layers, stride ? stride : 8, 1);
+    return combo_host::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n, const_cast<void*>(base), dims, strides, box, ones,
+                                    CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int CG, int MODE> cudaError_t launch_tc_inst(const TcParams& q, const CUtensorMap& a, const CUtensorMap& b, int out_bytes, int grid,
-                                                       cudaStream_t st) {
+template <int CG, int MODE> cudaError_t launch_tc_inst(const TcParams& q, const TcMaps& maps, int out_bytes, int grid, cudaStream_t st) {
     auto kern = out_bytes == 2 ? k_tc<CG, MODE, 2> : k_tc<CG, MODE, 4>;
-    const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + 4 * kTurn;
+    const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOutWarps * kTurn;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -571,11 +628,11 @@ template <int CG, int MODE> cudaError_t launch_tc_inst(const TcParams& q, const 
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CG > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, q, a, b);
+    return cudaLaunchKernelEx(&cfg, kern, q, maps);
 }
 
 template <int CG> combo_status launch_tc(const Product& p, int mode, int out_bytes, int sms, int smem_optin, cudaStream_t st) {
-    TcParams q = {p, 256, 0, 0};
+    TcParams q = {p, 256, 0, 0, 0, 0};
     // the height is W's (forward: n_out, rows' gradient: n_in) or n_out; see the table above
     const long long mt = (p.I + 128 * CG - 1) / (128 * CG);
     long long tiles;
@@ -592,26 +649,35 @@ template <int CG> combo_status launch_tc(const Product& p, int mode, int out_byt
     }
     if (tiles > 0x40000000LL) return COMBO_ERR_INVALID_ARG;
     const int half = q.width / CG;
-    q.stage_bytes = kOperandA + (half > kRowBox ? half : kRowBox) * kStep * 2;
-    q.stages = (smem_optin - 2048 - 4 * kTurn) / q.stage_bytes;
+    q.stage_bytes = kOperandA + half * kStep * 2;
+    q.stages = (smem_optin - 2048 - kOutWarps * kTurn) / q.stage_bytes;
     if (q.stages > kMaxStages) q.stages = kMaxStages;
     int grid = sms / CG * CG;
     if (tiles * CG < grid) grid = (int)tiles * CG;
     if (grid < CG) grid = CG;
-    CUtensorMap a, b;
-    bool fine;
-    // p.a: the rows' operand of the first kind (X, dY, dY), p.b: W, W, X
-    if (mode == kForward)
-        fine = encode(&a, p.b, p.R, p.I, p.b_pitch, p.N, p.stride, 128) && encode(&b, p.a, p.R, p.M, p.a_pitch, 0, 0, kRowBox);
-    else if (mode == kGradInput)
-        fine = encode(&a, p.b, p.I, p.R, p.b_pitch, p.N, p.stride, 64) && encode(&b, p.a, p.R, p.M, p.a_pitch, 0, 0, kRowBox);
-    else
-        fine = encode(&a, p.a, p.I, p.M, p.a_pitch, 0, 0, 64) && encode(&b, p.b, p.J, p.M, p.b_pitch, 0, 0, 64);
+    TcMaps maps;
+    memset(&maps, 0, sizeof(maps));
+    bool fine = true;
+    // p.a: the rows' operand of the first kind (X, dY, dY), p.b: W, W, X.  An operand along i or j comes in blocks of 64: in
+    // one copy where its width is a multiple of that, else (a block would run into the next row) in one copy a block
+    if (mode == kForward) {
+        fine = encode(&maps.a, p.b, p.R, p.I, p.b_pitch, p.N, p.stride, 128, 0);
+    } else if (mode == kGradInput) {
+        q.a_blocks = p.I % kStep == 0;
+        fine = encode(&maps.a, p.b, p.I, p.R, p.b_pitch, p.N, p.stride, kStep, q.a_blocks ? 2 : 0);
+    } else {
+        q.a_blocks = p.I % kStep == 0;
+        q.b_blocks = p.J % kStep == 0;
+        fine = encode(&maps.a, p.a, p.I, p.M, p.a_pitch, 0, 0, kStep, q.a_blocks ? 2 : 0) &&
+               encode(&maps.b[0], p.b, p.J, p.M, p.b_pitch, 0, 0, kStep, q.b_blocks ? half / kStep : 0);
+    }
+    for (int m = 0; mode != kGradWeight && m < kRowBoxes && (32 << m) <= half && fine; ++m)
+        fine = encode(&maps.b[m], p.a, p.R, p.M, p.a_pitch, 0, 0, 32 << m, 0);
     if (!fine) return COMBO_ERR_CUDA;
     cudaError_t e;
-    if (mode == kForward) e = launch_tc_inst<CG, kForward>(q, a, b, out_bytes, grid, st);
-    else if (mode == kGradInput) e = launch_tc_inst<CG, kGradInput>(q, a, b, out_bytes, grid, st);
-    else e = launch_tc_inst<CG, kGradWeight>(q, a, b, out_bytes, grid, st);
+    if (mode == kForward) e = launch_tc_inst<CG, kForward>(q, maps, out_bytes, grid, st);
+    else if (mode == kGradInput) e = launch_tc_inst<CG, kGradInput>(q, maps, out_bytes, grid, st);
+    else e = launch_tc_inst<CG, kGradWeight>(q, maps, out_bytes, grid, st);
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "grouped product launch");
 }
 
@@ -686,6 +752,11 @@ combo_status product(int mode, const void* rows1, int64_t pitch1, const void* ro
     if (elem_bytes == 2 && p.a_vec && p.b_vec && (mode == kGradWeight ? M > 0 : true)) {
         Product t = p;
         if (mode != kGradWeight) t.I = p.J;      // the weights' index is the height there
+        // Pairs of CTAs halve what the tensor cores and L2 deliver for a product; a single one wastes less where there are
+        // too few tiles of 256 outputs for all pairs.  Measured: 16 x 1065 rows, 1024 -> 4096: 118 us against 131; 16 rows,
+        // 1024 -> 1024: no difference.
+        const long long heights = (t.I + 255) / 256, widths = mode == kGradWeight ? (t.J + 255) / 256 : 1;
+        if (heights * widths * N >= sms / 2) return launch_tc<2>(t, mode, out_bytes, sms, smem, st);
         return launch_tc<1>(t, mode, out_bytes, sms, smem, st);
     }
     cudaError_t e;

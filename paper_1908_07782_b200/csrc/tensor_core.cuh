@@ -10,34 +10,52 @@ namespace combo_tc {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// One thread of the warp, the same at every call: the whole warp asks.  What it issues alone stands under this test and
+// not under a comparison of lane numbers, which would have the compiler expect many threads there (100 cycles a copy).
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 __device__ __forceinline__ void mbar_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
-// The same place in the shared memory of the pair's leader, as a cluster address: bit 24 of a cluster address holds
-// the parity of the CTA's rank.
-__device__ __forceinline__ uint32_t at_leader(uint32_t addr) { return addr & 0xfeffffffu; }
+// The same place in the shared memory of the pair's leader, as a cluster address.
+__device__ __forceinline__ uint32_t at_leader(uint32_t addr) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
 
-// Arrivals.  `bar` is a cluster address (an own address is one).
+// Arrivals; `bar` is a cluster address (an own address is one).  Cluster-wide release costs about a microsecond, so it
+// is asked for only where a thread's own writes are handed over: bytes that TMA brings are published by the barrier
+// itself, and TMEM by tcgen05's fences.
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_release(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
-constexpr uint32_t kPolls = 1u << 21;        // polls of about a microsecond before a wait is given up
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+constexpr uint32_t kPolls = 1u << 22;        // polls before a wait is given up: seconds
+// Waits for the phase of that parity; false if it is given up, or if `dead` was set meanwhile.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const volatile int* dead) {
     uint32_t ok;
 #pragma unroll 1
-    for (uint32_t it = 0; it < kPolls; ++it) {
-        asm volatile(
-            "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(1000u)
-            : "memory");
+    for (uint32_t it = 1; it <= kPolls; ++it) {
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                     : "=r"(ok)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
         if (ok) return true;
+        if (it % 1024 == 0 && *dead) return false;
     }
     return false;
 }
@@ -61,6 +79,17 @@ template <int CG> __device__ __forceinline__ void tma_3d(uint32_t dst, const CUt
     else
         asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
                      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int u, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+                     "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(u)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+                     "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(u)
                      : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
@@ -96,7 +125,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
           "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(addr));
 }
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// All loads so far have arrived in `v`: naming the registers keeps their uses behind the wait.
+__device__ __forceinline__ void tmem_load_wait(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                   "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                   "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                   "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
 
 // ---- products
 // Shared-memory operand, 128-byte swizzle (8 lines of 128 bytes to an atom).
