@@ -206,7 +206,7 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
 // warp that issues the products, four warps that take finished accumulators out of TMEM (two of them there, 256 columns
 // each, so that the next tile's products run meanwhile), turn them through shared memory and store them.  The last rows
 // of a worker in the gradient of the weights: what the load brought beyond them is zeroed in shared memory before the
-// products see it, by a warp of its own (another worker's NaN would not vanish by being multiplied with zero).
+// products see it, by a warp of its own in a stage of its own (another worker's NaN would not vanish by being multiplied with zero).
 using namespace combo_tc;
 
 __device__ int g_linear_status;              // 0, or the site of the first wait that gave up
@@ -308,10 +308,9 @@ template <int CG, int MODE> struct Tiles {
 // Zeroes lines [left, next multiple of 16) of `blocks` blocks of 64 lines of 128 bytes; a warp.
 __device__ __forceinline__ void zero_tail(uint32_t at, int blocks, int left, int lane) {
     const int words = ((left + 15) / 16 * 16 - left) * 8;
-    for (int e = lane; e < blocks * words; e += 32) {
-        const int block = e / words, o = e - block * words;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + block * 64 * kStep * 2 + left * 128 + o * 16), "r"(0u) : "memory");
-    }
+    for (int block = 0; block < blocks; ++block)
+        for (int o = lane; o < words; o += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + block * 64 * kStep * 2 + left * 128 + o * 16), "r"(0u) : "memory");
     fence_async();
     __syncwarp();
 }
@@ -320,7 +319,7 @@ template <int CG, int MODE, int OB>
 __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __grid_constant__ TcMaps maps) {
     constexpr bool A_R = MODE == kForward, B_R = MODE != kGradWeight;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 4];
+    __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 7];
     __shared__ uint32_t tmem_at;
     __shared__ int dead;                     // a wait of this CTA gave up: every role leaves its loop
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -329,21 +328,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8 * s; };
     const auto empty = [&](int s) { return bar0 + 8 * (kMaxStages + s); };
-    const auto tail = [&](int s) { return bar0 + 8 * (2 * kMaxStages + s); };
-    const auto peer_zeroed = [&](int s) { return bar0 + 8 * (3 * kMaxStages + s); };
-    const auto acc_full = [&](int b) { return bar0 + 8 * (4 * kMaxStages + b); };
-    const auto acc_empty = [&](int b) { return bar0 + 8 * (4 * kMaxStages + 2 + b); };
+    const auto acc_full = [&](int b) { return bar0 + 8 * (2 * kMaxStages + b); };
+    const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * kMaxStages + 2 + b); };
+    // the stage behind the ring, for the rows of a tile's end (gradient of the weights): loaded, zeroed, free
+    const uint32_t tail_full = bar0 + 8 * (2 * kMaxStages + 4), tail_ready = tail_full + 8, tail_empty = tail_full + 16;
+    const uint32_t tail_at = smem + q.stages * q.stage_bytes;
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.stages; ++s) {
             mbar_init(full(s), 2);           // one arrival for either operand, and the bytes of all CTAs
             mbar_init(empty(s), 1);
-            mbar_init(tail(s), 2);
-            mbar_init(peer_zeroed(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_empty(b), kOutWarps * CG);
         }
+        mbar_init(tail_full, 2);             // of this CTA alone
+        mbar_init(tail_ready, CG);           // the leader's: from either CTA
+        mbar_init(tail_empty, 1);
         mbar_init_fence();
         dead = 0;
         prefetch_map(&maps.a);
@@ -365,7 +366,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
         // ------------------------------------------------------------ loads: warp 0 the height's operand, warp 2 the width's
         const int operand = warp == 0 ? 0 : 1;
         Tiles<CG, MODE> tiles(q, first);
-        uint32_t done = 0;                   // stages issued
+        uint32_t done = 0, tails = 0;        // stages of the ring issued; tiles with an end of their own
+        const uint32_t bar_leader = CG == 1 ? full(0) : at_leader(full(0));
         bool ok = true;
         while (tiles.next(x, stride)) {
             const int half = x.n / CG;       // of the width: this CTA's share
@@ -381,14 +383,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
                 map = &maps.b[m];
             }
             const int at = operand == 0 ? x.i0 + rank * 128 : MODE == kGradWeight ? x.j0 + rank * half : (int)x.row0 + rank * half;
-            // the last rows, if some of a 16 are another's: that load counts on a barrier of this CTA alone, and the warp
-            // that zeroes the others arrives for it
+            // the last rows, if some of a 16 are another's: they go to a stage of their own, where a warp zeroes the others,
+            // and are asked for as soon as that stage is sure to be free, when the ring has come round to this tile
             const int rest = MODE == kGradWeight ? (int)((x.row1 - x.row0) % kStep) : 0;
             const int plain = rest % 16 != 0 ? x.steps - 1 : x.steps;
+            const int ahead = plain < x.steps ? min(plain, q.stages) : -1;
             uint32_t s = done % q.stages, ph = done / q.stages & 1u;
-            const auto load = [&](int k, uint32_t bar) {
+            const auto load = [&](int k, uint32_t to, uint32_t bar) {
                 const int r = MODE == kGradWeight ? (int)x.row0 + k * kStep : k * kStep;
-                const uint32_t to = smem + s * q.stage_bytes + operand * kOperandA;
+                to += operand * kOperandA;
                 if (operand == 0 && MODE == kForward) tma_3d<CG>(to, map, r, at, x.w, bar);
                 else if (operand == 1 && MODE != kGradWeight) tma_2d<CG>(to, map, r, at, bar);
                 else if (blocks && MODE == kGradInput) tma_4d<CG>(to, map, 0, r, at / 64, x.w, bar);
@@ -400,22 +403,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
                     }
             };
             if (elect()) {
-                for (int k = 0; k < x.steps; ++k) {
-                    if (!mbar_wait(empty(s), ph ^ 1u, dead_v)) { ok = give_up(40); break; }
-                    if (k == plain) {
-                        mbar_arrive_expect(tail(s), bytes);
-                        load(k, tail(s));
-                    } else {
-                        // the leader expects the bytes of both CTAs; the other one's may come before
-                        if (rank == 0) mbar_arrive_expect(full(s), bytes * CG);
-                        load(k, CG == 1 ? full(s) : at_leader(full(s)));
+                for (int k = 0; k <= plain; ++k) {
+                    if (MODE == kGradWeight && k == ahead) {
+                        if (!mbar_wait(tail_empty, tails & 1u ^ 1u, dead_v)) { ok = give_up(42); break; }
+                        mbar_arrive_expect(tail_full, bytes);
+                        load(plain, tail_at, tail_full);
                     }
+                    if (k == plain) break;
+                    if (!mbar_wait(empty(s), ph ^ 1u, dead_v)) { ok = give_up(40); break; }
+                    // the leader expects the bytes of both CTAs; the other one's may come before
+                    if (rank == 0) mbar_arrive_expect(full(s), bytes * CG);
+                    load(k, smem + s * q.stage_bytes, bar_leader + 8 * s);
                     if (++s == q.stages) { s = 0; ph ^= 1u; }
                 }
             }
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            done += x.steps;
+            done += plain;
+            if (plain < x.steps) ++tails;
         }
         if (!ok) {
             // after a wait that gave up nothing tells when the copies under way have landed: far longer than they take
@@ -425,48 +430,56 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
         // No copy may be under way when the CTA leaves: the products have freed the last stages.
         for (uint32_t k = 1; k <= done && k <= (uint32_t)q.stages && ok; ++k)
             ok = mbar_wait(empty((done - k) % q.stages), (done - k) / q.stages & 1u, dead_v) || give_up(43);
+        if (ok && tails > 0 && !mbar_wait(tail_empty, (tails - 1) & 1u, dead_v)) {
+            give_up(48);
+            *dead_v = 1;
+        }
     } else if (warp == 1) {
         // ------------------------------------------------------------ products, by one thread of the leader
         if (rank == 0) {
             Tiles<CG, MODE> tiles(q, first);
-            uint32_t done = 0, accs = 0, zeroed = 0;     // `zeroed`: parities of peer_zeroed, of the issuing thread
+            uint32_t done = 0, accs = 0, tails = 0;
             bool ok = true;
             while (tiles.next(x, stride)) {
                 if (x.steps == 0) continue;
                 const uint32_t buf = accs & 1u;
                 const int rest = MODE == kGradWeight ? (int)((x.row1 - x.row0) % kStep) : 0;
+                const int plain = rest % 16 != 0 ? x.steps - 1 : x.steps;
                 if (elect()) {
                     const uint32_t d = tmem + buf * 256, kind = product_kind(128 * CG, x.n, A_R, B_R);
                     uint32_t s = done % q.stages, ph = done / q.stages & 1u;
                     ok = mbar_wait(acc_empty(buf), (accs >> 1 & 1u) ^ 1u, dead_v) || give_up(44);
                     tc_fence_after();
-                    for (int k = 0; k < x.steps && ok; ++k) {
-                        if (!mbar_wait(full(s), ph, dead_v)) { ok = give_up(45); break; }
-                        const bool last = k + 1 == x.steps;
-                        if (MODE == kGradWeight && last && rest % 16 != 0) {
-                            if (CG == 2 && !mbar_wait(peer_zeroed(s), zeroed >> s & 1u, dead_v)) { ok = give_up(46); break; }
-                            zeroed ^= 1u << s;
-                            fence_cluster();         // threads of both CTAs have written zeros
-                        }
-                        tc_fence_after();
-                        const uint32_t a = smem + s * q.stage_bytes;
+                    const auto issue = [&](uint32_t a, int n16, bool add) {
                         const uint64_t da = operand(a, A_R, 64 * kStep * 2), db = operand(a + kOperandA, B_R, 64 * kStep * 2);
-                        if (MODE == kGradWeight && last && rest != 0) {
-                            for (int c = 0; c * 16 < rest; ++c)
-                                mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, k + c > 0);
-                        } else {
 #pragma unroll
-                            for (int c = 0; c < kStep / 16; ++c)
-                                mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, k + c > 0);
-                        }
+                        for (int c = 0; c < kStep / 16; ++c)
+                            if (MODE != kGradWeight || c < n16)
+                                mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, add || c > 0);
+                    };
+                    for (int k = 0; k < plain && ok; ++k) {
+                        if (!mbar_wait(full(s), ph, dead_v)) { ok = give_up(45); break; }
+                        tc_fence_after();
+                        issue(smem + s * q.stage_bytes, k + 1 == x.steps && rest ? rest / 16 : kStep / 16, k > 0);
                         mma_commit<CG>(empty(s));
                         if (++s == q.stages) { s = 0; ph ^= 1u; }
+                    }
+                    if (MODE == kGradWeight && plain < x.steps && ok) {
+                        // zeros that threads of both CTAs have written
+                        if (CG == 1 ? mbar_wait(tail_ready, tails & 1u, dead_v) : mbar_wait_cluster(tail_ready, tails & 1u, dead_v)) {
+                            tc_fence_after();
+                            issue(tail_at, (rest + 15) / 16, plain > 0);
+                            mma_commit<CG>(tail_empty);
+                        } else {
+                            ok = give_up(46);
+                        }
                     }
                     if (ok) mma_commit<CG>(acc_full(buf));
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                done += x.steps;
+                done += plain;
+                if (plain < x.steps) ++tails;
                 ++accs;
             }
             if (!ok) *dead_v = 1;
@@ -475,24 +488,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
         // ------------------------------------------------------------ rows of others, zeroed
         if (MODE == kGradWeight) {
             Tiles<CG, MODE> tiles(q, first);
-            uint32_t done = 0, parity = 0;
+            uint32_t tails = 0;
             bool ok = true;
             while (tiles.next(x, stride)) {
                 const int rest = (int)((x.row1 - x.row0) % kStep);
-                done += x.steps;
                 if (rest % 16 == 0) continue;
-                const uint32_t s = (done - 1) % q.stages;
-                ok = mbar_wait(tail(s), parity >> s & 1u, dead_v) || give_up(41);
+                ok = mbar_wait(tail_full, tails & 1u, dead_v) || give_up(41);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                parity ^= 1u << s;
-                zero_tail(smem + s * q.stage_bytes, 2 + x.n / CG / 64, rest, lane);
+                ++tails;
+                zero_tail(tail_at, 2 + x.n / CG / 64, rest, lane);
                 if (elect()) {
-                    if (rank == 0) {
-                        mbar_arrive(full(s));
-                        mbar_arrive(full(s));
-                    } else {
-                        mbar_arrive_release(at_leader(peer_zeroed(s)));
-                    }
+                    if (rank == 0) mbar_arrive(tail_ready);
+                    else mbar_arrive_release(at_leader(tail_ready));
                 }
                 __syncwarp();
             }
@@ -502,7 +509,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
         // ------------------------------------------------------------ results
         Tiles<CG, MODE> tiles(q, first);
         const int quarter = warp & 3;        // a warp reads the 32 lanes of TMEM that its number allows
-        float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + q.stages * q.stage_bytes + quarter * kTurn);
+        float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + (q.stages + (MODE == kGradWeight ? 1 : 0)) * q.stage_bytes + quarter * kTurn);
         uint32_t accs = 0;
         bool ok = true;
         while (tiles.next(x, stride)) {
@@ -614,7 +621,7 @@ bool encode(CUtensorMap* map, const void* base, long long width, long long rows,
 
 template <int CG, int MODE> cudaError_t launch_tc_inst(const TcParams& q, const TcMaps& maps, int out_bytes, int grid, cudaStream_t st) {
     auto kern = out_bytes == 2 ? k_tc<CG, MODE, 2> : k_tc<CG, MODE, 4>;
-    const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOutWarps * kTurn;
+    const size_t smem = 1024 + (size_t)(q.stages + (MODE == kGradWeight ? 1 : 0)) * q.stage_bytes + kOutWarps * kTurn;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -651,6 +658,7 @@ template <int CG> combo_status launch_tc(const Product& p, int mode, int out_byt
     const int half = q.width / CG;
     q.stage_bytes = kOperandA + half * kStep * 2;
     q.stages = (smem_optin - 2048 - kOutWarps * kTurn) / q.stage_bytes;
+    if (mode == kGradWeight) --q.stages;         // one behind the ring
     if (q.stages > kMaxStages) q.stages = kMaxStages;
     int grid = sms / CG * CG;
     if (tiles * CG < grid) grid = (int)tiles * CG;

@@ -30,7 +30,7 @@ __device__ __forceinline__ uint32_t at_leader(uint32_t addr) {
     return r;
 }
 
-// Arrivals; `bar` is a cluster address (an own address is one).  Cluster-wide release costs about a microsecond, so it
+// Arrivals on an own barrier, or (`bar` a cluster address; an own address is one) on any.  Cluster-wide release costs about a microsecond, so it
 // is asked for only where a thread's own writes are handed over: bytes that TMA brings are published by the barrier
 // itself, and TMEM by tcgen05's fences.
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -40,25 +40,33 @@ __device__ __forceinline__ void mbar_arrive_release(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
 constexpr uint32_t kPolls = 1u << 22;        // polls before a wait is given up: seconds
-// Waits for the phase of that parity; false if it is given up, or if `dead` was set meanwhile.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const volatile int* dead) {
+// Waits for the phase of that parity; false if it is given up, or if `dead` was set meanwhile.  CLUSTER: what threads of
+// the other CTA wrote before they arrived is seen behind the wait.
+template <bool CLUSTER> __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, const volatile int* dead) {
     uint32_t ok;
 #pragma unroll 1
     for (uint32_t it = 1; it <= kPolls; ++it) {
-        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-                     : "=r"(ok)
-                     : "r"(bar), "r"(parity)
-                     : "memory");
+        if constexpr (CLUSTER)
+            asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                         : "=r"(ok)
+                         : "r"(bar), "r"(parity)
+                         : "memory");
+        else
+            asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                         : "=r"(ok)
+                         : "r"(bar), "r"(parity)
+                         : "memory");
         if (ok) return true;
         if (it % 1024 == 0 && *dead) return false;
     }
     return false;
 }
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const volatile int* dead) { return mbar_poll<false>(bar, parity, dead); }
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, const volatile int* dead) { return mbar_poll<true>(bar, parity, dead); }
 
 // ---- TMA: boxes of global memory into this CTA's shared memory; bytes are counted on `bar` (CG = 2: the leader's)
 template <int CG> __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
