@@ -99,12 +99,15 @@ def load():
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    """Handle of ``stream``, or of the current device's current stream (asked for without making a
+    Stream object, which takes 3 us where a small call takes 10)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _check(status: int, where: str):
@@ -282,42 +285,54 @@ def combo_check_tensors(tensors, begin, first, n_tensors, N, total, elem_bytes, 
     return int(flag.item())
 
 
-def _same(name: str, what: str, ok: bool) -> None:
-    if not ok:
-        raise ValueError("%s: %s" % (name, what))
+_SIZES = {torch.float32: 4, torch.bfloat16: 2}
 
 
-def _pitch(t, name, arg) -> int:
+def _refuse(name: str, what: str):
+    raise ValueError("%s: %s" % (name, what))
+
+
+def _pitch(shape, stride, name, arg) -> int:
     """Elements between the positions of a channels-last [B, L, C] tensor."""
-    B, L, C = t.shape
-    pitch = t.stride(1) if L > 1 else t.stride(0) if B > 1 else C
-    _same(name, "%s: channels must be neighbours, samples L positions apart" % arg,
-          (C == 1 or t.stride(2) == 1) and (B <= 1 or L <= 1 or t.stride(0) == L * pitch))
+    B, L, C = shape
+    pitch = stride[1] if L > 1 else stride[0] if B > 1 else C
+    if (C > 1 and stride[2] != 1) or (B > 1 and stride[0] != L * pitch):
+        _refuse(name, "%s: channels must be neighbours, samples L positions apart" % arg)
     return pitch
 
 
-def _rows(t, name, arg) -> int:
-    """Elements between the rows of an [N, C] tensor."""
-    _same(name, "%s: a row's elements must be neighbours" % arg, t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1))
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _rows(shape, stride, name, arg) -> int:
+    """Elements between the rows of a two-dimensional tensor."""
+    if shape[1] > 1 and stride[1] != 1:
+        _refuse(name, "%s: a row's elements must be neighbours" % arg)
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
-def _size(t, name) -> int:
-    _same(name, "types are float32 and bfloat16", t.dtype in (torch.float32, torch.bfloat16))
-    return t.element_size()
-
-
-def _norm_args(name, x, gamma, beta, begin):
-    """What the two group norm calls check and pass alike: parameters, their size and pitch, workers."""
-    _same(name, "x must be [B, L, C]", x.dim() == 3)
-    N = 1 if begin is None else begin.numel() - 1
-    _same(name, "begin must be int64", begin is None or (begin.dtype == torch.int64 and begin.is_contiguous()))
+def _norm_args(name, x, others, gamma, beta, begin, stats, groups):
+    """What the two group norm calls check alike; size of x's elements, workers, size and pitch of the parameters."""
+    shape = x.shape
+    if len(shape) != 3 or x.dtype not in _SIZES:
+        _refuse(name, "x must be [B, L, C], float32 or bfloat16")
+    for t in others:
+        if t.shape != shape or t.dtype != x.dtype:
+            _refuse(name, "y (dy, dx) must be like x")
+    for t in stats:
+        if t is not None and (t.dtype != torch.float32 or t.numel() != shape[0] * groups or not t.is_contiguous()):
+            _refuse(name, "mean and rstd must be float32 [B, groups]")
+    if begin is None:
+        N = 1
+    else:
+        N = begin.numel() - 1
+        if begin.dtype != torch.int64 or not begin.is_contiguous():
+            _refuse(name, "begin must be int64 [N + 1]")
     if gamma is None or beta is None:
-        return N, 4, 0
-    _same(name, "gamma and beta must be [N, C] of one type and one pitch", gamma.shape == beta.shape == (N, x.shape[2])
-          and gamma.dtype == beta.dtype and gamma.dtype in (torch.float32, torch.bfloat16)
-          and _rows(gamma, name, "gamma") == _rows(beta, name, "beta"))
-    return N, gamma.element_size(), _rows(gamma, name, "gamma")
+        return _SIZES[x.dtype], N, 4, 0
+    if gamma.shape != (N, shape[2]) or beta.shape != (N, shape[2]) or gamma.dtype != beta.dtype or gamma.dtype not in _SIZES:
+        _refuse(name, "gamma and beta must be [N, C] of one type, float32 or bfloat16")
+    pitch = _rows(gamma.shape, gamma.stride(), name, "gamma")
+    if pitch != _rows(beta.shape, beta.stride(), name, "beta"):
+        _refuse(name, "gamma and beta must have one pitch")
+    return _SIZES[x.dtype], N, _SIZES[gamma.dtype], pitch
 
 
 def combo_group_norm(x, y, gamma, beta, begin, groups, eps, act, mean=None, rstd=None, scratch=None, stream=None):
@@ -326,15 +341,12 @@ def combo_group_norm(x, y, gamma, beta, begin, groups, eps, act, mean=None, rstd
     worker; mean, rstd: float32 [B, groups] or None.  The forward pass needs no scratch: it is
     taken so that one set of arguments serves both directions."""
     name = "combo_group_norm"
-    N, pb, pp = _norm_args(name, x, gamma, beta, begin)
-    _same(name, "y must be like x", y.shape == x.shape and y.dtype == x.dtype and x.dtype in (torch.float32, torch.bfloat16))
-    for t in (mean, rstd):
-        _same(name, "mean and rstd must be float32 [B, groups]",
-              t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == x.shape[0] * groups))
-    B, L, C = x.shape
-    _check(load().combo_group_norm(_ptr(x), _pitch(x, name, "x"), _ptr(y), _pitch(y, name, "y"), x.element_size(),
-                                   _ptr(gamma), _ptr(beta), pb, pp, _ptr(begin), N, B, L, C, groups, eps, act,
-                                   _ptr(mean), _ptr(rstd), _stream(stream)), name)
+    size, N, param_size, param_pitch = _norm_args(name, x, (y,), gamma, beta, begin, (mean, rstd), groups)
+    B, L, C = shape = x.shape
+    _check(load().combo_group_norm(x.data_ptr(), _pitch(shape, x.stride(), name, "x"), y.data_ptr(),
+                                   _pitch(shape, y.stride(), name, "y"), size, _ptr(gamma), _ptr(beta), param_size,
+                                   param_pitch, _ptr(begin), N, B, L, C, groups, eps, act, _ptr(mean), _ptr(rstd),
+                                   _stream(stream)), name)
     return y
 
 
@@ -348,35 +360,39 @@ def combo_group_norm_backward(dy, x, dx, gamma, beta, begin, groups, act, mean, 
     """Gradients of combo_group_norm: dx [B, L, C] and, per worker, dgamma and dbeta (float32
     [N, C], views of flat gradient vectors, or None), from the forward call's mean and rstd."""
     name = "combo_group_norm_backward"
-    N, pb, pp = _norm_args(name, x, gamma, beta, begin)
-    _same(name, "dy and dx must be like x", dy.shape == dx.shape == x.shape and dy.dtype == dx.dtype == x.dtype
-          and x.dtype in (torch.float32, torch.bfloat16))
-    for t in (mean, rstd):
-        _same(name, "mean and rstd must be float32 [B, groups]",
-              t.dtype == torch.float32 and t.is_contiguous() and t.numel() == x.shape[0] * groups)
-    gp = 0
+    size, N, param_size, param_pitch = _norm_args(name, x, (dy, dx), gamma, beta, begin, (mean, rstd), groups)
+    B, L, C = shape = x.shape
+    grad_pitch = 0
     if dgamma is not None and dbeta is not None:
-        gp = _rows(dgamma, name, "dgamma")
-        _same(name, "dgamma and dbeta must be float32 [N, C] of one pitch", dgamma.shape == dbeta.shape == (N, x.shape[2])
-              and dgamma.dtype == dbeta.dtype == torch.float32 and gp == _rows(dbeta, name, "dbeta"))
-    B, L, C = x.shape
+        if dgamma.shape != (N, C) or dbeta.shape != (N, C) or dgamma.dtype != torch.float32 or dbeta.dtype != torch.float32:
+            _refuse(name, "dgamma and dbeta must be float32 [N, C]")
+        grad_pitch = _rows(dgamma.shape, dgamma.stride(), name, "dgamma")
+        if grad_pitch != _rows(dbeta.shape, dbeta.stride(), name, "dbeta"):
+            _refuse(name, "dgamma and dbeta must have one pitch")
     _check(load().combo_group_norm_backward(
-        _ptr(dy), _pitch(dy, name, "dy"), _ptr(x), _pitch(x, name, "x"), _ptr(dx), _pitch(dx, name, "dx"),
-        x.element_size(), _ptr(gamma), _ptr(beta), pb, pp, _ptr(begin), N, B, L, C, groups, act, _ptr(mean), _ptr(rstd),
-        _ptr(dgamma), _ptr(dbeta), gp, _ptr(scratch), _bytes(scratch), _stream(stream)), name)
+        dy.data_ptr(), _pitch(shape, dy.stride(), name, "dy"), x.data_ptr(), _pitch(shape, x.stride(), name, "x"),
+        dx.data_ptr(), _pitch(shape, dx.stride(), name, "dx"), size, _ptr(gamma), _ptr(beta), param_size, param_pitch,
+        _ptr(begin), N, B, L, C, groups, act, _ptr(mean), _ptr(rstd), _ptr(dgamma), _ptr(dbeta), grad_pitch,
+        _ptr(scratch), _bytes(scratch), _stream(stream)), name)
     return dx
 
 
-def _product_args(name, rows, weights, begin, row_widths):
-    """Shapes and pitches of a grouped product: row operands [M, width], weights [N, n_out, n_in]."""
-    N, n_out, n_in = weights.shape
-    _same(name, "begin must be int64 [N + 1]", begin.dtype == torch.int64 and begin.shape == (N + 1,) and begin.is_contiguous())
-    _same(name, "weights: a row's elements must be neighbours", n_in == 1 or weights.stride(2) == 1)
-    M = rows[0].shape[0]
-    for t, width in zip(rows, row_widths):
-        _same(name, "rows must be [M, %d]" % width, t.shape == (M, width))
-    w_pitch = weights.stride(1) if n_out > 1 else n_in
-    return N, M, n_in, n_out, w_pitch, weights.stride(0) if N > 1 else 0
+def _product_args(name, a, b, weights, begin, a_width, b_width, same):
+    """Checks the operands of a grouped product: rows a [M, a_width], b [M, b_width] (widths: 1 = n_out, 2 = n_in),
+    weights [N, n_out, n_in]; `same`: the two that are inputs."""
+    shape, stride = weights.shape, weights.stride()
+    N, n_out, n_in = shape
+    M = a.shape[0]
+    if a.shape != (M, shape[a_width]) or b.shape != (M, shape[b_width]):
+        _refuse(name, "rows must be [M, %d] and [M, %d]" % (shape[a_width], shape[b_width]))
+    if begin.dtype != torch.int64 or begin.numel() != N + 1 or not begin.is_contiguous():
+        _refuse(name, "begin must be int64 [N + 1]")
+    if n_in > 1 and stride[2] != 1:
+        _refuse(name, "weights: a row's elements must be neighbours")
+    if same[0].dtype != same[1].dtype or a.dtype not in _SIZES or b.dtype not in _SIZES or weights.dtype not in _SIZES:
+        _refuse(name, "types are float32 and bfloat16, one for both inputs")
+    return (N, M, n_in, n_out, _rows(a.shape, a.stride(), name, "rows"), _rows(b.shape, b.stride(), name, "rows"),
+            stride[1] if n_out > 1 else n_in, stride[0] if N > 1 else 0)
 
 
 def combo_grouped_linear(x, w, y, begin, stream=None):
@@ -384,21 +400,19 @@ def combo_grouped_linear(x, w, y, begin, stream=None):
     w [N, n_out, n_in] (a view of flat parameter vectors, strides as they are), y [M, n_out] of x's
     type or, for bfloat16, float32."""
     name = "combo_grouped_linear"
-    N, M, n_in, n_out, wp, ws = _product_args(name, (x, y), w, begin, (w.shape[2], w.shape[1]))
-    _same(name, "x and w must have one type", x.dtype == w.dtype)
-    _check(load().combo_grouped_linear(_ptr(x), _rows(x, name, "x"), _ptr(w), wp, ws, _ptr(y), _rows(y, name, "y"),
-                                       _size(x, name), _size(y, name), _ptr(begin), N, M, n_in, n_out, _stream(stream)), name)
+    N, M, n_in, n_out, xp, yp, wp, ws = _product_args(name, x, y, w, begin, 2, 1, (x, w))
+    _check(load().combo_grouped_linear(x.data_ptr(), xp, w.data_ptr(), wp, ws, y.data_ptr(), yp, _SIZES[x.dtype],
+                                       _SIZES[y.dtype], begin.data_ptr(), N, M, n_in, n_out, _stream(stream)), name)
     return y
 
 
 def combo_grouped_linear_grad_input(dy, w, dx, begin, stream=None):
     """dx[m] = dy[m] W_w: the gradient of combo_grouped_linear for its rows."""
     name = "combo_grouped_linear_grad_input"
-    N, M, n_in, n_out, wp, ws = _product_args(name, (dy, dx), w, begin, (w.shape[1], w.shape[2]))
-    _same(name, "dy and w must have one type", dy.dtype == w.dtype)
-    _check(load().combo_grouped_linear_grad_input(_ptr(dy), _rows(dy, name, "dy"), _ptr(w), wp, ws, _ptr(dx),
-                                                  _rows(dx, name, "dx"), _size(dy, name), _size(dx, name), _ptr(begin), N, M,
-                                                  n_in, n_out, _stream(stream)), name)
+    N, M, n_in, n_out, yp, xp, wp, ws = _product_args(name, dy, dx, w, begin, 1, 2, (dy, w))
+    _check(load().combo_grouped_linear_grad_input(dy.data_ptr(), yp, w.data_ptr(), wp, ws, dx.data_ptr(), xp,
+                                                  _SIZES[dy.dtype], _SIZES[dx.dtype], begin.data_ptr(), N, M, n_in, n_out,
+                                                  _stream(stream)), name)
     return dx
 
 
@@ -406,10 +420,9 @@ def combo_grouped_linear_grad_weight(dy, x, dw, begin, stream=None):
     """dw[w] = sum over worker w's rows of dy[m]^T x[m]: the gradient for the weights, [N, n_out, n_in]
     (a view of flat gradient vectors), of dy's type or float32."""
     name = "combo_grouped_linear_grad_weight"
-    N, M, n_in, n_out, wp, ws = _product_args(name, (dy, x), dw, begin, (dw.shape[1], dw.shape[2]))
-    _same(name, "dy and x must have one type", dy.dtype == x.dtype)
-    _check(load().combo_grouped_linear_grad_weight(_ptr(dy), _rows(dy, name, "dy"), _ptr(x), _rows(x, name, "x"), _ptr(dw),
-                                                   wp, ws, _size(dy, name), _size(dw, name), _ptr(begin), N, M, n_in, n_out,
+    N, M, n_in, n_out, yp, xp, wp, ws = _product_args(name, dy, x, dw, begin, 1, 2, (dy, x))
+    _check(load().combo_grouped_linear_grad_weight(dy.data_ptr(), yp, x.data_ptr(), xp, dw.data_ptr(), wp, ws,
+                                                   _SIZES[dy.dtype], _SIZES[dw.dtype], begin.data_ptr(), N, M, n_in, n_out,
                                                    _stream(stream)), name)
     return dw
 

@@ -674,8 +674,10 @@ combo_status plan_norm(NormParams& p, Plan& plan, int eb, bool vec, bool back, i
     return plan.grid > 0x7fffffffLL ? COMBO_ERR_INVALID_ARG : COMBO_OK;
 }
 
-cudaError_t launch_norm(void (*kern)(NormParams), const NormParams& p, const Plan& plan, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem);
+// `which`: a number of its own for every kernel
+cudaError_t launch_norm(void (*kern)(NormParams), int which, const NormParams& p, const Plan& plan, int smem_optin, cudaStream_t st) {
+    static uint64_t allowed[48];
+    cudaError_t e = combo_host::allow_smem(kern, smem_optin, &allowed[which]);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)plan.grid);
@@ -702,6 +704,10 @@ template <int EB, bool VEC, bool RES> NormKernel pick_act(bool back, int act) {
 template <int EB> NormKernel pick(bool back, bool vec, bool res, int act) {
     if (vec) return res ? pick_act<EB, true, true>(back, act) : pick_act<EB, true, false>(back, act);
     return res ? pick_act<EB, false, true>(back, act) : pick_act<EB, false, false>(back, act);
+}
+
+int number_of(int eb, bool back, const Plan& plan, int act) {
+    return (((eb == 4 ? 1 : 0) * 2 + back) * 2 + plan.vec) * 2 * 3 + plan.res * 3 + act;
 }
 
 // What forward and backward ask alike.
@@ -778,7 +784,7 @@ combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y
     Plan plan;
     if ((rc = plan_norm(p, plan, elem_bytes, vec, false, sms, smem)) != COMBO_OK) return rc;
     auto kern = elem_bytes == 4 ? pick<4>(false, plan.vec, plan.res, act) : pick<2>(false, plan.vec, plan.res, act);
-    cudaError_t e = launch_norm(kern, p, plan, static_cast<cudaStream_t>(stream));
+    cudaError_t e = launch_norm(kern, number_of(elem_bytes, false, plan, act), p, plan, smem, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "group norm launch");
 }
 
@@ -836,7 +842,7 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
         Plan plan;
         if ((rc = plan_norm(p, plan, elem_bytes, vec, true, sms, smem)) != COMBO_OK) return rc;
         auto kern = elem_bytes == 4 ? pick<4>(true, plan.vec, plan.res, act) : pick<2>(true, plan.vec, plan.res, act);
-        if ((e = launch_norm(kern, p, plan, st)) != cudaSuccess) return combo_host::fail(e, "group norm backward launch");
+        if ((e = launch_norm(kern, number_of(elem_bytes, true, plan, act), p, plan, smem, st)) != cudaSuccess) return combo_host::fail(e, "group norm backward launch");
     }
     if (dgamma) {
         const dim3 grid((unsigned)((C + 31) / 32), (unsigned)N);

@@ -224,6 +224,7 @@ constexpr int kRowBoxes = 4;                 // boxes of 32, 64, 128 or 256 rows
 constexpr int kMaxStages = 8;
 constexpr int kTurn = 32 * 33 * 4;           // bytes in which an epilogue warp turns 32 x 32 outputs
 constexpr int kTmemColumns = 512;
+constexpr int kStaticSmem = 1024;           // room for the kernel's barriers
 
 struct TcParams {
     Product p;
@@ -619,10 +620,11 @@ bool encode(CUtensorMap* map, const void* base, long long width, long long rows,
                                     CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int CG, int MODE> cudaError_t launch_tc_inst(const TcParams& q, const TcMaps& maps, int out_bytes, int grid, cudaStream_t st) {
-    auto kern = out_bytes == 2 ? k_tc<CG, MODE, 2> : k_tc<CG, MODE, 4>;
+template <int CG, int MODE, int OB> cudaError_t launch_tc_inst(const TcParams& q, const TcMaps& maps, int smem_most, int grid, cudaStream_t st) {
+    static uint64_t allowed;
+    auto kern = k_tc<CG, MODE, OB>;
     const size_t smem = 1024 + (size_t)(q.stages + (MODE == kGradWeight ? 1 : 0)) * q.stage_bytes + kOutWarps * kTurn;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = combo_host::allow_smem(kern, smem_most, &allowed);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
@@ -657,7 +659,7 @@ template <int CG> combo_status launch_tc(const Product& p, int mode, int out_byt
     if (tiles > 0x40000000LL) return COMBO_ERR_INVALID_ARG;
     const int half = q.width / CG;
     q.stage_bytes = kOperandA + half * kStep * 2;
-    q.stages = (smem_optin - 2048 - kOutWarps * kTurn) / q.stage_bytes;
+    q.stages = (smem_optin - kStaticSmem - 1024 - kOutWarps * kTurn) / q.stage_bytes;
     if (mode == kGradWeight) --q.stages;         // one behind the ring
     if (q.stages > kMaxStages) q.stages = kMaxStages;
     int grid = sms / CG * CG;
@@ -683,9 +685,10 @@ template <int CG> combo_status launch_tc(const Product& p, int mode, int out_byt
         fine = encode(&maps.b[m], p.a, p.R, p.M, p.a_pitch, 0, 0, 32 << m, 0);
     if (!fine) return COMBO_ERR_CUDA;
     cudaError_t e;
-    if (mode == kForward) e = launch_tc_inst<CG, kForward>(q, maps, out_bytes, grid, st);
-    else if (mode == kGradInput) e = launch_tc_inst<CG, kGradInput>(q, maps, out_bytes, grid, st);
-    else e = launch_tc_inst<CG, kGradWeight>(q, maps, out_bytes, grid, st);
+    const int most = smem_optin - kStaticSmem;
+    if (mode == kForward) e = out_bytes == 2 ? launch_tc_inst<CG, kForward, 2>(q, maps, most, grid, st) : launch_tc_inst<CG, kForward, 4>(q, maps, most, grid, st);
+    else if (mode == kGradInput) e = out_bytes == 2 ? launch_tc_inst<CG, kGradInput, 2>(q, maps, most, grid, st) : launch_tc_inst<CG, kGradInput, 4>(q, maps, most, grid, st);
+    else e = out_bytes == 2 ? launch_tc_inst<CG, kGradWeight, 2>(q, maps, most, grid, st) : launch_tc_inst<CG, kGradWeight, 4>(q, maps, most, grid, st);
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "grouped product launch");
 }
 

@@ -29,6 +29,19 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return na && nb && x < y + nb && y < x + na;
 }
 
+// Lets `kern` use up to `bytes` of dynamic shared memory, once per kernel and device: `done` is the kernel's own word
+// of device bits (asking the driver costs as much as a launch).
+template <typename K> inline cudaError_t allow_smem(K kern, int bytes, uint64_t* done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (__atomic_load_n(done, __ATOMIC_RELAXED) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) __atomic_fetch_or(done, bit, __ATOMIC_RELAXED);
+    return e;
+}
+
 // Launches `kern` so that it may become resident while the stream's preceding kernel drains; the kernel
 // itself waits for that one (pdl_wait) before it touches anything that one writes.
 template <typename... P, typename... A>
