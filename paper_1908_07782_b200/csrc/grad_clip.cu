@@ -24,12 +24,12 @@ namespace {
 using combo_step::Elem;
 using combo_step::warp_sum;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnitBytes = 4096;
 constexpr int kVecs = kUnitBytes / 16 / 32;     // vectors per lane and unit
-constexpr int kCtasPerSm = 2;
-constexpr int kMaxGrid = 1024;                  // bound of the scratch size: 2 CTAs on each of at most 512 SMs
+constexpr int kCtasPerSm = 3;                   // 256 x 3 against 512 x 2 (64 registers a thread, spilled): 722 us against 798
+constexpr int kMaxGrid = 1024;                  // bound of the scratch size
 
 struct Table {
     const unsigned char* const* src;
@@ -50,16 +50,22 @@ __device__ __forceinline__ long long owner_end(const Table& p, int w) {
     return min(max((long long)p.begin[t], 0LL), p.total);
 }
 
-// How many of the values f(0) <= f(1) <= ... <= f(n - 1) are <= pos; the whole block counts.
-template <typename F> __device__ __forceinline__ int block_count_le(int n, long long pos, F f) {
+// The tensor that holds position `pos`, the last one that begins at or before it, and its worker, the last one whose
+// first tensor is at or before that: the whole block counts, both tables' loads under way together.
+__device__ __forceinline__ void locate(const Table& p, long long pos, int& t, int& w) {
+    const int i = (int)threadIdx.x;
+    const int f0 = i < p.N ? p.first[i] : 0x7fffffff;
     int c = 0;
-    for (int base = 0; base < n; base += kThreads) {
-        const int i = base + (int)threadIdx.x;
-        const int got = __syncthreads_count(i < n && f(i) <= pos);
+    for (int base = 0; base < p.n_tensors; base += kThreads) {
+        const int got = __syncthreads_count(base + i < p.n_tensors && (long long)p.begin[base + i] <= pos);
         c += got;
         if (got < kThreads) break;
     }
-    return c;
+    t = max(c - 1, 0);
+    c = __syncthreads_count(f0 <= t);
+    for (int base = kThreads; base < p.N && c == base; base += kThreads)
+        c += __syncthreads_count(base + i < p.N && p.first[base + i] <= t);
+    w = max(c - 1, 0);
 }
 
 // One warp's place in the sequence: the tensor that holds position `pos`, found forwards or backwards.
@@ -215,10 +221,10 @@ template <int EB> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_grad
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r0 = p.piece * blockIdx.x, r1 = min(r0 + p.piece, p.total);
     if (r0 >= r1) return;
-    // the worker that holds r0: the last one whose first element lies at or before it
-    int w = max(block_count_le(p.N, r0, [&](int i) { return owner_end(p, i); }) - 1, 0);
+    int w, t;
+    locate(p, r0, t, w);
     Cursor cur;
-    cur.set(p, max(block_count_le(p.n_tensors, r0, [&](int i) { return (long long)p.begin[i]; }) - 1, 0));
+    cur.set(p, t);
     long long lo = r0;
     while (lo < r1 && w < p.N) {
         const long long hi = min(owner_end(p, w + 1), r1);
@@ -279,10 +285,10 @@ template <int EB> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_grad
     __shared__ double sh[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r0 = min(p.piece * blockIdx.x, p.total), r1 = min(r0 + p.piece, p.total);
-    // last worker with an element before r1, and its tensor
-    int w = max(block_count_le(p.N, r1 - 1, [&](int i) { return owner_end(p, i); }) - 1, 0);
+    int w, t;                                    // of the last element before r1
+    locate(p, r1 - 1, t, w);
     Cursor cur;
-    cur.set(p, max(block_count_le(p.n_tensors, r1 - 1, [&](int i) { return (long long)p.begin[i]; }) - 1, 0));
+    cur.set(p, t);
     combo_step::pdl_wait();
     if (blockIdx.x == 0) {                       // workers without an element
         for (int i = threadIdx.x; i < p.N; i += kThreads)
