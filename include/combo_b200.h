@@ -387,7 +387,8 @@ combo_status combo_check_tensors(const void* const* d_tensors, const int64_t* d_
  * (z <= 0), dz is 0 whatever dy holds.  ReLU keeps NaN; NaN and infinity stay in their
  * (sample, group).  Results do not change from run to run.
  *
- * scratch (backward): combo_group_norm_scratch_bytes bytes, 8-byte aligned.
+ * scratch (both calls): device memory of at least combo_group_norm_scratch_bytes bytes,
+ * 16-byte aligned, contents undefined afterwards.
  * C / groups <= COMBO_NORM_MAX_CHANNELS, B * L * C <= 2^40.
  */
 enum { COMBO_ACT_NONE = 0, COMBO_ACT_RELU = 1, COMBO_ACT_SILU = 2 /* z / (1 + exp(-z)) */ };
@@ -395,8 +396,9 @@ enum { COMBO_ACT_NONE = 0, COMBO_ACT_RELU = 1, COMBO_ACT_SILU = 2 /* z / (1 + ex
 combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y_pitch, int elem_bytes,
                               const void* gamma, const void* beta, int param_bytes, int64_t param_pitch,
                               const int64_t* d_begin, int N, int64_t B, int64_t L, int64_t C, int groups,
-                              float eps, int act, float* mean_out, float* rstd_out, void* stream);
-size_t combo_group_norm_scratch_bytes(int64_t B, int64_t L, int64_t C);
+                              float eps, int act, float* mean_out, float* rstd_out, void* scratch,
+                              size_t scratch_bytes, void* stream);
+size_t combo_group_norm_scratch_bytes(int64_t B, int64_t L, int64_t C, int groups);
 combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch,
                                        void* dx, int64_t dx_pitch, int elem_bytes, const void* gamma,
                                        const void* beta, int param_bytes, int64_t param_pitch,

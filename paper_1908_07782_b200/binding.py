@@ -59,7 +59,8 @@ def load():
         "combo_grad_norm": [vp, vp, vp, i32, i32, i64, i32, f32, vp, vp, vp, ctypes.c_size_t, vp],
         "combo_grad_clip": [vp, vp, vp, vp, i32, i32, i64, i32, f32, vp, vp, vp, ctypes.c_size_t, vp],
         "combo_check_tensors": [vp, vp, vp, i32, i32, i64, i32, vp, vp],
-        "combo_group_norm": [vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, vp, vp],
+        "combo_group_norm": [vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, vp, vp,
+                             ctypes.c_size_t, vp],
         "combo_group_norm_backward": [vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i64, vp, i32, i64, i64, i64, i32, i32,
                                       vp, vp, vp, vp, i64, vp, ctypes.c_size_t, vp],
         "combo_grouped_linear": [vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, i32, i64, i64, i64, vp],
@@ -78,7 +79,7 @@ def load():
     lib.combo_divergence_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_grad_scratch_bytes.argtypes = [i32]
     lib.combo_grad_scratch_bytes.restype = ctypes.c_size_t
-    lib.combo_group_norm_scratch_bytes.argtypes = [i64, i64, i64]
+    lib.combo_group_norm_scratch_bytes.argtypes = [i64, i64, i64, i32]
     lib.combo_group_norm_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_set_kernel_path.argtypes = [i32]
     lib.combo_set_kernel_path.restype = None
@@ -335,24 +336,23 @@ def _norm_args(name, x, others, gamma, beta, begin, stats, groups):
     return _SIZES[x.dtype], N, _SIZES[gamma.dtype], pitch
 
 
-def combo_group_norm(x, y, gamma, beta, begin, groups, eps, act, mean=None, rstd=None, scratch=None, stream=None):
+def combo_group_norm(x, y, gamma, beta, begin, groups, eps, act, mean, rstd, scratch, stream=None):
     """y = act(group norm of x), channels last: x, y [B, L, C]; gamma, beta [N, C] (views of flat
     parameter vectors, or None); begin: device int64 [N + 1], the workers' samples, or None for one
-    worker; mean, rstd: float32 [B, groups] or None.  The forward pass needs no scratch: it is
-    taken so that one set of arguments serves both directions."""
+    worker; mean, rstd: float32 [B, groups] or None; scratch: device memory of
+    combo_group_norm_scratch_bytes(B, L, C, groups) bytes."""
     name = "combo_group_norm"
     size, N, param_size, param_pitch = _norm_args(name, x, (y,), gamma, beta, begin, (mean, rstd), groups)
     B, L, C = shape = x.shape
     _check(load().combo_group_norm(x.data_ptr(), _pitch(shape, x.stride(), name, "x"), y.data_ptr(),
                                    _pitch(shape, y.stride(), name, "y"), size, _ptr(gamma), _ptr(beta), param_size,
                                    param_pitch, _ptr(begin), N, B, L, C, groups, eps, act, _ptr(mean), _ptr(rstd),
-                                   _stream(stream)), name)
+                                   _ptr(scratch), _bytes(scratch), _stream(stream)), name)
     return y
 
 
-def combo_group_norm_scratch_bytes(B: int, L: int, C: int, groups: int = 1) -> int:
-    """Bytes the backward pass wants (the same for any number of groups)."""
-    return int(load().combo_group_norm_scratch_bytes(B, L, C))
+def combo_group_norm_scratch_bytes(B: int, L: int, C: int, groups: int) -> int:
+    return int(load().combo_group_norm_scratch_bytes(B, L, C, groups))
 
 
 def combo_group_norm_backward(dy, x, dx, gamma, beta, begin, groups, act, mean, rstd, dgamma, dbeta, scratch,

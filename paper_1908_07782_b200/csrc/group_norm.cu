@@ -5,18 +5,24 @@
 //   dz = dy * act'(z),  dgamma_w = sum dz * h,  dbeta_w = sum dz,  t = dz * gamma_w
 //   dx = rstd * (t - mean(t) - h * mean(t * h))
 //
-// Bound by HBM: forward 1 read and 1 write of x, backward 2 reads and 1 write.  To read everything once, the unit of
-// work is a (sample, block of whole groups): its L x CB slab is brought into shared memory, reduced and written out
-// from there.  A cluster of up to 8 CTAs shares the slab along L and exchanges its sums through distributed shared
-// memory.  Every thread works on the vectors it loaded itself (thread = (row, column)).  Slabs that 8 CTAs cannot hold are read again from global memory (L2)
-// in place of shared memory (RES = false).
+// Bound by HBM: forward 1 read and 1 write of x, backward 2 reads and 1 write.  Two ways, by a rule on sizes (choose()):
+//
+//   resident   small inputs and short samples, one launch: a CTA brings the slab of a (sample, block of whole groups) into
+//              shared memory, reduces it and writes the result from there.  Every thread works on the vectors it loaded
+//              itself (thread = (row, column)).
+//   streamed   k_*_sums takes chunks of a sample straight from global memory into registers and leaves each chunk's sums
+//              in scratch; k_*_apply merges them and reads its chunk again, from L2 (126 MB) if that still holds it -- chunks
+//              are taken from the last one back.  A CTA has no phases in which its SM's memory pipe idles, which is worth
+//              more than the second read costs.
 //
 // Forward statistics: each thread takes mean and M2 (sum of squared deviations from its own mean) of its positions,
-// for each run of channels of its vector that lie in one group, and these are merged by counts: sum of n_i * mean_i for the mean, M2_i + n_i (mean_i - mean)^2 for M2.
-// Nothing is cancelled, whatever the size of the mean.
+// for each run of channels of its vector that lie in one group, and these are merged by counts: sum of n_i * mean_i for
+// the mean, M2_i + n_i (mean_i - mean)^2 for M2.  Nothing is cancelled, whatever the size of the mean.
 //
 // z is formed in the roundings of the formula as written (no FMA), in both directions alike: a value that the forward
 // pass clipped at zero is a value whose gradient the backward pass drops.
+#include <type_traits>
+
 #include "host_common.h"
 #include "step_common.cuh"
 
@@ -34,9 +40,9 @@ using combo_step::pair;
 using combo_step::warp_sum;
 
 constexpr int kThreads = 128;
-constexpr int kCtasPerSm = 4;           // that many slabs are in flight on an SM
+constexpr int kCtasPerSm = 4;           // resident: that many slabs are in flight on an SM
+constexpr int kStreamCtas = 3;          // streamed: with 160 registers a thread and two batches of loads under way; four and six were slower
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;          // portable cluster size
 
 struct NormParams {
     const unsigned char* x;
@@ -47,36 +53,23 @@ struct NormParams {
     const int64_t* begin;               // [N + 1], or NULL: one worker
     float* mean;                        // [B][G]
     float* rstd;
-    float2* partial;                    // backward: [B][C] sums of dz * h and dz of a CTA's samples of one worker, at the first of them
+    float2* chan;                       // backward: sums of dz * h and dz per channel; streamed [B][chunks][C]; resident [B][C],
+                                        // of a CTA's samples of one worker, at the first of them
+    float2* part;                       // streamed: [B][chunks][G] a chunk's mean and M2, or its sums of t and t * h
     long long x_pitch, y_pitch, dy_pitch, par_pitch;
     long long B;
-    int L, C, G, Cg, GB, nblk, CS, Lc, N, ns, par_bytes, sub;
+    int L, C, G, Cg, GB, nblk, chunks, Lc, N, ns, par_bytes, sub;
     float eps;
     // sub: channels of a vector that surely share a group, the largest power of two up to V that divides Cg
     int cb_max;                         // channels of a full block of groups, rounded up to a multiple of 4
+    float* dgamma;                      // backward
+    float* dbeta;
+    long long grad_pitch;
+    int param_ctas;                     // CTAs that add the parameters' gradients
     unsigned stat_off, par_off, grp_off, slab_off, slab_bytes;
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-// only tells the peers that this CTA has read what it wanted of theirs
-__device__ __forceinline__ void cluster_done() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-// positions of the slab that the cluster's CTA `rank` holds
-__device__ __forceinline__ int rank_len(const NormParams& p, int rank) { return max(0, min(p.Lc, p.L - rank * p.Lc)); }
-// float2 at the same shared-memory place of the cluster's CTA `rank`
-__device__ __forceinline__ float2 peer_float2(const float2* p, uint32_t rank) {
-    uint32_t a = smem_u32(p), r;
-    float2 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(r) : "memory");
-    return v;
-}
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ float load_par(const unsigned char* p, long long i, int bytes) {
@@ -126,6 +119,7 @@ template <int EB, bool VEC> struct Lane {
     static constexpr int V = VEC ? Elem<EB>::V : 1;
     static constexpr int VB = V * EB;
     static constexpr int P = VEC ? V / 2 : 1;
+    typedef typename std::conditional<VEC, uint4, typename std::conditional<EB == 4, float, unsigned short>::type>::type Raw;
     __device__ static __forceinline__ void unpack(uint32_t shared, f32x2 (&x)[P]) {
         if constexpr (VEC) {
             uint4 v;
@@ -134,23 +128,14 @@ template <int EB, bool VEC> struct Lane {
         } else if constexpr (EB == 4) {
             float v;
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(shared));
-            x[0] = pair(v, v);
+            widen(v, x);
         } else {
             unsigned short v;
             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(shared));
-            const float f = __uint_as_float((uint32_t)v << 16);
-            x[0] = pair(f, f);
+            widen(v, x);
         }
     }
-    __device__ static __forceinline__ void unpack(const unsigned char* q, f32x2 (&x)[P]) {
-        if constexpr (VEC) {
-            widen(*reinterpret_cast<const uint4*>(q), x);
-        } else {
-            const float v = Elem<EB>::get(q);
-            x[0] = pair(v, v);
-        }
-    }
-    __device__ static __forceinline__ void widen(const uint4& v, f32x2 (&x)[P]) {
+    __device__ static __forceinline__ void widen(const Raw& v, f32x2 (&x)[P]) {
         if constexpr (VEC) {
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -158,6 +143,11 @@ template <int EB, bool VEC> struct Lane {
                 if constexpr (EB == 2) x[i] = pair(combo_step::widen_lo(w[i]), combo_step::widen_hi(w[i]));
                 else x[i] = pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
             }
+        } else if constexpr (EB == 4) {
+            x[0] = pair(v, v);
+        } else {
+            const float f = __uint_as_float((uint32_t)v << 16);
+            x[0] = pair(f, f);
         }
     }
     __device__ static __forceinline__ void store(void* q, const f32x2 (&x)[P]) {
@@ -189,6 +179,34 @@ template <int EB, bool VEC> struct Lane {
                 if (sub >= 8) { x[0] = add2(x[0], x[2]); x[1] = x[2] = x[3] = x[0]; }
         }
     }
+    // Means m and M2 q of n values each, channel by channel, merged over each run, in every pair of the run.
+    __device__ static __forceinline__ void merge(f32x2 (&m)[P], f32x2 (&q)[P], int sub, float n) {
+        if constexpr (VEC) {
+            if (sub >= 2)
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const float d = lo_of(m[i]) - hi_of(m[i]), a = 0.5f * (lo_of(m[i]) + hi_of(m[i]));
+                    const float v = fmaf(0.5f * n * d, d, lo_of(q[i]) + hi_of(q[i]));
+                    m[i] = pair(a, a);
+                    q[i] = pair(v, v);
+                }
+            if (sub >= 4)
+#pragma unroll
+                for (int i = 0; i + 1 < P; i += 2) merge2(m[i], q[i], m[i + 1], q[i + 1], n);
+            if constexpr (P == 4)
+                if (sub >= 8) {
+                    merge2(m[0], q[0], m[2], q[2], 2.0f * n);
+                    m[1] = m[3] = m[0];
+                    q[1] = q[3] = q[0];
+                }
+        }
+    }
+    // two such pairs of 2 n values each, merged in both
+    __device__ static __forceinline__ void merge2(f32x2& m0, f32x2& q0, f32x2& m1, f32x2& q1, float n) {
+        const f32x2 d = add2(m0, neg2(m1)), half = pair(0.5f, 0.5f);
+        q0 = q1 = fma2(mul2(d, pair(n, n)), d, add2(q0, q1));
+        m0 = m1 = mul2(add2(m0, m1), half);
+    }
     // brings n vectors of one column, `step` bytes apart, into shared memory, `to_step` bytes apart
     __device__ static __forceinline__ void fetch(uint32_t to, uint32_t to_step, const unsigned char* q, long long step, int n) {
         if constexpr (VEC) {
@@ -213,38 +231,30 @@ template <int EB, bool VEC> struct Lane {
     }
 };
 
-// A thread's vectors of one column, one after another: in shared memory, or where they came from.
-template <bool RES> struct Walk;
-template <> struct Walk<true> {
+// A thread's vectors of one column of a slab in shared memory, one after another.
+struct Walk {
     uint32_t q, step;
-    __device__ __forceinline__ Walk(uint32_t slab, int vb, int nv, int rows, int trow, int col, const unsigned char*, long long)
+    __device__ __forceinline__ Walk(uint32_t slab, int vb, int nv, int rows, int trow, int col)
         : q(slab + (uint32_t)((trow * nv + col) * vb)), step((uint32_t)(rows * nv * vb)) {}
     __device__ __forceinline__ void next() { q += step; }
 };
-template <> struct Walk<false> {
-    const unsigned char* q;
-    long long step;
-    __device__ __forceinline__ Walk(uint32_t, int vb, int, int rows, int trow, int col, const unsigned char* g, long long pitch)
-        : q(g + trow * pitch + col * vb), step(rows * pitch) {}
-    __device__ __forceinline__ void next() { q += step; }
-};
 
-// What a CTA works on, the same in both directions.
+// What a CTA works on: a chunk of positions of a block of groups of a sample (resident: of a lot of p.ns samples).
 template <int V> struct Place {
-    int rank, g0, ng, c0, cb, nv, nl, l0, rows, cstep, trow, tcol, sub, base, extra;
-    long long unit;
-    __device__ __forceinline__ Place(const NormParams& p) {
+    int chunk, g0, ng, c0, cb, nv, nl, l0, rows, cstep, trow, tcol, sub, base, extra;
+    long long lot;
+    __device__ __forceinline__ Place(const NormParams& p, unsigned unit) {
         const int tid = threadIdx.x;
-        rank = p.CS > 1 ? (int)cluster_rank() : 0;
-        const unsigned u = blockIdx.x / (unsigned)p.CS;
-        unit = u / (unsigned)p.nblk;
+        unsigned u = unit / (unsigned)p.chunks;
+        chunk = (int)(unit - u * p.chunks);
+        lot = u / (unsigned)p.nblk;
         g0 = (int)(u % (unsigned)p.nblk) * p.GB;
         ng = min(p.GB, p.G - g0);
         c0 = g0 * p.Cg;
         cb = ng * p.Cg;
         nv = cb / V;
-        l0 = rank * p.Lc;
-        nl = rank_len(p, rank);
+        l0 = chunk * p.Lc;
+        nl = min(p.Lc, p.L - l0);
         rows = nv < kThreads ? kThreads / nv : 1;
         cstep = nv < kThreads ? nv : kThreads;
         trow = tid / cstep;
@@ -280,32 +290,151 @@ template <typename Ln> __device__ __forceinline__ void group_pairs(const float2*
     }
 }
 
-template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm(const NormParams p) {
+// Lanes that share a group, out of a warp: as many as it has entries, a power of two.
+__device__ __forceinline__ int lanes_for(int entries) {
+    int n = 1;
+    while (n < entries && n < 32) n *= 2;
+    return n;
+}
+// sum over neighbouring lots of n lanes
+__device__ __forceinline__ float lot_sum(float v, int n) {
+    for (int o = n / 2; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Merges a block's entries (mean, M2) of runs, [rows][cb / sub], each with the count of its row, to one pair for each group,
+// which one lane passes on.
+template <typename At, typename F> __device__ __forceinline__ void merge_groups(const NormParams& p, const At& at, const float2* stat, F out) {
+    const int per = p.Cg / at.sub, runs = at.cb / at.sub, entries = at.rows * per;
+    const int n = lanes_for(entries), lane = threadIdx.x & (n - 1), lots = kThreads / n;
+    const float inv = 1.0f / (float)((long long)at.nl * p.Cg);
+    for (int g0 = 0; g0 < at.ng; g0 += lots) {
+        const int g = g0 + (int)threadIdx.x / n;
+        const bool mine = g < at.ng;
+        float s = 0.0f, q = 0.0f;
+        for (int i = lane; mine && i < entries; i += n) {
+            const int r = per == 1 ? i : i / per;
+            s = fmaf((float)(at.positions(r) * at.sub), stat[r * runs + g * per + i - r * per].x, s);
+        }
+        const float m = lot_sum(s, n) * inv;
+        for (int i = lane; mine && i < entries; i += n) {
+            const int r = per == 1 ? i : i / per;
+            const float2 e = stat[r * runs + g * per + i - r * per];
+            const float d = e.x - m;
+            q += fmaf((float)(at.positions(r) * at.sub) * d, d, e.y);
+        }
+        q = lot_sum(q, n);
+        if (mine && lane == 0) out(g, m, q);
+    }
+}
+// A thread's entries for merge_groups: (negated) means and M2 of a vector's runs.
+template <typename Ln> __device__ __forceinline__ void store_runs(float2* mine, int sub, const f32x2 (&neg_m)[Ln::P], const f32x2 (&q)[Ln::P]) {
+#pragma unroll
+    for (int i = 0; i < Ln::P; ++i) {
+        if (2 * i % sub == 0) mine[2 * i / sub] = make_float2(-lo_of(neg_m[i]), lo_of(q[i]));
+        if (Ln::V > 1 && sub == 1) mine[2 * i + 1] = make_float2(-hi_of(neg_m[i]), hi_of(q[i]));
+    }
+}
+template <typename Ln, int ACT>
+__device__ __forceinline__ void forward_vector(f32x2 (&v)[Ln::P], const f32x2 (&m)[Ln::P], const f32x2 (&rs)[Ln::P], const f32x2 (&ga)[Ln::P],
+                                               const f32x2 (&be)[Ln::P]) {
+#pragma unroll
+    for (int i = 0; i < Ln::P; ++i) {
+        const f32x2 z = affine(normed(v[i], m[i], rs[i]), ga[i], be[i]);
+        v[i] = pair(activate<ACT>(lo_of(z)), activate<ACT>(hi_of(z)));
+    }
+}
+// h and dz of a pair of values
+template <int ACT>
+__device__ __forceinline__ void back_pair(f32x2 x, f32x2 d, f32x2 m, f32x2 rs, f32x2 ga, f32x2 be, f32x2& h, f32x2& dz) {
+    h = normed(x, m, rs);
+    const f32x2 z = affine(h, ga, be);
+    dz = pair(back_activate<ACT>(lo_of(d), lo_of(z)), back_activate<ACT>(hi_of(d), hi_of(z)));
+}
+template <typename Ln, int ACT>
+__device__ __forceinline__ void back_vector(f32x2 (&v)[Ln::P], const f32x2 (&d)[Ln::P], const f32x2 (&m)[Ln::P], const f32x2 (&rs)[Ln::P],
+                                            const f32x2 (&ga)[Ln::P], const f32x2 (&be)[Ln::P], const f32x2 (&neg_m1)[Ln::P], const f32x2 (&m2)[Ln::P]) {
+#pragma unroll
+    for (int i = 0; i < Ln::P; ++i) {
+        f32x2 h, dz;
+        back_pair<ACT>(v[i], d[i], m[i], rs[i], ga[i], be[i], h, dz);
+        v[i] = mul2(rs[i], fma2(neg2(h), m2[i], fma2(dz, ga[i], neg_m1[i])));
+    }
+}
+
+// Adds the block's table of sums, [P][rows][nv] of (dz * h, dz) for pairs of channels, over the rows: out(channel, sums).
+// Rows are added in lots side by side, then the lots.  The block; the table is overwritten.
+template <typename Ln, typename At, typename F> __device__ __forceinline__ void add_rows(const At& at, float4* stat, F out) {
+    const int tid = threadIdx.x, nv = at.nv, rows = at.rows;
+    const int pairs = nv * Ln::P, parts = min(max(kThreads / pairs, 1), rows);
+    if (parts > 1) {                             // pair k = (i, col): its rows lie nv entries apart
+        const int part = tid / pairs, k = tid - part * pairs, i = k / nv;
+        float4* mine = stat + i * (rows - 1) * nv + k;
+        if (part < parts) {
+            float4 s = mine[part * nv];
+            for (int r = part + parts; r < rows; r += parts) {
+                const float4 e = mine[r * nv];
+                s.x += e.x; s.y += e.y; s.z += e.z; s.w += e.w;
+            }
+            mine[part * nv] = s;                 // row `part` is read by this thread alone
+        }
+        __syncthreads();
+    }
+    for (int k = tid; k < pairs; k += kThreads) {
+        const int i = k / nv, col = k - i * nv;
+        const float4* mine = stat + i * rows * nv + col;
+        float4 s = mine[0];
+        const int n = parts > 1 ? parts : rows;
+        for (int r = 1; r < n; ++r) {
+            const float4 e = mine[r * nv];
+            s.x += e.x; s.y += e.y; s.z += e.z; s.w += e.w;
+        }
+        const int c = col * Ln::V + 2 * i;
+        out(c, make_float2(s.x, s.z));
+        if (Ln::V > 1) out(c + 1, make_float2(s.y, s.w));
+    }
+}
+// Sums of t = dz * gamma and of t * h over each group's channels, which one lane passes on.
+template <typename At, typename F>
+__device__ __forceinline__ void add_groups(const NormParams& p, const At& at, const float2* chan, const float* ga_s, F out) {
+    const int n = lanes_for(p.Cg), lane = threadIdx.x & (n - 1), lots = kThreads / n;
+    for (int g0 = 0; g0 < at.ng; g0 += lots) {
+        const int g = g0 + (int)threadIdx.x / n;
+        const bool mine = g < at.ng;
+        float t = 0.0f, th = 0.0f;
+        for (int c = g * p.Cg + lane; mine && c < (g + 1) * p.Cg; c += n) {
+            const float2 s = chan[c];
+            th = fmaf(ga_s[c], s.x, th);
+            t = fmaf(ga_s[c], s.y, t);
+        }
+        t = lot_sum(t, n);
+        th = lot_sum(th, n);
+        if (mine && lane == 0) out(g, t, th);
+    }
+}
+
+// ---------------------------------------------------------------- resident
+template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm(const NormParams p) {
     using Ln = Lane<EB, VEC>;
     constexpr int V = Ln::V, VB = Ln::VB, P = Ln::P;
     extern __shared__ __align__(128) unsigned char smem[];
     float2* stat = reinterpret_cast<float2*>(smem + p.stat_off);       // [rows][cb / sub] mean, M2 of a thread's runs
     float* ga_s = reinterpret_cast<float*>(smem + p.par_off);          // [cb]
     float* be_s = ga_s + p.cb_max;                                     // [cb]
-    float2* grp = reinterpret_cast<float2*>(smem + p.grp_off);         // [GB] this CTA's mean and M2, read by the cluster
-    float2* fin = grp + p.GB;                                          // [GB] mean and rstd
+    float2* fin = reinterpret_cast<float2*>(smem + p.grp_off);         // [GB] mean and rstd
     const uint32_t slab = smem_u32(smem + p.slab_off);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const Place<V> at(p);
-    const int nl = at.nl, nv = at.nv, rows = at.rows;
-    const long long b = at.unit;
+    const Place<V> at(p, blockIdx.x);
+    const int nv = at.nv, rows = at.rows;
+    const long long b = at.lot;
     const long long xp = p.x_pitch * EB, yp = p.y_pitch * EB;
-    const unsigned char* x = p.x + (b * p.L + at.l0) * xp + (long long)at.c0 * EB;
-    unsigned char* y = p.y + (b * p.L + at.l0) * yp + (long long)at.c0 * EB;
+    const unsigned char* x = p.x + b * p.L * xp + (long long)at.c0 * EB;
+    unsigned char* y = p.y + b * p.L * yp + (long long)at.c0 * EB;
     const int n = at.positions(at.trow);        // of this thread
-    const auto walk = [&](int col) { return Walk<RES>(slab, VB, nv, rows, at.trow, col, x, xp); };
-    if (RES)
-        for (int col = at.tcol; col < nv; col += at.cstep) {
-            const Walk<true> to(slab, VB, nv, rows, at.trow, col, x, xp);
-            Ln::fetch(to.q, to.step, x + at.trow * xp + col * VB, rows * xp, n);
-        }
+    for (int col = at.tcol; col < nv; col += at.cstep) {
+        const Walk to(slab, VB, nv, rows, at.trow, col);
+        Ln::fetch(to.q, to.step, x + at.trow * xp + col * VB, rows * xp, n);
+    }
     load_params(p, worker_of(p, b), at.c0, at.cb, ga_s, be_s);
-    if (RES) cp_async_wait();
+    cp_async_wait();
 
     const int runs = at.cb / at.sub;
     const float inv = 1.0f / (float)max(n * at.sub, 1);
@@ -313,7 +442,7 @@ template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__
         f32x2 m[P], q[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) m[i] = q[i] = 0;
-        auto at_v = walk(col);
+        Walk at_v(slab, VB, nv, rows, at.trow, col);
 #pragma unroll 4
         for (int k = 0; k < n; ++k, at_v.next()) {
             f32x2 v[P];
@@ -324,7 +453,7 @@ template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__
         Ln::fold(m, at.sub);
 #pragma unroll
         for (int i = 0; i < P; ++i) m[i] = neg2(mul2(m[i], pair(inv, inv)));
-        at_v = walk(col);
+        at_v = Walk(slab, VB, nv, rows, at.trow, col);
 #pragma unroll 4
         for (int k = 0; k < n; ++k, at_v.next()) {
             f32x2 v[P];
@@ -336,131 +465,68 @@ template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__
             }
         }
         Ln::fold(q, at.sub);
-        float2* mine = stat + at.trow * runs + col * V / at.sub;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            if (2 * i % at.sub == 0) mine[2 * i / at.sub] = make_float2(-lo_of(m[i]), lo_of(q[i]));
-            if (VEC && at.sub == 1) mine[2 * i + 1] = make_float2(-hi_of(m[i]), hi_of(q[i]));
-        }
+        store_runs<Ln>(stat + at.trow * runs + col * V / at.sub, at.sub, m, q);
     }
     __syncthreads();
-    // a warp per group: merge of rows * (Cg / sub) entries, each with the count of its row
-    const int per = p.Cg / at.sub;
-    for (int g = warp; g < at.ng; g += kWarps) {
-        const int entries = rows * per;
-        float s = 0.0f, q = 0.0f;
-        for (int i = lane; i < entries; i += 32) {
-            const int r = per == 1 ? i : i / per;
-            s = fmaf((float)(at.positions(r) * at.sub), stat[r * runs + g * per + i - r * per].x, s);
-        }
-        const float m = nl > 0 ? warp_sum(s) / (float)((long long)nl * p.Cg) : 0.0f;
-        for (int i = lane; i < entries; i += 32) {
-            const int r = per == 1 ? i : i / per;
-            const float2 e = stat[r * runs + g * per + i - r * per];
-            const float d = e.x - m;
-            q += fmaf((float)(at.positions(r) * at.sub) * d, d, e.y);
-        }
-        q = warp_sum(q);
-        if (lane == 0) grp[g] = make_float2(m, q);
-    }
-    if (p.CS > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-    for (int g = tid; g < at.ng; g += kThreads) {
-        const float total = (float)((long long)p.L * p.Cg);
-        float m = grp[g].x, q = grp[g].y;
-        if (p.CS > 1) {
-            float2 e[kMaxCluster];
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r)
-                if (r < p.CS) e[r] = peer_float2(grp + g, r);
-            float s = 0.0f;
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r)
-                if (r < p.CS) s = fmaf((float)((long long)rank_len(p, r) * p.Cg), e[r].x, s);
-            m = s / total;
-            q = 0.0f;
-#pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r)
-                if (r < p.CS) {
-                    const float d = e[r].x - m;
-                    q += fmaf((float)((long long)rank_len(p, r) * p.Cg) * d, d, e[r].y);
-                }
-        }
-        const float rs = 1.0f / sqrtf(q / total + p.eps);
+    merge_groups(p, at, stat, [&](int g, float m, float q) {
+        const float rs = 1.0f / sqrtf(q / (float)((long long)p.L * p.Cg) + p.eps);
         fin[g] = make_float2(m, rs);
-        if (at.rank == 0) {
-            if (p.mean) p.mean[b * p.G + at.g0 + g] = m;
-            if (p.rstd) p.rstd[b * p.G + at.g0 + g] = rs;
-        }
-    }
+        if (p.mean) p.mean[b * p.G + at.g0 + g] = m;
+        if (p.rstd) p.rstd[b * p.G + at.g0 + g] = rs;
+    });
     __syncthreads();
-    if (p.CS > 1) cluster_done();               // peers' sums are read; waited for before this CTA leaves
     for (int col = at.tcol; col < nv; col += at.cstep) {
         f32x2 m[P], rs[P], ga[P], be[P];
         group_pairs<Ln>(fin, col * V, p.Cg, at.sub, m, rs);
         Ln::table(ga_s + col * V, ga);
         Ln::table(be_s + col * V, be);
-        auto at_v = walk(col);
+        Walk at_v(slab, VB, nv, rows, at.trow, col);
         unsigned char* to = y + at.trow * yp + col * VB;
 #pragma unroll 4
         for (int k = 0; k < n; ++k, at_v.next(), to += rows * yp) {
             f32x2 v[P];
             Ln::unpack(at_v.q, v);
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                const f32x2 z = affine(normed(v[i], m[i], rs[i]), ga[i], be[i]);
-                v[i] = pair(activate<ACT>(lo_of(z)), activate<ACT>(hi_of(z)));
-            }
+            forward_vector<Ln, ACT>(v, m, rs, ga, be);
             Ln::store(to, v);
         }
     }
-    if (p.CS > 1) cluster_wait();
 }
 
-template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm_back(const NormParams p) {
+template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm_back(const NormParams p) {
     using Ln = Lane<EB, VEC>;
     constexpr int V = Ln::V, VB = Ln::VB, P = Ln::P;
     extern __shared__ __align__(128) unsigned char smem[];
     float4* stat = reinterpret_cast<float4*>(smem + p.stat_off);       // [P][rows][nv] a thread's sums of dz * h and of dz, by pairs of channels
     float* ga_s = reinterpret_cast<float*>(smem + p.par_off);          // [cb]
     float* be_s = ga_s + p.cb_max;                                     // [cb]
-    float2* grp = reinterpret_cast<float2*>(smem + p.grp_off);         // [GB] sums of t and t * h of this CTA
-    float2* fin = grp + p.GB;                                          // [GB] their means over the whole slab
+    float2* fin = reinterpret_cast<float2*>(smem + p.grp_off);         // [GB] means of t and t * h
     float2* norm = fin + p.GB;                                         // [GB] mean and rstd
-    float2* chan = norm + p.GB;                                        // [cb] this CTA's sums per channel
+    float2* chan = norm + p.GB;                                        // [cb] sums per channel
     float2* acc = chan + p.cb_max;                                     // [cb] the same over the worker's samples
     const uint32_t slab = smem_u32(smem + p.slab_off);
     combo_step::pdl_release();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const Place<V> at(p);
-    const int nl = at.nl, nv = at.nv, rows = at.rows, cb = at.cb;
+    const int tid = threadIdx.x;
+    const Place<V> at(p, blockIdx.x);
+    const int nv = at.nv, rows = at.rows, cb = at.cb;
     const long long xp = p.x_pitch * EB, yp = p.y_pitch * EB, dp = p.dy_pitch * EB;
-    const long long b0 = at.unit * p.ns, b1 = min(b0 + p.ns, p.B);
+    const long long b0 = at.lot * p.ns, b1 = min(b0 + p.ns, p.B);
     const float inv = 1.0f / (float)((long long)p.L * p.Cg);
     const int n = at.positions(at.trow);        // of this thread
-    // rows of the table of sums are added in `parts` lots side by side, then the lots
-    const int pairs = nv * P, parts = min(max(kThreads / pairs, 1), rows);
-    const auto add_channel = [&](int c, float2 s) {
-        chan[c] = s;
-        if (p.CS == 1) acc[c] = make_float2(acc[c].x + s.x, acc[c].y + s.y);
-    };
     int w = -1;
     long long wb = b0;                          // the worker's first sample here
     for (long long b = b0; b < b1; ++b) {
-        const long long first = b * p.L + at.l0;
-        const unsigned char* x = p.x + first * xp + (long long)at.c0 * EB;
-        const unsigned char* dy = p.dy + first * dp + (long long)at.c0 * EB;
-        unsigned char* dx = p.y + first * yp + (long long)at.c0 * EB;
-        if (RES) {
-            for (int col = at.tcol; col < nv; col += at.cstep) {
-                const Walk<true> to(slab, VB, nv, rows, at.trow, col, x, xp);
-                Ln::fetch(to.q, to.step, x + at.trow * xp + col * VB, rows * xp, n);
-                Ln::fetch(to.q + p.slab_bytes, to.step, dy + at.trow * dp + col * VB, rows * dp, n);
-            }
+        const unsigned char* x = p.x + b * p.L * xp + (long long)at.c0 * EB;
+        const unsigned char* dy = p.dy + b * p.L * dp + (long long)at.c0 * EB;
+        unsigned char* dx = p.y + b * p.L * yp + (long long)at.c0 * EB;
+        for (int col = at.tcol; col < nv; col += at.cstep) {
+            const Walk to(slab, VB, nv, rows, at.trow, col);
+            Ln::fetch(to.q, to.step, x + at.trow * xp + col * VB, rows * xp, n);
+            Ln::fetch(to.q + p.slab_bytes, to.step, dy + at.trow * dp + col * VB, rows * dp, n);
         }
         const int owner = worker_of(p, b);
-        if (owner != w) {                       // (behind worker_of's or the loop's barrier) the channels' sums of the worker before leave for its slot
+        if (owner != w) {                       // (behind the loop's barrier) the sums of the worker before leave for their slot
             for (int c = tid; c < cb; c += kThreads) {
-                if (w >= 0) p.partial[wb * p.C + at.c0 + c] = acc[c];
+                if (w >= 0) p.chan[wb * p.C + at.c0 + c] = acc[c];
                 acc[c] = make_float2(0.0f, 0.0f);
             }
             load_params(p, owner, at.c0, cb, ga_s, be_s);
@@ -469,9 +535,7 @@ template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__
         }
         for (int g = tid; g < at.ng; g += kThreads) norm[g] = make_float2(p.mean[b * p.G + at.g0 + g], p.rstd[b * p.G + at.g0 + g]);
         __syncthreads();
-        if (RES) cp_async_wait();
-        const auto walk = [&](int col) { return Walk<RES>(slab, VB, nv, rows, at.trow, col, x, xp); };
-        const auto dwalk = [&](int col) { return Walk<RES>(slab + p.slab_bytes, VB, nv, rows, at.trow, col, dy, dp); };
+        cp_async_wait();
         for (int col = at.tcol; col < nv; col += at.cstep) {
             f32x2 m[P], rs[P], ga[P], be[P], s1[P], s2[P];
             group_pairs<Ln>(norm, col * V, p.Cg, at.sub, m, rs);
@@ -479,17 +543,16 @@ template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__
             Ln::table(be_s + col * V, be);
 #pragma unroll
             for (int i = 0; i < P; ++i) s1[i] = s2[i] = 0;
-            auto at_v = walk(col);
-            auto at_d = dwalk(col);
+            Walk at_v(slab, VB, nv, rows, at.trow, col);
 #pragma unroll 2
-            for (int k = 0; k < n; ++k, at_v.next(), at_d.next()) {
+            for (int k = 0; k < n; ++k, at_v.next()) {
                 f32x2 v[P], d[P];
                 Ln::unpack(at_v.q, v);
-                Ln::unpack(at_d.q, d);
+                Ln::unpack(at_v.q + p.slab_bytes, d);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const f32x2 h = normed(v[i], m[i], rs[i]), z = affine(h, ga[i], be[i]);
-                    const f32x2 dz = pair(back_activate<ACT>(lo_of(d[i]), lo_of(z)), back_activate<ACT>(hi_of(d[i]), hi_of(z)));
+                    f32x2 h, dz;
+                    back_pair<ACT>(v[i], d[i], m[i], rs[i], ga[i], be[i], h, dz);
                     s1[i] = fma2(dz, h, s1[i]);
                     s2[i] = add2(s2[i], dz);
                 }
@@ -499,111 +562,297 @@ template <int EB, bool VEC, bool RES, int ACT> __global__ void __launch_bounds__
                 stat[(i * rows + at.trow) * nv + col] = make_float4(lo_of(s1[i]), hi_of(s1[i]), lo_of(s2[i]), hi_of(s2[i]));
         }
         __syncthreads();
-        if (parts > 1) {                         // pair k = (i, col): its rows lie nv entries apart
-            const int part = tid / pairs, k = tid - part * pairs, i = k / nv;
-            float4* mine = stat + i * (rows - 1) * nv + k;
-            if (part < parts) {
-                float4 s = mine[part * nv];
-                for (int r = part + parts; r < rows; r += parts) {
-                    const float4 e = mine[r * nv];
-                    s.x += e.x; s.y += e.y; s.z += e.z; s.w += e.w;
-                }
-                mine[part * nv] = s;             // row `part` is read by this thread alone
-            }
-            __syncthreads();
-        }
-        for (int k = tid; k < pairs; k += kThreads) {
-            const int i = k / nv, col = k - i * nv;
-            const float4* mine = stat + i * rows * nv + col;
-            float4 s = mine[0];
-            for (int r = 1; r < parts; ++r) {
-                const float4 e = mine[r * nv];
-                s.x += e.x; s.y += e.y; s.z += e.z; s.w += e.w;
-            }
-            const int c = col * V + 2 * i;
-            add_channel(c, make_float2(s.x, s.z));
-            if (VEC) add_channel(c + 1, make_float2(s.y, s.w));
-        }
+        add_rows<Ln>(at, stat, [&](int c, float2 s) {
+            chan[c] = s;
+            acc[c] = make_float2(acc[c].x + s.x, acc[c].y + s.y);
+        });
         __syncthreads();
-        for (int g = warp; g < at.ng; g += kWarps) {
-            float t = 0.0f, th = 0.0f;
-            for (int c = g * p.Cg + lane; c < (g + 1) * p.Cg; c += 32) {
-                const float2 s = chan[c];
-                th = fmaf(ga_s[c], s.x, th);
-                t = fmaf(ga_s[c], s.y, t);
-            }
-            t = warp_sum(t);
-            th = warp_sum(th);
-            if (lane == 0) grp[g] = make_float2(t, th);
-        }
-        if (p.CS > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-        for (int g = tid; g < at.ng; g += kThreads) {
-            float2 s = p.CS > 1 ? make_float2(0.0f, 0.0f) : grp[g];
-            for (int r = 0; p.CS > 1 && r < p.CS; ++r) {
-                const float2 e = peer_float2(grp + g, r);
-                s.x += e.x;
-                s.y += e.y;
-            }
-            fin[g] = make_float2(s.x * inv, s.y * inv);
-        }
-        if (p.CS > 1) {                          // the cluster's CTAs share the channels among them
-            for (int c = tid * p.CS + at.rank; c < cb; c += kThreads * p.CS) {
-                float2 s = make_float2(0.0f, 0.0f);
-                for (int r = 0; r < p.CS; ++r) {
-                    const float2 e = peer_float2(chan + c, r);
-                    s.x += e.x;
-                    s.y += e.y;
-                }
-                p.partial[b * p.C + at.c0 + c] = s;
-            }
-        }
+        add_groups(p, at, chan, ga_s, [&](int g, float t, float th) { fin[g] = make_float2(t * inv, th * inv); });
         __syncthreads();
-        if (p.CS > 1) cluster_done();
         for (int col = at.tcol; col < nv; col += at.cstep) {
             f32x2 m[P], rs[P], ga[P], be[P], m1[P], m2[P];
             group_pairs<Ln>(norm, col * V, p.Cg, at.sub, m, rs);
             group_pairs<Ln>(fin, col * V, p.Cg, at.sub, m1, m2);
             Ln::table(ga_s + col * V, ga);
             Ln::table(be_s + col * V, be);
-            auto at_v = walk(col);
-            auto at_d = dwalk(col);
+            Walk at_v(slab, VB, nv, rows, at.trow, col);
             unsigned char* to = dx + at.trow * yp + col * VB;
 #pragma unroll 2
-            for (int k = 0; k < n; ++k, at_v.next(), at_d.next(), to += rows * yp) {
+            for (int k = 0; k < n; ++k, at_v.next(), to += rows * yp) {
                 f32x2 v[P], d[P];
                 Ln::unpack(at_v.q, v);
-                Ln::unpack(at_d.q, d);
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const f32x2 h = normed(v[i], m[i], rs[i]), z = affine(h, ga[i], be[i]);
-                    const f32x2 dz = pair(back_activate<ACT>(lo_of(d[i]), lo_of(z)), back_activate<ACT>(hi_of(d[i]), hi_of(z)));
-                    v[i] = mul2(rs[i], fma2(neg2(h), m2[i], fma2(dz, ga[i], m1[i])));    // m1 comes negated
-                }
+                Ln::unpack(at_v.q + p.slab_bytes, d);
+                back_vector<Ln, ACT>(v, d, m, rs, ga, be, m1, m2);
                 Ln::store(to, v);
             }
         }
-        if (p.CS > 1) cluster_wait();            // ns is 1 here: the last thing this CTA does
-        else __syncthreads();                    // the tables are free for the next sample
+        __syncthreads();                         // the tables are free for the next sample
     }
-    if (p.CS == 1)                               // the loop's last barrier has made acc whole
-        for (int c = tid; c < cb; c += kThreads) p.partial[wb * p.C + at.c0 + c] = acc[c];
+    for (int c = tid; c < cb; c += kThreads) p.chan[wb * p.C + at.c0 + c] = acc[c];
 }
 
-// dgamma and dbeta of worker blockIdx.y: what each CTA left at its first sample of the worker, added in a fixed order.
-constexpr int kSumRows = 8;
-__global__ void __launch_bounds__(32 * kSumRows) k_norm_params(const NormParams p, float* dgamma, float* dbeta, long long pitch) {
-    __shared__ float2 sh[kSumRows][32];
+// ---------------------------------------------------------------- streamed
+// A thread's vectors of one column in global memory, N at a time in registers.
+template <int EB, bool VEC, int N> struct Batch {
+    using Ln = Lane<EB, VEC>;
+    typename Ln::Raw raw[N];
+    // the first n of them
+    __device__ __forceinline__ void load(const unsigned char* q, long long step, int n) {
+        if (n >= N) {
+#pragma unroll
+            for (int j = 0; j < N; ++j, q += step) raw[j] = *reinterpret_cast<const typename Ln::Raw*>(q);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (j < n) raw[j] = *reinterpret_cast<const typename Ln::Raw*>(q + j * step);
+        }
+    }
+};
+constexpr int kBatch = 8, kPair = 4;     // vectors a thread asks for at once, of one array and of each of two
+
+template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads, kStreamCtas) k_norm_sums(const NormParams p) {
+    using Ln = Lane<EB, VEC>;
+    constexpr int V = Ln::V, VB = Ln::VB, P = Ln::P;
+    extern __shared__ __align__(128) unsigned char smem[];
+    float2* stat = reinterpret_cast<float2*>(smem + p.stat_off);
+    combo_step::pdl_release();
+    const Place<V> at(p, blockIdx.x);
+    const long long b = at.lot, xp = p.x_pitch * EB, step = at.rows * xp;
+    const unsigned char* x = p.x + (b * p.L + at.l0 + at.trow) * xp + (long long)at.c0 * EB;
+    const int n = at.positions(at.trow);
+    for (int col = at.tcol; col < at.nv; col += at.cstep) {
+        // sums of the distances from a channel's first value and of their squares: mean and M2 of the thread's few
+        // positions by one pass (the first value lies among them, so the squares do not outgrow what they measure)
+        f32x2 pivot[P], s[P], q[P];
+        const unsigned char* from = x + col * VB;
+        if (n > 0) Ln::widen(*reinterpret_cast<const typename Ln::Raw*>(from), pivot);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            pivot[i] = n > 0 ? neg2(pivot[i]) : 0;
+            s[i] = q[i] = 0;
+        }
+        const auto take = [&](const typename Ln::Raw& raw) {
+            f32x2 e[P];
+            Ln::widen(raw, e);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const f32x2 d = add2(e[i], pivot[i]);
+                s[i] = add2(s[i], d);
+                q[i] = fma2(d, d, q[i]);
+            }
+        };
+        Batch<EB, VEC, kBatch> v, next;          // the next ones are under way while these are added
+        next.load(from, step, n);
+        for (int k = 0; k < n; k += kBatch) {
+            v = next;
+            from += kBatch * step;
+            next.load(from, step, n - k - kBatch);
+            if (n - k >= kBatch) {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) take(v.raw[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    if (j < n - k) take(v.raw[j]);
+            }
+        }
+        // (negated) mean and M2 of each channel, then of each run: equal counts merge as means and half squared distances
+        const float inv = 1.0f / (float)max(n, 1);
+        f32x2 m[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            m[i] = fma2(s[i], pair(-inv, -inv), pivot[i]);
+            q[i] = fma2(neg2(s[i]), mul2(s[i], pair(inv, inv)), q[i]);
+        }
+        Ln::merge(m, q, at.sub, (float)n);
+        store_runs<Ln>(stat + at.trow * (at.cb / at.sub) + col * V / at.sub, at.sub, m, q);
+    }
+    __syncthreads();
+    merge_groups(p, at, stat, [&](int g, float m, float q) {
+        p.part[(b * p.chunks + at.chunk) * p.G + at.g0 + g] = make_float2(m, q);
+    });
+}
+
+// Adds what the sample's chunks left for each of the block's groups, groups side by side and a group's chunks in lots:
+// acc = add(chunk's pair, first chunk's pair, chunk, acc), then done(group, sums, first chunk's pair).  The block.
+template <typename At, typename A, typename D>
+__device__ __forceinline__ void gather_chunks(const NormParams& p, const At& at, float2* lots, A add, D done) {
+    const int parts = max(kThreads / at.ng, 1), part = (int)threadIdx.x / at.ng;
+    const float2* e = p.part + at.lot * p.chunks * p.G + at.g0;
+    if (part < parts)
+        for (int g = (int)threadIdx.x - part * at.ng; g < at.ng; g += kThreads) {
+            const float2 v0 = e[g];
+            float2 acc = make_float2(0.0f, 0.0f);
+#pragma unroll 8
+            for (int k = part; k < p.chunks; k += parts) acc = add(e[(long long)k * p.G + g], v0, k, acc);
+            if (parts == 1) done(g, acc, v0);
+            else lots[part * at.ng + g] = acc;
+        }
+    if (parts == 1) return;
+    __syncthreads();
+    for (int g = threadIdx.x; g < at.ng; g += kThreads) {
+        float2 s = lots[g];
+        for (int r = 1; r < parts; ++r) { s.x += lots[r * at.ng + g].x; s.y += lots[r * at.ng + g].y; }
+        done(g, s, e[g]);
+    }
+}
+
+template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads, kStreamCtas) k_norm_apply(const NormParams p) {
+    using Ln = Lane<EB, VEC>;
+    constexpr int V = Ln::V, VB = Ln::VB, P = Ln::P;
+    extern __shared__ __align__(128) unsigned char smem[];
+    float* ga_s = reinterpret_cast<float*>(smem + p.par_off);
+    float* be_s = ga_s + p.cb_max;
+    float2* fin = reinterpret_cast<float2*>(smem + p.grp_off);
+    float2* lots = reinterpret_cast<float2*>(smem + p.stat_off);
+    const Place<V> at(p, gridDim.x - 1 - blockIdx.x);
+    const long long b = at.lot, xp = p.x_pitch * EB, yp = p.y_pitch * EB, step = at.rows * xp;
+    const unsigned char* x = p.x + (b * p.L + at.l0 + at.trow) * xp + (long long)at.c0 * EB;
+    unsigned char* y = p.y + (b * p.L + at.l0 + at.trow) * yp + (long long)at.c0 * EB;
+    const int n = at.positions(at.trow);
+    Batch<EB, VEC, kBatch> r, next;              // the next ones are under way while these are taken
+    if (at.tcol < at.nv) next.load(x + at.tcol * VB, step, n);
+    load_params(p, worker_of(p, b), at.c0, at.cb, ga_s, be_s);
     combo_step::pdl_wait();
-    const int w = blockIdx.y, lane = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + lane;
+    // the chunks' pairs merged by counts, about the first chunk's mean
+    gather_chunks(p, at, lots, [&](float2 v, float2 v0, int k, float2 acc) {
+        const float cnt = (float)((long long)min(p.Lc, p.L - k * p.Lc) * p.Cg), d = v.x - v0.x;
+        return make_float2(fmaf(cnt, d, acc.x), acc.y + fmaf(cnt * d, d, v.y));
+    }, [&](int g, float2 s, float2 v0) {
+        const float total = (float)((long long)p.L * p.Cg), off = s.x / total;
+        const float around = fmaf(-s.x, off, s.y);       // about the mean; below zero by rounding alone
+        const float m = v0.x + off, rs = 1.0f / sqrtf((around < 0.0f ? 0.0f : around) / total + p.eps);
+        fin[g] = make_float2(m, rs);
+        if (at.chunk == 0) {
+            if (p.mean) p.mean[b * p.G + at.g0 + g] = m;
+            if (p.rstd) p.rstd[b * p.G + at.g0 + g] = rs;
+        }
+    });
+    __syncthreads();
+    for (int col = at.tcol; col < at.nv; col += at.cstep) {
+        f32x2 m[P], rs[P], ga[P], be[P];
+        group_pairs<Ln>(fin, col * V, p.Cg, at.sub, m, rs);
+        Ln::table(ga_s + col * V, ga);
+        Ln::table(be_s + col * V, be);
+        const unsigned char* from = x + col * VB;
+        unsigned char* to = y + col * VB;
+        if (col != at.tcol) next.load(from, step, n);
+        for (int k = 0; k < n; k += kBatch) {
+            r = next;
+            from += kBatch * step;
+            next.load(from, step, n - k - kBatch);
+            const auto give = [&](int j) {
+                f32x2 v[P];
+                Ln::widen(r.raw[j], v);
+                forward_vector<Ln, ACT>(v, m, rs, ga, be);
+                Ln::store(to, v);
+                to += at.rows * yp;
+            };
+            if (n - k >= kBatch) {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) give(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    if (j < n - k) give(j);
+            }
+        }
+    }
+}
+
+template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads, kStreamCtas) k_back_sums(const NormParams p) {
+    using Ln = Lane<EB, VEC>;
+    constexpr int V = Ln::V, VB = Ln::VB, P = Ln::P;
+    extern __shared__ __align__(128) unsigned char smem[];
+    float4* stat = reinterpret_cast<float4*>(smem + p.stat_off);
+    float* ga_s = reinterpret_cast<float*>(smem + p.par_off);
+    float* be_s = ga_s + p.cb_max;
+    float2* norm = reinterpret_cast<float2*>(smem + p.grp_off);        // [GB] mean and rstd
+    float2* chan = norm + p.GB;                                        // [cb]
+    combo_step::pdl_release();
+    const Place<V> at(p, blockIdx.x);
+    const long long b = at.lot, xp = p.x_pitch * EB, dp = p.dy_pitch * EB;
+    const long long first = b * p.L + at.l0 + at.trow;
+    const unsigned char* x = p.x + first * xp + (long long)at.c0 * EB;
+    const unsigned char* dy = p.dy + first * dp + (long long)at.c0 * EB;
+    const int n = at.positions(at.trow);
+    Batch<EB, VEC, kPair> rx, rd, nx, nd;        // the next ones are under way while these are taken
+    if (at.tcol < at.nv) {
+        nx.load(x + at.tcol * VB, at.rows * xp, n);
+        nd.load(dy + at.tcol * VB, at.rows * dp, n);
+    }
+    for (int g = threadIdx.x; g < at.ng; g += kThreads) norm[g] = make_float2(p.mean[b * p.G + at.g0 + g], p.rstd[b * p.G + at.g0 + g]);
+    load_params(p, worker_of(p, b), at.c0, at.cb, ga_s, be_s);
+    __syncthreads();
+    for (int col = at.tcol; col < at.nv; col += at.cstep) {
+        f32x2 m[P], rs[P], ga[P], be[P], s1[P], s2[P];
+        group_pairs<Ln>(norm, col * V, p.Cg, at.sub, m, rs);
+        Ln::table(ga_s + col * V, ga);
+        Ln::table(be_s + col * V, be);
+#pragma unroll
+        for (int i = 0; i < P; ++i) s1[i] = s2[i] = 0;
+        const unsigned char *from = x + col * VB, *dfrom = dy + col * VB;
+        if (col != at.tcol) {
+            nx.load(from, at.rows * xp, n);
+            nd.load(dfrom, at.rows * dp, n);
+        }
+        for (int k = 0; k < n; k += kPair) {
+            rx = nx;
+            rd = nd;
+            from += kPair * at.rows * xp;
+            dfrom += kPair * at.rows * dp;
+            nx.load(from, at.rows * xp, n - k - kPair);
+            nd.load(dfrom, at.rows * dp, n - k - kPair);
+            const auto take = [&](int j) {
+                f32x2 v[P], d[P];
+                Ln::widen(rx.raw[j], v);
+                Ln::widen(rd.raw[j], d);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    f32x2 h, dz;
+                    back_pair<ACT>(v[i], d[i], m[i], rs[i], ga[i], be[i], h, dz);
+                    s1[i] = fma2(dz, h, s1[i]);
+                    s2[i] = add2(s2[i], dz);
+                }
+            };
+            if (n - k >= kPair) {
+#pragma unroll
+                for (int j = 0; j < kPair; ++j) take(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kPair; ++j)
+                    if (j < n - k) take(j);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            stat[(i * at.rows + at.trow) * at.nv + col] = make_float4(lo_of(s1[i]), hi_of(s1[i]), lo_of(s2[i]), hi_of(s2[i]));
+    }
+    __syncthreads();
+    const long long slot = b * p.chunks + at.chunk;
+    add_rows<Ln>(at, stat, [&](int c, float2 s) {
+        chan[c] = s;
+        p.chan[slot * p.C + at.c0 + c] = s;
+    });
+    __syncthreads();
+    add_groups(p, at, chan, ga_s, [&](int g, float t, float th) { p.part[slot * p.G + at.g0 + g] = make_float2(t, th); });
+}
+
+// dgamma and dbeta of 32 channels of a worker: what the CTAs left of its samples, added in a fixed order; the block.
+__device__ __forceinline__ void add_params(const NormParams& p, unsigned unit, float2 (*sh)[32]) {
+    const int blocks = (p.C + 31) / 32;
+    const int w = (int)(unit / blocks), lane = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int c = (int)(unit - (unsigned)w * blocks) * 32 + lane;
     const long long s0 = p.begin ? max((long long)p.begin[w], 0LL) : 0;
     const long long s1 = p.begin ? min((long long)p.begin[w + 1], p.B) : p.B;
     float2 s = make_float2(0.0f, 0.0f);
     if (c < p.C && s0 < s1) {
-        const long long k0 = s0 / p.ns, k1 = (s1 - 1) / p.ns;
-#pragma unroll 4
-        for (long long k = k0 + row; k <= k1; k += kSumRows) {
-            const float2 e = p.partial[max(k * p.ns, s0) * p.C + c];
+        // resident: a slot for each CTA's samples, the first one's; streamed: for each chunk
+        const bool lots = p.chunks == 1;
+        const long long k0 = lots ? s0 / p.ns : s0 * p.chunks, k1 = lots ? (s1 - 1) / p.ns : s1 * p.chunks - 1;
+#pragma unroll 8
+        for (long long k = k0 + row; k <= k1; k += kWarps) {
+            const float2 e = p.chan[(lots ? max(k * p.ns, s0) : k) * p.C + c];
             s.x += e.x;
             s.y += e.y;
         }
@@ -613,15 +862,94 @@ __global__ void __launch_bounds__(32 * kSumRows) k_norm_params(const NormParams 
     if (row == 0 && c < p.C) {
         s = sh[0][lane];
 #pragma unroll
-        for (int r = 1; r < kSumRows; ++r) { s.x += sh[r][lane].x; s.y += sh[r][lane].y; }
-        dgamma[w * pitch + c] = s.x;
-        dbeta[w * pitch + c] = s.y;
+        for (int r = 1; r < kWarps; ++r) { s.x += sh[r][lane].x; s.y += sh[r][lane].y; }
+        p.dgamma[w * p.grad_pitch + c] = s.x;
+        p.dbeta[w * p.grad_pitch + c] = s.y;
+    }
+}
+__global__ void __launch_bounds__(kThreads) k_norm_params(const NormParams p) {
+    __shared__ float2 sh[kWarps][32];
+    combo_step::pdl_wait();
+    add_params(p, blockIdx.x, sh);
+}
+
+template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads, kStreamCtas) k_back_apply(const NormParams p) {
+    using Ln = Lane<EB, VEC>;
+    constexpr int V = Ln::V, VB = Ln::VB, P = Ln::P;
+    extern __shared__ __align__(128) unsigned char smem[];
+    float* ga_s = reinterpret_cast<float*>(smem + p.par_off);
+    float* be_s = ga_s + p.cb_max;
+    float2* norm = reinterpret_cast<float2*>(smem + p.grp_off);        // [GB] mean and rstd
+    float2* fin = norm + p.GB;                                         // [GB] means of t and t * h
+    if (blockIdx.x < (unsigned)p.param_ctas) {       // the parameters' gradients need the same sums
+        combo_step::pdl_wait();
+        add_params(p, blockIdx.x, reinterpret_cast<float2(*)[32]>(smem + p.stat_off));
+        return;
+    }
+    float2* lots = reinterpret_cast<float2*>(smem + p.stat_off);
+    const Place<V> at(p, gridDim.x - 1 - blockIdx.x);
+    const long long b = at.lot, xp = p.x_pitch * EB, yp = p.y_pitch * EB, dp = p.dy_pitch * EB;
+    const long long first = b * p.L + at.l0 + at.trow;
+    const unsigned char* x = p.x + first * xp + (long long)at.c0 * EB;
+    const unsigned char* dy = p.dy + first * dp + (long long)at.c0 * EB;
+    unsigned char* dx = p.y + first * yp + (long long)at.c0 * EB;
+    const int n = at.positions(at.trow);
+    Batch<EB, VEC, kPair> rx, rd, nx, nd;        // the next ones are under way while these are taken
+    if (at.tcol < at.nv) {
+        nx.load(x + at.tcol * VB, at.rows * xp, n);
+        nd.load(dy + at.tcol * VB, at.rows * dp, n);
+    }
+    for (int g = threadIdx.x; g < at.ng; g += kThreads) norm[g] = make_float2(p.mean[b * p.G + at.g0 + g], p.rstd[b * p.G + at.g0 + g]);
+    load_params(p, worker_of(p, b), at.c0, at.cb, ga_s, be_s);
+    combo_step::pdl_wait();
+    const float inv = 1.0f / (float)((long long)p.L * p.Cg);
+    gather_chunks(p, at, lots, [](float2 v, float2, int, float2 acc) { return make_float2(acc.x + v.x, acc.y + v.y); },
+                  [&](int g, float2 s, float2) { fin[g] = make_float2(s.x * inv, s.y * inv); });
+    __syncthreads();
+    for (int col = at.tcol; col < at.nv; col += at.cstep) {
+        f32x2 m[P], rs[P], ga[P], be[P], m1[P], m2[P];
+        group_pairs<Ln>(norm, col * V, p.Cg, at.sub, m, rs);
+        group_pairs<Ln>(fin, col * V, p.Cg, at.sub, m1, m2);
+        Ln::table(ga_s + col * V, ga);
+        Ln::table(be_s + col * V, be);
+        const unsigned char *from = x + col * VB, *dfrom = dy + col * VB;
+        unsigned char* to = dx + col * VB;
+        if (col != at.tcol) {
+            nx.load(from, at.rows * xp, n);
+            nd.load(dfrom, at.rows * dp, n);
+        }
+        for (int k = 0; k < n; k += kPair) {
+            rx = nx;
+            rd = nd;
+            from += kPair * at.rows * xp;
+            dfrom += kPair * at.rows * dp;
+            nx.load(from, at.rows * xp, n - k - kPair);
+            nd.load(dfrom, at.rows * dp, n - k - kPair);
+            const auto give = [&](int j) {
+                f32x2 v[P], d[P];
+                Ln::widen(rx.raw[j], v);
+                Ln::widen(rd.raw[j], d);
+                back_vector<Ln, ACT>(v, d, m, rs, ga, be, m1, m2);
+                Ln::store(to, v);
+                to += at.rows * yp;
+            };
+            if (n - k >= kPair) {
+#pragma unroll
+                for (int j = 0; j < kPair; ++j) give(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kPair; ++j)
+                    if (j < n - k) give(j);
+            }
+        }
     }
 }
 
 // ---------------------------------------------------------------- host
-constexpr unsigned kSlabTarget = 50 * 1024;     // shared memory of a CTA's slab aimed at: four CTAs on an SM
-constexpr int kRowBytes = 128;                  // least bytes of a position that a block of groups takes
+constexpr int kRowBytes = 128;                  // resident: least bytes of a position that a block of groups takes,
+constexpr int kSlabBytes = 8 * 1024;            // and of a slab
+constexpr long long kChunk = 8 * 1024;   // streamed: least elements of a chunk
+constexpr long long kResidentBytes = 8ll << 20;
 constexpr int kMaxChannels = COMBO_NORM_MAX_CHANNELS;   // of a block of groups: bounds the tables in shared memory (40 bytes each)
 constexpr int kShortSample = 32;                // positions under which a CTA of the backward pass takes several samples
 
@@ -632,83 +960,110 @@ struct Plan {
 };
 
 int samples_per_cta(int L) { return L >= kShortSample ? 1 : (kShortSample + L - 1) / L; }
+// most chunks of a sample
+int chunks_of(int64_t L, int64_t C) {
+    const int64_t n = (L * C + kChunk - 1) / kChunk;
+    return (int)(n < L ? n : L);
+}
 
-combo_status plan_norm(NormParams& p, Plan& plan, int eb, bool vec, bool back, int sms, int smem_optin) {
+// Tables and blocks of groups for one way; false where its shared memory does not suffice.
+bool layout(NormParams& p, Plan& plan, int eb, bool vec, bool res, bool back, int smem_optin, int sms) {
     const int V = vec ? 16 / eb : 1, arrays = back ? 2 : 1;
-    // whole groups, at least kRowBytes of a position, whole vectors
+    // whole groups and whole vectors; resident: as few as fill kRowBytes and kSlabBytes; streamed: as many as there are threads for
     int GB = 1;
-    while (GB < p.G && (GB * p.Cg * eb < kRowBytes || GB * p.Cg % V != 0)) ++GB;
-    if (vec && (long long)GB * p.Cg > kMaxChannels) return plan_norm(p, plan, eb, false, back, sms, smem_optin);
+    if (res) {
+        while (GB < p.G && ((long long)GB * p.Cg * eb < kRowBytes || (long long)p.L * GB * p.Cg * eb < kSlabBytes || GB * p.Cg % V != 0)) ++GB;
+    } else {
+        for (int n = p.G; n > 1; --n)
+            if (n * p.Cg % V == 0 && n * p.Cg / V <= kThreads) { GB = n; break; }
+        while (GB < p.G && GB * p.Cg % V != 0) ++GB;
+    }
+    if (GB > 1 && GB * p.Cg > kMaxChannels) {
+        if (vec) return false;                   // groups that only together make whole vectors
+        GB = kMaxChannels / p.Cg;
+    }
     p.GB = GB;
     p.nblk = (p.G + GB - 1) / GB;
-    p.ns = back ? samples_per_cta(p.L) : 1;
-    const long long cb = (long long)GB * p.Cg;
+    const long long cb = (long long)GB * p.Cg, nv = cb / V;
     p.cb_max = (int)(cb + 3) / 4 * 4;
-    const long long chunks = (p.B + p.ns - 1) / p.ns, units = chunks * p.nblk;
-    const long long nv = cb / V, rows = nv < kThreads ? kThreads / nv : 1;
+    p.ns = res && back ? samples_per_cta(p.L) : 1;
+    p.chunks = 1;
+    if (!res) {                                  // as many as have all CTAs on the device at once, where that is enough of them
+        const long long slots = (long long)sms * kStreamCtas / (p.B * p.nblk), most = chunks_of(p.L, p.C);
+        p.chunks = (int)(slots < 1 ? 1 : slots < most ? slots : most);
+    }
+    p.Lc = (p.L + p.chunks - 1) / p.chunks;
+    p.chunks = (p.L + p.Lc - 1) / p.Lc;          // none of them empty
     p.sub = 1;
     while (p.sub < V && p.Cg % (2 * p.sub) == 0) p.sub *= 2;
     // forward: rows * cb / sub entries of 8 bytes, backward: 16 bytes for every pair of channels; the last block of
     // groups may be narrower and have more rows, but never more than kThreads vectors
     const long long vecs = nv > kThreads ? nv : kThreads;
-    const unsigned long long stat = (unsigned long long)vecs * (back ? (V > 1 ? V / 2 : 1) * 16 : V / p.sub * 8), grp = (3ull * GB + (back ? 2 * p.cb_max : 0)) * 8;
     const auto round = [](unsigned long long v) { return (v + 127) / 128 * 128; };
-    const unsigned long long par = 8ull * p.cb_max, fixed = round(stat) + round(par) + round(grp);
-    const unsigned long long room = (unsigned long long)smem_optin - fixed;
-    int CS = 1;
-    const auto slab = [&](int cs) { return round((unsigned long long)((p.L + cs - 1) / cs) * cb * eb); };
-    // small slabs let several CTAs share an SM (one loads while others store); and no SM is left idle
-    while (CS < kMaxCluster && (arrays * slab(CS) > kSlabTarget || (units * CS * 2 <= sms && p.L >= 2 * CS * rows))) CS *= 2;
-    plan.res = arrays * slab(CS) <= room;
-    p.CS = CS;
-    if (CS > 1) p.ns = 1;
-    p.Lc = (p.L + CS - 1) / CS;
+    const unsigned long long stat = round((unsigned long long)vecs * (back ? (V > 1 ? V / 2 : 1) * 16 : V / p.sub * 8));   // at least kThreads pairs, as gather_chunks wants
+    const unsigned long long par = round(8ull * p.cb_max), grp = round((2ull * GB + (back ? 2 * p.cb_max : 0)) * 8);
+    const unsigned long long slab = res ? round((unsigned long long)p.L * cb * eb) : 0;
     p.stat_off = 0;
-    p.par_off = (unsigned)round(stat);
-    p.grp_off = (unsigned)(round(stat) + round(par));
-    p.slab_off = (unsigned)fixed;
-    p.slab_bytes = (unsigned)(plan.res ? slab(CS) : 0);
+    p.par_off = (unsigned)stat;
+    p.grp_off = (unsigned)(stat + par);
+    p.slab_off = (unsigned)(stat + par + grp);
+    p.slab_bytes = (unsigned)slab;
+    if (slab > (1u << 20) || stat + par + grp + arrays * slab > (unsigned long long)smem_optin) return false;
     plan.vec = vec;
-    plan.smem = fixed + (plan.res ? arrays * slab(CS) : 0);
-    plan.grid = (p.B + p.ns - 1) / p.ns * p.nblk * CS;
+    plan.res = res;
+    plan.smem = stat + par + grp + arrays * slab;
+    plan.grid = (p.B + p.ns - 1) / p.ns * p.nblk * p.chunks;
+    return true;
+}
+
+// Resident where everything is small (one launch, no second read) or where a sample is too short to be worth a CTA's
+// tables twice; else streamed.
+combo_status choose(NormParams& p, Plan& plan, int eb, bool vec, bool back, int smem_optin, int sms) {
+    const int arrays = back ? 2 : 1;
+    const long long sample = (long long)p.L * p.C * eb * arrays;
+    const bool res = sample * p.B <= kResidentBytes || sample <= 32 * 1024;
+    for (int v = vec ? 1 : 0; v >= 0; --v) {
+        if (res && layout(p, plan, eb, v != 0, true, back, smem_optin, sms)) break;
+        if (layout(p, plan, eb, v != 0, false, back, smem_optin, sms)) break;
+        if (v == 0) return COMBO_ERR_INVALID_ARG;
+    }
     return plan.grid > 0x7fffffffLL ? COMBO_ERR_INVALID_ARG : COMBO_OK;
 }
 
-// `which`: a number of its own for every kernel
-cudaError_t launch_norm(void (*kern)(NormParams), int which, const NormParams& p, const Plan& plan, int smem_optin, cudaStream_t st) {
-    static uint64_t allowed[48];
-    cudaError_t e = combo_host::allow_smem(kern, smem_optin, &allowed[which]);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)plan.grid);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = plan.smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.CS;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = p.CS > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, p);
-}
-
 typedef void (*NormKernel)(NormParams);
-template <int EB, bool VEC, bool RES> NormKernel pick_act(bool back, int act) {
-    switch (act) {
-        case COMBO_ACT_RELU: return back ? k_norm_back<EB, VEC, RES, COMBO_ACT_RELU> : k_norm<EB, VEC, RES, COMBO_ACT_RELU>;
-        case COMBO_ACT_SILU: return back ? k_norm_back<EB, VEC, RES, COMBO_ACT_SILU> : k_norm<EB, VEC, RES, COMBO_ACT_SILU>;
-        default: return back ? k_norm_back<EB, VEC, RES, COMBO_ACT_NONE> : k_norm<EB, VEC, RES, COMBO_ACT_NONE>;
-    }
+// The kernels of one call: resident one, streamed two, and a number for each kernel of the library.
+struct Kernels {
+    NormKernel first, second;
+    int number;
+};
+template <int EB, bool VEC, int ACT> Kernels pick_way(bool back, bool res) {
+    if (res) return {back ? k_norm_back<EB, VEC, ACT> : k_norm<EB, VEC, ACT>, nullptr, 0};
+    return {back ? k_back_sums<EB, VEC, ACT> : k_norm_sums<EB, VEC>, back ? k_back_apply<EB, VEC, ACT> : k_norm_apply<EB, VEC, ACT>, 0};
 }
-template <int EB> NormKernel pick(bool back, bool vec, bool res, int act) {
-    if (vec) return res ? pick_act<EB, true, true>(back, act) : pick_act<EB, true, false>(back, act);
-    return res ? pick_act<EB, false, true>(back, act) : pick_act<EB, false, false>(back, act);
+template <int EB, bool VEC> Kernels pick_act(bool back, bool res, int act) {
+    return act == COMBO_ACT_RELU ? pick_way<EB, VEC, COMBO_ACT_RELU>(back, res)
+           : act == COMBO_ACT_SILU ? pick_way<EB, VEC, COMBO_ACT_SILU>(back, res) : pick_way<EB, VEC, COMBO_ACT_NONE>(back, res);
+}
+Kernels pick(int eb, bool back, const Plan& plan, int act) {
+    Kernels k = eb == 4 ? (plan.vec ? pick_act<4, true>(back, plan.res, act) : pick_act<4, false>(back, plan.res, act))
+                        : (plan.vec ? pick_act<2, true>(back, plan.res, act) : pick_act<2, false>(back, plan.res, act));
+    k.number = ((((eb == 4) * 2 + back) * 2 + plan.vec) * 2 + plan.res) * 3 + act;
+    return k;
 }
 
-int number_of(int eb, bool back, const Plan& plan, int act) {
-    return (((eb == 4 ? 1 : 0) * 2 + back) * 2 + plan.vec) * 2 * 3 + plan.res * 3 + act;
+cudaError_t launch(const NormParams& p, const Plan& plan, int eb, bool back, int act, int smem_optin, cudaStream_t st) {
+    static uint64_t allowed[2][48];
+    const Kernels k = pick(eb, back, plan, act);
+    cudaError_t e = combo_host::allow_smem(k.first, smem_optin, &allowed[0][k.number]);
+    if (e != cudaSuccess) return e;
+    k.first<<<(unsigned)plan.grid, kThreads, plan.smem, st>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess || !k.second) return e;
+    if ((e = combo_host::allow_smem(k.second, smem_optin, &allowed[1][k.number])) != cudaSuccess) return e;
+    return combo_host::launch_after(k.second, dim3((unsigned)plan.grid + p.param_ctas), dim3(kThreads), plan.smem, st, p);
 }
+
+// Scratch: sums per chunk and group, then (backward) per chunk and channel
+size_t part_bytes(int64_t B, int64_t L, int64_t C, int groups) { return ((size_t)B * chunks_of(L, C) * groups * 8 + 127) / 128 * 128; }
 
 // What forward and backward ask alike.
 combo_status check_shape(int elem_bytes, int param_bytes, const void* gamma, const void* beta, int64_t param_pitch,
@@ -737,23 +1092,28 @@ bool clash(const void* out, int64_t out_pitch, size_t out_n, const void* in, int
     return combo_host::overlap(out, out_n, in, in_n) && !(out == in && out_pitch == in_pitch);
 }
 
+bool scratch_ok(const void* scratch, size_t bytes, int64_t B, int64_t L, int64_t C, int groups) {
+    return scratch && combo_host::aligned_to(scratch, 16) && bytes >= combo_group_norm_scratch_bytes(B, L, C, groups);
+}
+
 }  // namespace
 
 extern "C" {
 
-size_t combo_group_norm_scratch_bytes(int64_t B, int64_t L, int64_t C) {
-    if (B < 0 || L < 1 || C < 1 || L > (1 << 28) || C > (1 << 20) || B > (1LL << 40) / L / C)
+size_t combo_group_norm_scratch_bytes(int64_t B, int64_t L, int64_t C, int groups) {
+    if (B < 0 || L < 1 || C < 1 || L > (1 << 28) || C > (1 << 20) || B > (1LL << 40) / L / C || groups < 1 || groups > C)
         return 0;
-    return (size_t)(B < 1 ? 1 : B) * (size_t)C * sizeof(float2);
+    const int64_t n = B < 1 ? 1 : B;
+    return part_bytes(n, L, C, groups) + (size_t)n * chunks_of(L, C) * C * sizeof(float2);
 }
 
 combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y_pitch, int elem_bytes, const void* gamma,
                               const void* beta, int param_bytes, int64_t param_pitch, const int64_t* d_begin, int N,
                               int64_t B, int64_t L, int64_t C, int groups, float eps, int act, float* mean_out,
-                              float* rstd_out, void* stream) {
+                              float* rstd_out, void* scratch, size_t scratch_bytes, void* stream) {
     combo_status rc = check_shape(elem_bytes, param_bytes, gamma, beta, param_pitch, d_begin, N, B, L, C, groups, act);
     if (rc != COMBO_OK) return rc;
-    if (!(eps >= 0.0f)) return COMBO_ERR_INVALID_ARG;
+    if (!(eps >= 0.0f) || !scratch_ok(scratch, scratch_bytes, B, L, C, groups)) return COMBO_ERR_INVALID_ARG;
     if (B == 0) return COMBO_OK;
     if (!array_ok(x, x_pitch, C, elem_bytes) || !array_ok(y, y_pitch, C, elem_bytes)) return COMBO_ERR_INVALID_ARG;
     if (!combo_host::aligned_to(mean_out, 4) || !combo_host::aligned_to(rstd_out, 4)) return COMBO_ERR_INVALID_ARG;
@@ -781,10 +1141,10 @@ combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y
     p.N = N;
     p.eps = eps;
     const bool vec = C * elem_bytes % 16 == 0 && vec_ok(x, x_pitch, elem_bytes) && vec_ok(y, y_pitch, elem_bytes);
+    p.part = static_cast<float2*>(scratch);
     Plan plan;
-    if ((rc = plan_norm(p, plan, elem_bytes, vec, false, sms, smem)) != COMBO_OK) return rc;
-    auto kern = elem_bytes == 4 ? pick<4>(false, plan.vec, plan.res, act) : pick<2>(false, plan.vec, plan.res, act);
-    cudaError_t e = launch_norm(kern, number_of(elem_bytes, false, plan, act), p, plan, smem, static_cast<cudaStream_t>(stream));
+    if ((rc = choose(p, plan, elem_bytes, vec, false, smem, sms)) != COMBO_OK) return rc;
+    cudaError_t e = launch(p, plan, elem_bytes, false, act, smem, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "group norm launch");
 }
 
@@ -798,12 +1158,18 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
     if (rc != COMBO_OK) return rc;
     if ((dgamma == nullptr) != (dbeta == nullptr) || (dgamma && N > 1 && grad_pitch < C)) return COMBO_ERR_INVALID_ARG;
     if (!combo_host::aligned_to(dgamma, 4) || !combo_host::aligned_to(dbeta, 4)) return COMBO_ERR_INVALID_ARG;
-    if (!scratch || !combo_host::aligned_to(scratch, 8) || scratch_bytes < combo_group_norm_scratch_bytes(B, L, C))
-        return COMBO_ERR_INVALID_ARG;
+    if (!scratch_ok(scratch, scratch_bytes, B, L, C, groups)) return COMBO_ERR_INVALID_ARG;
     int sms = 0, smem = 0;
     NormParams p = {};
     p.begin = d_begin;
-    p.partial = static_cast<float2*>(scratch);
+    p.part = static_cast<float2*>(scratch);
+    p.chan = reinterpret_cast<float2*>(static_cast<unsigned char*>(scratch) + part_bytes(B < 1 ? 1 : B, L, C, groups));
+    p.chunks = 1;
+    p.dgamma = dgamma;
+    p.dbeta = dbeta;
+    p.grad_pitch = N > 1 ? grad_pitch : 0;
+    p.param_ctas = dgamma ? (int)((C + 31) / 32 * N) : 0;
+    Plan plan = {};
     p.B = B;
     p.C = (int)C;
     p.N = N;
@@ -839,14 +1205,11 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
         p.Cg = (int)(C / groups);
         const bool vec = C * elem_bytes % 16 == 0 && vec_ok(x, x_pitch, elem_bytes) && vec_ok(dx, dx_pitch, elem_bytes) &&
                          vec_ok(dy, dy_pitch, elem_bytes);
-        Plan plan;
-        if ((rc = plan_norm(p, plan, elem_bytes, vec, true, sms, smem)) != COMBO_OK) return rc;
-        auto kern = elem_bytes == 4 ? pick<4>(true, plan.vec, plan.res, act) : pick<2>(true, plan.vec, plan.res, act);
-        if ((e = launch_norm(kern, number_of(elem_bytes, true, plan, act), p, plan, smem, st)) != cudaSuccess) return combo_host::fail(e, "group norm backward launch");
+        if ((rc = choose(p, plan, elem_bytes, vec, true, smem, sms)) != COMBO_OK) return rc;
+        if ((e = launch(p, plan, elem_bytes, true, act, smem, st)) != cudaSuccess) return combo_host::fail(e, "group norm backward launch");
     }
-    if (dgamma) {
-        const dim3 grid((unsigned)((C + 31) / 32), (unsigned)N);
-        e = combo_host::launch_after(k_norm_params, grid, dim3(32 * kSumRows), 0, st, p, dgamma, dbeta, (long long)(N > 1 ? grad_pitch : 0));
+    if (p.param_ctas > 0 && (B == 0 || plan.res)) {
+        e = combo_host::launch_after(k_norm_params, dim3((unsigned)p.param_ctas), dim3(kThreads), 0, st, p);
         if (e != cudaSuccess) return combo_host::fail(e, "group norm parameter gradient launch");
     }
     return COMBO_OK;

@@ -57,9 +57,14 @@ class Case:
             self.B, self.L, self.C + self.wide)[:, :, :self.C] = False
         return bool((self.buf[m] == 3.0).all())
 
+    def scratch(self):
+        n = combo.combo_group_norm_scratch_bytes(self.B, self.L, self.C, self.G)
+        return torch.full((n // 4,), float("nan"), device=DEV)
+
     def forward(self, act, y=None):
         y = self.blank() if y is None else y
-        combo.combo_group_norm(self.x, y, self.gamma, self.beta, self.begin, self.G, EPS, act, self.mean, self.rstd)
+        combo.combo_group_norm(self.x, y, self.gamma, self.beta, self.begin, self.G, EPS, act, self.mean, self.rstd,
+                               self.scratch())
         torch.cuda.synchronize()
         return y
 
@@ -67,10 +72,8 @@ class Case:
         dx = self.blank() if dx is None else dx
         out = torch.full((self.N, 2 * self.C + 5), 3.0, device=DEV)
         dg, db = (out[:, 1:self.C + 1], out[:, self.C + 3:2 * self.C + 3]) if params else (None, None)
-        scratch = torch.full((combo.combo_group_norm_scratch_bytes(self.B, self.L, self.C, self.G) // 4,), float("nan"),
-                             device=DEV)
         combo.combo_group_norm_backward(self.dy, self.x, dx, self.gamma, self.beta, self.begin, self.G, act, self.mean,
-                                        self.rstd, dg, db, scratch)
+                                        self.rstd, dg, db, self.scratch())
         torch.cuda.synchronize()
         if params:
             out[:, 1:self.C + 1], kept = -1.0, out[:, 1:self.C + 1].clone()
@@ -191,17 +194,20 @@ SHAPES = [
     ([0, 3, 0, 2, 0], 33, 64, 32, 0, 0),           # 2 channels a group: a 16-byte vector spans groups
     ([2, 1], 100, 128, 32, 8, 8),
     ([1, 1], 784, 96, 3, 0, 0),
-    ([1], 3136, 256, 32, 0, 0),                    # a cluster shares a slab
+    ([1], 3136, 256, 32, 0, 0),                    # a long sample
     ([1, 1], 3137, 40, 4, 0, 0),                   # the same, ragged
     ([1], 997, 3, 3, 0, 0),                        # one channel a group, odd
     ([2], 7, 77, 7, 5, 3),
-    ([1], 20_001, 64, 1, 0, 0),                    # more than a cluster holds in 32 bits: read again
+    ([1], 20_001, 64, 1, 0, 0),                    # too long for shared memory: streamed
     ([1], 9_001, 61, 1, 0, 0),
     ([2, 1], 3, 4096, 1, 0, 0),                    # more vectors than threads
     ([1], 2, 2600, 2, 1, 0),
     ([5, 0, 30, 2, 1, 12], 1, 48, 4, 0, 0),        # short samples: several to a CTA, workers changing inside
     ([1] * 40 + [0] * 5 + [7], 4, 16, 2, 0, 0),
     ([1] * 300, 2, 8, 1, 0, 0),
+    ([3, 0, 2], 1500, 512, 32, 0, 0),              # streamed for its size, chunks of unequal length
+    ([2, 1], 1300, 1026, 18, 2, 0),                # the same, 57 channels a group, no whole vectors
+    ([2], 700, 2304, 9, 8, 8),                     # more vectors than threads in a block
 ]
 
 
@@ -225,7 +231,7 @@ def test_no_parameters_and_one_worker_without_a_table(dtype):
     # statistics and parameter gradients not wanted
     y = c.forward(combo.ACT_RELU).clone()
     c2 = c.blank()
-    combo.combo_group_norm(c.x, c2, None, None, None, 4, EPS, combo.ACT_RELU)
+    combo.combo_group_norm(c.x, c2, None, None, None, 4, EPS, combo.ACT_RELU, None, None, c.scratch())
     assert torch.equal(y, c2)
     dx = c.backward(combo.ACT_RELU)[0].clone()
     assert torch.equal(dx, c.backward(combo.ACT_RELU, params=False))
@@ -329,7 +335,8 @@ def test_many_positions_in_one_worker_at_large_offsets():
     x = torch.zeros(40, L, C, dtype=torch.bfloat16, device=DEV)
     x[39, :, 1::2] = 2.0
     mean, rstd = torch.empty(40, 8, device=DEV), torch.empty(40, 8, device=DEV)
-    combo.combo_group_norm(x, x, None, None, None, 8, 0.0 + EPS, combo.ACT_NONE, mean, rstd)
+    scratch = torch.empty(combo.combo_group_norm_scratch_bytes(40, L, C, 8), dtype=torch.uint8, device=DEV)
+    combo.combo_group_norm(x, x, None, None, None, 8, EPS, combo.ACT_NONE, mean, rstd, scratch)
     assert (mean[:39] == 0).all() and (mean[39] - 1.0).abs().max() <= 1e-6
     assert (x[:39] == 0).all()
     assert (x[39, :, 1::2] == 1.0).all() and (x[39, :, ::2] == -1.0).all()
@@ -340,7 +347,8 @@ def test_refusals():
     y = c.blank()
 
     def refused(status=1, **kw):
-        args = dict(x=c.x, y=y, gamma=c.gamma, beta=c.beta, begin=c.begin, groups=3, eps=EPS, act=0, mean=c.mean, rstd=c.rstd)
+        args = dict(x=c.x, y=y, gamma=c.gamma, beta=c.beta, begin=c.begin, groups=3, eps=EPS, act=0, mean=c.mean, rstd=c.rstd,
+                    scratch=c.scratch())
         args.update(kw)
         with pytest.raises(combo.ComboError) as e:
             combo.combo_group_norm(**args)
@@ -355,11 +363,11 @@ def test_refusals():
     shifted = torch.zeros(3 * 10 * 24 + 24, device=DEV)
     refused(status=2, x=shifted[:720].view(3, 10, 24), y=shifted[24:].view(3, 10, 24))
     with pytest.raises(ValueError):
-        combo.combo_group_norm(c.x.transpose(1, 2), y, c.gamma, c.beta, c.begin, 3, EPS, 0)
+        combo.combo_group_norm(c.x.transpose(1, 2), y, c.gamma, c.beta, c.begin, 3, EPS, 0, None, None, c.scratch())
     with pytest.raises(ValueError):
-        combo.combo_group_norm(c.x, y, c.gamma.double(), c.beta.double(), c.begin, 3, EPS, 0)
+        combo.combo_group_norm(c.x, y, c.gamma.double(), c.beta.double(), c.begin, 3, EPS, 0, None, None, c.scratch())
     with pytest.raises(ValueError):
-        combo.combo_group_norm(c.x, y, c.gamma, c.beta, c.begin[:-1], 3, EPS, 0)
+        combo.combo_group_norm(c.x, y, c.gamma, c.beta, c.begin[:-1], 3, EPS, 0, None, None, c.scratch())
     c.forward(0)
     s = torch.empty(combo.combo_group_norm_scratch_bytes(3, 10, 24, 3) - 8, dtype=torch.uint8, device=DEV)
     with pytest.raises(combo.ComboError):
@@ -370,3 +378,5 @@ def test_refusals():
     with pytest.raises(combo.ComboError):
         wide.forward(0)
     assert combo.combo_group_norm_scratch_bytes(1, 0, 4, 1) == 0
+    refused(scratch=None)
+    refused(scratch=s)
