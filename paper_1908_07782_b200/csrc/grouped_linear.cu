@@ -45,39 +45,35 @@ __device__ __forceinline__ void rows_of(const Product& p, int w, long long& r0, 
 }
 
 // ---------------------------------------------------------------- binary32 multiply-adds
-// 128 x 128 outputs for a block of 256 threads, 8 x 8 each, 16 values of r at a time through two shared-memory stages;
-// the next stage's loads are in registers while this one's products are formed.  Takes every type, pitch and alignment.
+// float operands: 128 x 128 outputs for a block of 256 threads, 8 x 8 each, 16 values of r at a time through two shared-
+// memory stages; the next stage's loads are in registers while this one's products are formed.  Any pitch and alignment.
 constexpr int kFT = 128, kFK = 16, kFThreads = 256;
 constexpr int kFPad = 4;
 
 // Eight neighbouring elements of one line; those at or beyond `left` are zero.
-template <int EB> __device__ __forceinline__ void load8(const unsigned char* q, int left, bool vec, float (&v)[8]) {
+__device__ __forceinline__ void load8(const unsigned char* q, int left, bool vec, float (&v)[8]) {
     if (vec && left >= 8) {
-        if constexpr (EB == 4) {
-            const uint4 a = *reinterpret_cast<const uint4*>(q), b = *reinterpret_cast<const uint4*>(q + 16);
-            float x[4], y[4];
-            Elem<4>::unpack(a, x);
-            Elem<4>::unpack(b, y);
+        const uint4 a = *reinterpret_cast<const uint4*>(q), b = *reinterpret_cast<const uint4*>(q + 16);
+        float x[4], y[4];
+        Elem<4>::unpack(a, x);
+        Elem<4>::unpack(b, y);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = x[i]; v[4 + i] = y[i]; }
-        } else {
-            Elem<2>::unpack(*reinterpret_cast<const uint4*>(q), v);
-        }
+        for (int i = 0; i < 4; ++i) { v[i] = x[i]; v[4 + i] = y[i]; }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<EB>::get(q + i * EB) : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<4>::get(q + i * 4) : 0.0f;
     }
 }
 
 // A thread's share of a 128 x 16 operand tile.  ALONG_R: r is contiguous; else the tile index is.
-template <int EB, bool ALONG_R>
+template <bool ALONG_R>
 __device__ __forceinline__ void load_part(const unsigned char* base, long long pitch, long long i0, long long i_end, long long r0,
                                           long long r_end, bool vec, float (&v)[8]) {
     const int t = threadIdx.x;
     const long long i = i0 + (ALONG_R ? t >> 1 : (t & 15) * 8), r = r0 + (ALONG_R ? (t & 1) * 8 : t >> 4);
     const long long left = ALONG_R ? (i < i_end ? r_end - r : 0) : (r < r_end ? i_end - i : 0);
     const int n = (int)min(max(left, 0LL), 8LL);
-    load8<EB>(base + (ALONG_R ? i * pitch + r : r * pitch + i) * EB, n, vec, v);
+    load8(base + (ALONG_R ? i * pitch + r : r * pitch + i) * 4, n, vec, v);
 }
 
 template <bool ALONG_R> __device__ __forceinline__ void store_part(float (*s)[kFT + kFPad], const float (&v)[8]) {
@@ -92,7 +88,7 @@ template <bool ALONG_R> __device__ __forceinline__ void store_part(float (*s)[kF
     }
 }
 
-template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const Product p) {
+template <int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const Product p) {
     constexpr bool A_R = MODE != kGradWeight, B_R = MODE == kForward;
     __shared__ __align__(16) float sa[2][kFK][kFT + kFPad];
     __shared__ __align__(16) float sb[2][kFK][kFT + kFPad];
@@ -126,7 +122,7 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
         i0 += ((long long)blockIdx.y - before) * kFT;
     }
     const unsigned char* a = p.a;
-    const unsigned char* b = MODE == kGradWeight ? p.b : p.b + w * p.stride * EB;
+    const unsigned char* b = MODE == kGradWeight ? p.b : p.b + w * p.stride * 4;
     f32x2 acc[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -136,8 +132,8 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
     float va[8], vb[8];
     int s = 0;
     if (r0 < r1) {
-        load_part<EB, A_R>(a, p.a_pitch, i0, i1, r0, r1, p.a_vec, va);
-        load_part<EB, B_R>(b, p.b_pitch, j0, p.J, r0, r1, p.b_vec, vb);
+        load_part<A_R>(a, p.a_pitch, i0, i1, r0, r1, p.a_vec, va);
+        load_part<B_R>(b, p.b_pitch, j0, p.J, r0, r1, p.b_vec, vb);
         store_part<A_R>(sa[0], va);
         store_part<B_R>(sb[0], vb);
     }
@@ -145,8 +141,8 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
     for (long long r = r0; r < r1; r += kFK) {
         const bool more = r + kFK < r1;
         if (more) {
-            load_part<EB, A_R>(a, p.a_pitch, i0, i1, r + kFK, r1, p.a_vec, va);
-            load_part<EB, B_R>(b, p.b_pitch, j0, p.J, r + kFK, r1, p.b_vec, vb);
+            load_part<A_R>(a, p.a_pitch, i0, i1, r + kFK, r1, p.a_vec, va);
+            load_part<B_R>(b, p.b_pitch, j0, p.J, r + kFK, r1, p.b_vec, vb);
         }
 #pragma unroll
         for (int k = 0; k < kFK; ++k) {
@@ -170,7 +166,7 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
         __syncthreads();
         s ^= 1;
     }
-    unsigned char* c = MODE == kGradWeight ? p.c + w * p.stride * OB : p.c;
+    unsigned char* c = MODE == kGradWeight ? p.c + w * p.stride * 4 : p.c;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const long long row = i0 + (i >> 2) * 64 + ti * 4 + (i & 3);
@@ -178,22 +174,21 @@ template <int EB, int OB, int MODE> __global__ void __launch_bounds__(kFThreads,
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long long col = j0 + h * 64 + tj * 4;
-            unsigned char* q = c + (row * p.c_pitch + col) * OB;
+            unsigned char* q = c + (row * p.c_pitch + col) * 4;
             const float v[4] = {lo_of(acc[i][2 * h]), hi_of(acc[i][2 * h]), lo_of(acc[i][2 * h + 1]), hi_of(acc[i][2 * h + 1])};
             if (p.c_vec && col + 4 <= p.J) {
-                if constexpr (OB == 4) *reinterpret_cast<float4*>(q) = make_float4(v[0], v[1], v[2], v[3]);
-                else *reinterpret_cast<uint2*>(q) = make_uint2(combo_step::pack_bf16(v[0], v[1]), combo_step::pack_bf16(v[2], v[3]));
+                *reinterpret_cast<float4*>(q) = make_float4(v[0], v[1], v[2], v[3]);
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (col + k < p.J) Elem<OB>::put(q + k * OB, v[k]);
+                    if (col + k < p.J) Elem<4>::put(q + k * 4, v[k]);
             }
         }
     }
 }
 
 // ---------------------------------------------------------------- tensor cores
-// bfloat16 operands on 16-byte boundaries.  The weights' index is the height of the product (128 CG outputs), the
+// bfloat16 operands.  The weights' index is the height of the product (128 CG outputs), the
 // ragged rows its width: a worker's rows are cut evenly into tiles of at most p.width, and the width of a product can
 // be any multiple of 16 CG, so that ragged rows cost at most 16 CG - 1 idle columns a worker, not half a tile.
 //
@@ -217,7 +212,8 @@ __device__ __forceinline__ bool give_up(int site) {
 
 constexpr int kOutWarps = 4;                 // one for each quarter of TMEM's lanes (eight were no faster)
 constexpr int kFirstOutWarp = 4;
-constexpr int kTcThreads = 32 * (kFirstOutWarp + kOutWarps);
+constexpr int kLoadWarps = 8;                // where threads load: warps behind those
+constexpr int tc_threads(bool by_threads) { return 32 * (kFirstOutWarp + kOutWarps + (by_threads ? kLoadWarps : 0)); }
 constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kOperandA = 128 * kStep * 2;   // bytes of the height's operand in a stage
 constexpr int kRowBoxes = 4;                 // boxes of 32, 64, 128 or 256 rows of X or dY
@@ -316,8 +312,72 @@ __device__ __forceinline__ void zero_tail(uint32_t at, int blocks, int left, int
     __syncwarp();
 }
 
-template <int CG, int MODE, int OB>
-__global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __grid_constant__ TcMaps maps) {
+// Loads by threads, for operands that TMA cannot take (bases, pitches or strides that are no multiples of 16 bytes).  A
+// warp brings lines of 64 values, a 32-bit word a lane; where a line begins in the middle of a word, each lane joins
+// halves of its own and its neighbour's.  (A word that the line's first or last value shares is read whole: 2 bytes of
+// the same aligned word.)  Lines and values that are not the operand's are zero, so nothing is left to be zeroed after.
+// All lines of a lot of three blocks are under way together: 24 KB of an SM's eight warps.
+template <int MODE>
+__device__ __forceinline__ void load_stage(const Product& p, const Tile& x, int k, uint32_t stage, int wl, int lane) {
+    constexpr bool A_R = MODE == kForward, B_R = MODE != kGradWeight;
+    const int blocks = 2 + (x.n + 63) / 64;
+    const unsigned char* wa = MODE == kGradWeight ? p.a : p.b + x.w * p.stride * 2;
+    const unsigned char* wb = MODE == kGradWeight ? p.b : p.a;
+    const long long pa = MODE == kGradWeight ? p.a_pitch : p.b_pitch, pb = MODE == kGradWeight ? p.b_pitch : p.a_pitch;
+    // r: first value of the stage and the end; an operand along r has its lines along its own index
+    const long long r0 = MODE == kGradWeight ? x.row0 + (long long)k * kStep : (long long)k * kStep;
+    const long long r_end = MODE == kGradWeight ? x.row1 : p.R;
+    for (int g0 = 0; g0 < blocks; g0 += 3) {
+        uint32_t w[24], last[24], odd = 0;
+        int valid[3], lines[3];
+#pragma unroll
+        for (int gi = 0; gi < 3; ++gi) {
+            const int g = g0 + gi;
+            const bool height = g < 2;
+            const int block = height ? g : g - 2;
+            const bool along_r = height ? A_R : B_R;
+            const long long index0 = height ? x.i0 : MODE == kGradWeight ? x.j0 : x.row0;        // of the operand's own index
+            const long long index_end = height ? p.I : MODE == kGradWeight ? p.J : x.row1;
+            const long long line0 = along_r ? index0 + block * 64 + wl : r0 + wl, line_end = along_r ? index_end : r_end;
+            const long long col0 = along_r ? r0 : index0 + block * 64, col_end = along_r ? r_end : index_end;
+            valid[gi] = g < blocks ? (int)min(max(col_end - col0, 0LL), 64LL) : 0;
+            lines[gi] = (int)min(max((line_end - line0 + 7) / 8, 0LL), 8LL);
+            const long long pitch = (height ? pa : pb) * 2;
+            const unsigned char* q = (height ? wa : wb) + line0 * pitch + col0 * 2;
+#pragma unroll
+            for (int u = 0; u < 8; ++u, q += 8 * pitch) {
+                const int e = gi * 8 + u;
+                const bool half = (reinterpret_cast<uintptr_t>(q) & 2u) != 0, on = u < lines[gi];
+                const uint32_t* word = reinterpret_cast<const uint32_t*>(q - (half ? 2 : 0)) + lane;
+                w[e] = on && 2 * lane - (half ? 1 : 0) < valid[gi] && valid[gi] > 0 ? __ldg(word) : 0u;
+                last[e] = on && half && lane == 31 && valid[gi] == 64 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(q + 126)) : 0u;
+                if (half) odd |= 1u << e;
+            }
+        }
+#pragma unroll
+        for (int gi = 0; gi < 3; ++gi) {
+            const int g = g0 + gi;
+            if (g >= blocks) break;
+            const uint32_t to = stage + (g < 2 ? g * 64 * kStep * 2 : kOperandA + (g - 2) * 64 * kStep * 2) + wl * 128 + ((lane * 4) ^ (wl << 4));
+            const uint32_t keep = (2 * lane < valid[gi] ? 0xffffu : 0u) | (2 * lane + 1 < valid[gi] ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int e = gi * 8 + u;
+                uint32_t next = __shfl_down_sync(0xffffffffu, w[e], 1);
+                if (lane == 31) next = last[e];
+                const uint32_t v = (odd >> e & 1u ? __funnelshift_r(w[e], next, 16) : w[e]) & (u < lines[gi] ? keep : 0u);
+                // the width's operand along r has x.n lines
+                if (g < 2 || !B_R || (g - 2) * 64 + wl + u * 8 < x.n)
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + u * 1024), "r"(v) : "memory");
+            }
+        }
+    }
+    fence_async();
+    __syncwarp();
+}
+
+template <int CG, int MODE, int OB, bool THREADS>
+__global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q, const __grid_constant__ TcMaps maps) {
     constexpr bool A_R = MODE == kForward, B_R = MODE != kGradWeight;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 7];
@@ -336,7 +396,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
     const uint32_t tail_at = smem + q.stages * q.stage_bytes;
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.stages; ++s) {
-            mbar_init(full(s), 2);           // one arrival for either operand, and the bytes of all CTAs
+            // one arrival for either operand, and the bytes of all CTAs; or one for each warp that loads
+            mbar_init(full(s), THREADS ? kLoadWarps : 2);
             mbar_init(empty(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -348,7 +409,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
         mbar_init(tail_empty, 1);
         mbar_init_fence();
         dead = 0;
-        prefetch_map(&maps.a);
+        if (!THREADS) prefetch_map(&maps.a);
     }
     if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_at), kTmemColumns);
     tc_fence_before();
@@ -363,7 +424,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
     const int first = (int)blockIdx.x / CG, stride = (int)gridDim.x / CG;
     Tile x;
 
-    if (warp == 0 || warp == 2) {
+    if (THREADS && warp >= kFirstOutWarp + kOutWarps) {
+        // ------------------------------------------------------------ loads by threads
+        Tiles<CG, MODE> tiles(q, first);
+        uint32_t s = 0, ph = 0;
+        bool ok = true;
+        while (ok && tiles.next(x, stride)) {
+            for (int k = 0; k < x.steps && ok; ++k) {
+                ok = mbar_wait(empty(s), ph ^ 1u, dead_v) || give_up(49);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                load_stage<MODE>(q.p, x, k, smem + s * q.stage_bytes, warp - kFirstOutWarp - kOutWarps, lane);
+                if (elect()) mbar_arrive(full(s));
+                __syncwarp();
+                if (++s == (uint32_t)q.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+        if (!ok) *dead_v = 1;
+    } else if (!THREADS && (warp == 0 || warp == 2)) {
         // ------------------------------------------------------------ loads: warp 0 the height's operand, warp 2 the width's
         const int operand = warp == 0 ? 0 : 1;
         Tiles<CG, MODE> tiles(q, first);
@@ -445,7 +523,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
                 if (x.steps == 0) continue;
                 const uint32_t buf = accs & 1u;
                 const int rest = MODE == kGradWeight ? (int)((x.row1 - x.row0) % kStep) : 0;
-                const int plain = rest % 16 != 0 ? x.steps - 1 : x.steps;
+                const int plain = !THREADS && rest % 16 != 0 ? x.steps - 1 : x.steps;
                 if (elect()) {
                     const uint32_t d = tmem + buf * 256, kind = product_kind(128 * CG, x.n, A_R, B_R);
                     uint32_t s = done % q.stages, ph = done / q.stages & 1u;
@@ -461,7 +539,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
                     for (int k = 0; k < plain && ok; ++k) {
                         if (!mbar_wait(full(s), ph, dead_v)) { ok = give_up(45); break; }
                         tc_fence_after();
-                        issue(smem + s * q.stage_bytes, k + 1 == x.steps && rest ? rest / 16 : kStep / 16, k > 0);
+                        issue(smem + s * q.stage_bytes, k + 1 == x.steps && rest ? (rest + 15) / 16 : kStep / 16, k > 0);
                         mma_commit<CG>(empty(s));
                         if (++s == q.stages) { s = 0; ph ^= 1u; }
                     }
@@ -487,7 +565,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
         }
     } else if (warp == 3) {
         // ------------------------------------------------------------ rows of others, zeroed
-        if (MODE == kGradWeight) {
+        if (MODE == kGradWeight && !THREADS) {
             Tiles<CG, MODE> tiles(q, first);
             uint32_t tails = 0;
             bool ok = true;
@@ -506,11 +584,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
             }
             if (!ok) *dead_v = 1;
         }
-    } else if (warp >= kFirstOutWarp) {
+    } else if (warp >= kFirstOutWarp && warp < kFirstOutWarp + kOutWarps) {
         // ------------------------------------------------------------ results
         Tiles<CG, MODE> tiles(q, first);
         const int quarter = warp & 3;        // a warp reads the 32 lanes of TMEM that its number allows
-        float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + (q.stages + (MODE == kGradWeight ? 1 : 0)) * q.stage_bytes + quarter * kTurn);
+        float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + (q.stages + (MODE == kGradWeight && !THREADS ? 1 : 0)) * q.stage_bytes + quarter * kTurn);
         uint32_t accs = 0;
         bool ok = true;
         while (tiles.next(x, stride)) {
@@ -585,17 +663,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_tc(const TcParams q, const __
 }
 
 // ---------------------------------------------------------------- host
-template <int EB, int OB> cudaError_t launch_fma(const Product& p, int mode, cudaStream_t st) {
+cudaError_t launch_fma(const Product& p, int mode, cudaStream_t st) {
     const unsigned cols = (unsigned)((p.J + kFT - 1) / kFT);
     if (mode == kGradWeight) {
         const dim3 grid(cols, (unsigned)((p.I + kFT - 1) / kFT), (unsigned)p.N);
-        k_fma<EB, OB, kGradWeight><<<grid, kFThreads, 0, st>>>(p);
+        k_fma<kGradWeight><<<grid, kFThreads, 0, st>>>(p);
     } else {
         // every worker adds less than one tile to those its rows fill
         const long long tiles = p.M / kFT + (p.N < p.M ? p.N : p.M);
         const dim3 grid(cols, (unsigned)(tiles < 1 ? 1 : tiles));
-        if (mode == kForward) k_fma<EB, OB, kForward><<<grid, kFThreads, 0, st>>>(p);
-        else k_fma<EB, OB, kGradInput><<<grid, kFThreads, 0, st>>>(p);
+        if (mode == kForward) k_fma<kForward><<<grid, kFThreads, 0, st>>>(p);
+        else k_fma<kGradInput><<<grid, kFThreads, 0, st>>>(p);
     }
     return cudaGetLastError();
 }
@@ -620,15 +698,15 @@ bool encode(CUtensorMap* map, const void* base, long long width, long long rows,
                                     CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int CG, int MODE, int OB> cudaError_t launch_tc_inst(const TcParams& q, const TcMaps& maps, int smem_most, int grid, cudaStream_t st) {
+template <int CG, int MODE, int OB, bool THREADS> cudaError_t launch_tc_inst(const TcParams& q, const TcMaps& maps, int smem_most, int grid, cudaStream_t st) {
     static uint64_t allowed;
-    auto kern = k_tc<CG, MODE, OB>;
-    const size_t smem = 1024 + (size_t)(q.stages + (MODE == kGradWeight ? 1 : 0)) * q.stage_bytes + kOutWarps * kTurn;
+    auto kern = k_tc<CG, MODE, OB, THREADS>;
+    const size_t smem = 1024 + (size_t)(q.stages + (MODE == kGradWeight && !THREADS ? 1 : 0)) * q.stage_bytes + kOutWarps * kTurn;
     cudaError_t e = combo_host::allow_smem(kern, smem_most, &allowed);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(kTcThreads);
+    cfg.blockDim = dim3(tc_threads(THREADS));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -640,7 +718,7 @@ template <int CG, int MODE, int OB> cudaError_t launch_tc_inst(const TcParams& q
     return cudaLaunchKernelEx(&cfg, kern, q, maps);
 }
 
-template <int CG> combo_status launch_tc(const Product& p, int mode, int out_bytes, int sms, int smem_optin, cudaStream_t st) {
+template <int CG, bool THREADS> combo_status launch_tc(const Product& p, int mode, int out_bytes, int sms, int smem_optin, cudaStream_t st) {
     TcParams q = {p, 256, 0, 0, 0, 0};
     // the height is W's (forward: n_out, rows' gradient: n_in) or n_out; see the table above
     const long long mt = (p.I + 128 * CG - 1) / (128 * CG);
@@ -660,17 +738,18 @@ template <int CG> combo_status launch_tc(const Product& p, int mode, int out_byt
     const int half = q.width / CG;
     q.stage_bytes = kOperandA + half * kStep * 2;
     q.stages = (smem_optin - kStaticSmem - 1024 - kOutWarps * kTurn) / q.stage_bytes;
-    if (mode == kGradWeight) --q.stages;         // one behind the ring
+    if (mode == kGradWeight && !THREADS) --q.stages;     // one behind the ring
     if (q.stages > kMaxStages) q.stages = kMaxStages;
     int grid = sms / CG * CG;
     if (tiles * CG < grid) grid = (int)tiles * CG;
     if (grid < CG) grid = CG;
     TcMaps maps;
     memset(&maps, 0, sizeof(maps));
-    bool fine = true;
+    bool fine = true;                            // threads load by the addresses alone
     // p.a: the rows' operand of the first kind (X, dY, dY), p.b: W, W, X.  An operand along i or j comes in blocks of 64: in
     // one copy where its width is a multiple of that, else (a block would run into the next row) in one copy a block
-    if (mode == kForward) {
+    if (THREADS) {
+    } else if (mode == kForward) {
         fine = encode(&maps.a, p.b, p.R, p.I, p.b_pitch, p.N, p.stride, 128, 0);
     } else if (mode == kGradInput) {
         q.a_blocks = p.I % kStep == 0;
@@ -681,14 +760,14 @@ template <int CG> combo_status launch_tc(const Product& p, int mode, int out_byt
         fine = encode(&maps.a, p.a, p.I, p.M, p.a_pitch, 0, 0, kStep, q.a_blocks ? 2 : 0) &&
                encode(&maps.b[0], p.b, p.J, p.M, p.b_pitch, 0, 0, kStep, q.b_blocks ? half / kStep : 0);
     }
-    for (int m = 0; mode != kGradWeight && m < kRowBoxes && (32 << m) <= half && fine; ++m)
+    for (int m = 0; !THREADS && mode != kGradWeight && m < kRowBoxes && (32 << m) <= half && fine; ++m)
         fine = encode(&maps.b[m], p.a, p.R, p.M, p.a_pitch, 0, 0, 32 << m, 0);
     if (!fine) return COMBO_ERR_CUDA;
     cudaError_t e;
     const int most = smem_optin - kStaticSmem;
-    if (mode == kForward) e = out_bytes == 2 ? launch_tc_inst<CG, kForward, 2>(q, maps, most, grid, st) : launch_tc_inst<CG, kForward, 4>(q, maps, most, grid, st);
-    else if (mode == kGradInput) e = out_bytes == 2 ? launch_tc_inst<CG, kGradInput, 2>(q, maps, most, grid, st) : launch_tc_inst<CG, kGradInput, 4>(q, maps, most, grid, st);
-    else e = out_bytes == 2 ? launch_tc_inst<CG, kGradWeight, 2>(q, maps, most, grid, st) : launch_tc_inst<CG, kGradWeight, 4>(q, maps, most, grid, st);
+    if (mode == kForward) e = out_bytes == 2 ? launch_tc_inst<CG, kForward, 2, THREADS>(q, maps, most, grid, st) : launch_tc_inst<CG, kForward, 4, THREADS>(q, maps, most, grid, st);
+    else if (mode == kGradInput) e = out_bytes == 2 ? launch_tc_inst<CG, kGradInput, 2, THREADS>(q, maps, most, grid, st) : launch_tc_inst<CG, kGradInput, 4, THREADS>(q, maps, most, grid, st);
+    else e = out_bytes == 2 ? launch_tc_inst<CG, kGradWeight, 2, THREADS>(q, maps, most, grid, st) : launch_tc_inst<CG, kGradWeight, 4, THREADS>(q, maps, most, grid, st);
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "grouped product launch");
 }
 
@@ -760,20 +839,19 @@ combo_status product(int mode, const void* rows1, int64_t pitch1, const void* ro
         p.R = (int)width1;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (elem_bytes == 2 && p.a_vec && p.b_vec && (mode == kGradWeight ? M > 0 : true)) {
+    if (elem_bytes == 2) {
         Product t = p;
         if (mode != kGradWeight) t.I = p.J;      // the weights' index is the height there
+        // TMA wants 16-byte bases, pitches and strides (and a row at least)
+        if (!p.a_vec || !p.b_vec || M == 0) return launch_tc<1, true>(t, mode, out_bytes, sms, smem, st);
         // Pairs of CTAs halve what the tensor cores and L2 deliver for a product; a single one wastes less where there are
         // too few tiles of 256 outputs for all pairs.  Measured: 16 x 1065 rows, 1024 -> 4096: 118 us against 131; 16 rows,
         // 1024 -> 1024: no difference.
         const long long heights = (t.I + 255) / 256, widths = mode == kGradWeight ? (t.J + 255) / 256 : 1;
-        if (heights * widths * N >= sms / 2) return launch_tc<2>(t, mode, out_bytes, sms, smem, st);
-        return launch_tc<1>(t, mode, out_bytes, sms, smem, st);
+        if (heights * widths * N >= sms / 2) return launch_tc<2, false>(t, mode, out_bytes, sms, smem, st);
+        return launch_tc<1, false>(t, mode, out_bytes, sms, smem, st);
     }
-    cudaError_t e;
-    if (elem_bytes == 4) e = launch_fma<4, 4>(p, mode, st);
-    else if (out_bytes == 2) e = launch_fma<2, 2>(p, mode, st);
-    else e = launch_fma<2, 4>(p, mode, st);
+    const cudaError_t e = launch_fma(p, mode, st);
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "grouped product launch");
 }
 
