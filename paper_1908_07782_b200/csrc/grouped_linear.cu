@@ -212,7 +212,7 @@ __device__ __forceinline__ bool give_up(int site) {
 
 constexpr int kOutWarps = 4;                 // one for each quarter of TMEM's lanes (eight were no faster)
 constexpr int kFirstOutWarp = 4;
-constexpr int kLoadWarps = 8;                // where threads load: warps behind those
+constexpr int kLoadWarps = 16;               // where threads load: warps behind those, two sets of eight
 constexpr int tc_threads(bool by_threads) { return 32 * (kFirstOutWarp + kOutWarps + (by_threads ? kLoadWarps : 0)); }
 constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kOperandA = 128 * kStep * 2;   // bytes of the height's operand in a stage
@@ -316,64 +316,76 @@ __device__ __forceinline__ void zero_tail(uint32_t at, int blocks, int left, int
 // warp brings lines of 64 values, a 32-bit word a lane; where a line begins in the middle of a word, each lane joins
 // halves of its own and its neighbour's.  (A word that the line's first or last value shares is read whole: 2 bytes of
 // the same aligned word.)  Lines and values that are not the operand's are zero, so nothing is left to be zeroed after.
-// All lines of a lot of three blocks are under way together: 24 KB of an SM's eight warps.
-template <int MODE>
-__device__ __forceinline__ void load_stage(const Product& p, const Tile& x, int k, uint32_t stage, int wl, int lane) {
+// A set of eight warps takes a lot of three blocks of 64 lines at once, so that a whole stage is under way together.  (One
+// set that asked for its next lot before storing the one at hand was slower: what bounds is the issue of the joining.)
+struct Lot {
+    uint32_t w[24];              // a warp's words: line u * 8 + wl of block gi in w[gi * 8 + u]
+    uint32_t odd, end;           // lines that begin in the middle of a word; of lane e, the value behind line e's last whole word
+    int valid[3], lines[3];      // values of a line, lines of a warp
+};
+// blocks g0 .. g0 + 2 of stage k: two of the height's operand, then the width's
+template <int MODE> __device__ __forceinline__ void load_lot(Lot& t, const Product& p, const Tile& x, int k, int g0, int blocks, int wl, int lane) {
     constexpr bool A_R = MODE == kForward, B_R = MODE != kGradWeight;
-    const int blocks = 2 + (x.n + 63) / 64;
     const unsigned char* wa = MODE == kGradWeight ? p.a : p.b + x.w * p.stride * 2;
     const unsigned char* wb = MODE == kGradWeight ? p.b : p.a;
     const long long pa = MODE == kGradWeight ? p.a_pitch : p.b_pitch, pb = MODE == kGradWeight ? p.b_pitch : p.a_pitch;
-    // r: first value of the stage and the end; an operand along r has its lines along its own index
+    // first value of the stage along r and the end of r; an operand along r has its lines along its own index
     const long long r0 = MODE == kGradWeight ? x.row0 + (long long)k * kStep : (long long)k * kStep;
     const long long r_end = MODE == kGradWeight ? x.row1 : p.R;
-    for (int g0 = 0; g0 < blocks; g0 += 3) {
-        uint32_t w[24], last[24], odd = 0;
-        int valid[3], lines[3];
+    t.odd = t.end = 0;
 #pragma unroll
-        for (int gi = 0; gi < 3; ++gi) {
-            const int g = g0 + gi;
-            const bool height = g < 2;
-            const int block = height ? g : g - 2;
-            const bool along_r = height ? A_R : B_R;
-            const long long index0 = height ? x.i0 : MODE == kGradWeight ? x.j0 : x.row0;        // of the operand's own index
-            const long long index_end = height ? p.I : MODE == kGradWeight ? p.J : x.row1;
-            const long long line0 = along_r ? index0 + block * 64 + wl : r0 + wl, line_end = along_r ? index_end : r_end;
-            const long long col0 = along_r ? r0 : index0 + block * 64, col_end = along_r ? r_end : index_end;
-            valid[gi] = g < blocks ? (int)min(max(col_end - col0, 0LL), 64LL) : 0;
-            lines[gi] = (int)min(max((line_end - line0 + 7) / 8, 0LL), 8LL);
-            const long long pitch = (height ? pa : pb) * 2;
-            const unsigned char* q = (height ? wa : wb) + line0 * pitch + col0 * 2;
-#pragma unroll
-            for (int u = 0; u < 8; ++u, q += 8 * pitch) {
-                const int e = gi * 8 + u;
-                const bool half = (reinterpret_cast<uintptr_t>(q) & 2u) != 0, on = u < lines[gi];
-                const uint32_t* word = reinterpret_cast<const uint32_t*>(q - (half ? 2 : 0)) + lane;
-                w[e] = on && 2 * lane - (half ? 1 : 0) < valid[gi] && valid[gi] > 0 ? __ldg(word) : 0u;
-                last[e] = on && half && lane == 31 && valid[gi] == 64 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(q + 126)) : 0u;
-                if (half) odd |= 1u << e;
-            }
+    for (int gi = 0; gi < 3; ++gi) {
+        const int g = g0 + gi;
+        const bool height = g < 2;
+        const int block = height ? g : g - 2;
+        const bool along_r = height ? A_R : B_R;
+        const long long index0 = height ? x.i0 : MODE == kGradWeight ? x.j0 : x.row0;        // of the operand's own index
+        const long long index_end = height ? p.I : MODE == kGradWeight ? p.J : x.row1;
+        const long long line0 = along_r ? index0 + block * 64 + wl : r0 + wl, line_end = along_r ? index_end : r_end;
+        const long long col0 = along_r ? r0 : index0 + block * 64, col_end = along_r ? r_end : index_end;
+        const int valid = g < blocks ? (int)min(max(col_end - col0, 0LL), 64LL) : 0;
+        const int lines = (int)min(max((line_end - line0 + 7) / 8, 0LL), 8LL);
+        t.valid[gi] = valid;
+        t.lines[gi] = lines;
+        const long long step = (height ? pa : pb) * 16;
+        const unsigned char* q = (height ? wa : wb) + line0 * (step / 8) + col0 * 2;
+        if (lane >> 3 == gi && valid == 64 && (lane & 7) < lines) {
+            const unsigned char* mine = q + (lane & 7) * step;
+            if (reinterpret_cast<uintptr_t>(mine) & 2u) t.end = __ldg(reinterpret_cast<const unsigned short*>(mine + 126));
         }
 #pragma unroll
-        for (int gi = 0; gi < 3; ++gi) {
-            const int g = g0 + gi;
-            if (g >= blocks) break;
-            const uint32_t to = stage + (g < 2 ? g * 64 * kStep * 2 : kOperandA + (g - 2) * 64 * kStep * 2) + wl * 128 + ((lane * 4) ^ (wl << 4));
-            const uint32_t keep = (2 * lane < valid[gi] ? 0xffffu : 0u) | (2 * lane + 1 < valid[gi] ? 0xffff0000u : 0u);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int e = gi * 8 + u;
-                uint32_t next = __shfl_down_sync(0xffffffffu, w[e], 1);
-                if (lane == 31) next = last[e];
-                const uint32_t v = (odd >> e & 1u ? __funnelshift_r(w[e], next, 16) : w[e]) & (u < lines[gi] ? keep : 0u);
-                // the width's operand along r has x.n lines
-                if (g < 2 || !B_R || (g - 2) * 64 + wl + u * 8 < x.n)
-                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + u * 1024), "r"(v) : "memory");
-            }
+        for (int u = 0; u < 8; ++u, q += step) {
+            const int e = gi * 8 + u, half = (int)(reinterpret_cast<uintptr_t>(q) >> 1 & 1u);
+            const uint32_t* word = reinterpret_cast<const uint32_t*>(q - 2 * half) + lane;
+            t.w[e] = u < lines && 2 * lane - half < valid && valid > 0 ? __ldg(word) : 0u;
+            t.odd |= (uint32_t)half << e;
         }
     }
-    fence_async();
-    __syncwarp();
+}
+template <int MODE> __device__ __forceinline__ void store_lot(const Lot& t, const Tile& x, int g0, int blocks, uint32_t stage, int wl, int lane) {
+    constexpr bool B_R = MODE != kGradWeight;
+#pragma unroll
+    for (int gi = 0; gi < 3; ++gi) {
+        const int g = g0 + gi;
+        if (g >= blocks) break;
+        const uint32_t to = stage + (g < 2 ? g * 64 * kStep * 2 : kOperandA + (g - 2) * 64 * kStep * 2) + wl * 128 + ((lane * 4) ^ (wl << 4));
+        const uint32_t keep = (2 * lane < t.valid[gi] ? 0xffffu : 0u) | (2 * lane + 1 < t.valid[gi] ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int e = gi * 8 + u;
+            uint32_t v = t.w[e];
+            if (t.odd >> e & 1u) {               // the same for the whole warp
+                uint32_t next = __shfl_down_sync(0xffffffffu, v, 1);
+                const uint32_t behind = __shfl_sync(0xffffffffu, t.end, e);
+                if (lane == 31) next = behind;
+                v = __funnelshift_r(v, next, 16);
+            }
+            v &= u < t.lines[gi] ? keep : 0u;
+            // the width's operand along r has x.n lines
+            if (g < 2 || !B_R || (g - 2) * 64 + wl + u * 8 < x.n)
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + u * 1024), "r"(v) : "memory");
+        }
+    }
 }
 
 template <int CG, int MODE, int OB, bool THREADS>
@@ -427,14 +439,21 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
     if (THREADS && warp >= kFirstOutWarp + kOutWarps) {
         // ------------------------------------------------------------ loads by threads
         Tiles<CG, MODE> tiles(q, first);
+        // two sets of three blocks: six, the most there are
+        const int set = (warp - kFirstOutWarp - kOutWarps) >> 3, wl = (warp - kFirstOutWarp - kOutWarps) & 7;
         uint32_t s = 0, ph = 0;
         bool ok = true;
         while (ok && tiles.next(x, stride)) {
+            const int blocks = 2 + (x.n + 63) / 64;
             for (int k = 0; k < x.steps && ok; ++k) {
+                Lot t;
+                load_lot<MODE>(t, q.p, x, k, set * 3, blocks, wl, lane);
                 ok = mbar_wait(empty(s), ph ^ 1u, dead_v) || give_up(49);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                load_stage<MODE>(q.p, x, k, smem + s * q.stage_bytes, warp - kFirstOutWarp - kOutWarps, lane);
+                store_lot<MODE>(t, x, set * 3, blocks, smem + s * q.stage_bytes, wl, lane);
+                fence_async();
+                __syncwarp();
                 if (elect()) mbar_arrive(full(s));
                 __syncwarp();
                 if (++s == (uint32_t)q.stages) { s = 0; ph ^= 1u; }
