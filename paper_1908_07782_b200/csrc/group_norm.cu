@@ -949,7 +949,12 @@ template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads,
 constexpr int kRowBytes = 128;                  // resident: least bytes of a position that a block of groups takes,
 constexpr int kSlabBytes = 8 * 1024;            // and of a slab
 constexpr long long kChunk = 8 * 1024;   // streamed: least elements of a chunk
+// Resident up to 8 MB and for slabs of up to 112 KB.  Measured (resident / streamed, 1, 4, 8, 16, 32 MB of input): forward,
+// bfloat16, 196 positions of 256 channels 5.1 / 6.4, 5.9 / 8.0, 6.9 / 9.7, 8.9 / 13.3, 19.4 / 22.8 us; 49 of 512 5.4 / 6.1,
+// 6.8 / 7.8, 12.0 / 9.1, 18.9 / 13.4, 35.8 / 27.9; backward, floats, 196 of 256 7.7 / 8.6, 8.2 / 8.7, 9.8 / 10.5, 11.5 / 13.5,
+// 24.8 / 21.5; backward, bfloat16, 784 of 128 (two slabs of 100 KB) 13.6 / 9.4, 14.6 / 10.6, 15.3 / 12.6.
 constexpr long long kResidentBytes = 8ll << 20;
+constexpr unsigned long long kMostSlab = 112 * 1024;
 constexpr int kMaxChannels = COMBO_NORM_MAX_CHANNELS;   // of a block of groups: bounds the tables in shared memory (40 bytes each)
 constexpr int kShortSample = 32;                // positions under which a CTA of the backward pass takes several samples
 
@@ -1008,7 +1013,7 @@ bool layout(NormParams& p, Plan& plan, int eb, bool vec, bool res, bool back, in
     p.grp_off = (unsigned)(stat + par);
     p.slab_off = (unsigned)(stat + par + grp);
     p.slab_bytes = (unsigned)slab;
-    if (slab > (1u << 20) || stat + par + grp + arrays * slab > (unsigned long long)smem_optin) return false;
+    if (arrays * slab > kMostSlab || stat + par + grp + arrays * slab > (unsigned long long)smem_optin) return false;
     plan.vec = vec;
     plan.res = res;
     plan.smem = stat + par + grp + arrays * slab;
