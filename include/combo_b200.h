@@ -424,9 +424,11 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
  * is written (not added to), zeros for a worker without rows.
  *
  * elem_bytes (of the inputs) / out_bytes: 4 / 4 float; 2 / 2 and 2 / 4 bfloat16 in,
- * bfloat16 or float out.  Products are exact to binary32 or better and accumulated in
- * binary32, the result is rounded once.  Outputs must not overlap inputs.  A NaN or
- * infinity reaches the results that its row and its worker's weights enter, no others.
+ * bfloat16 or float out.  float: multiply-adds in binary32, in the order of the sum.
+ * bfloat16: exact products, summed in binary32 by the tensor cores, which truncate at every
+ * addition of 16 products (about 1e-6 of the result's size for sums over 1000).  The result is
+ * rounded once.  Outputs must not overlap inputs.  A NaN or infinity reaches the results that
+ * its row and its worker's weights enter, no others.  Results do not change from run to run.
  * Fastest where all bases, pitches and strides are multiples of 16 bytes.
  */
 #define COMBO_LINEAR_MAX_WIDTH (1 << 20)   /* n_in, n_out */
