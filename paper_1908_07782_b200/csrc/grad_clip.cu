@@ -5,8 +5,8 @@
 // A worker's gradient is a list of tensors; all lists, one after another, form one sequence of `total` elements
 // (begin[t] = position of tensor t, first[w] = first tensor of worker w).  Every CTA takes one contiguous piece of the
 // sequence, so that it meets few workers (one or two when there are fewer workers than CTAs) and one search at
-// its start finds its place.  Inside a piece the warps take 4 KB units in turn; a unit is 8 vectors of 16
-// bytes per lane, all in flight at once, with ragged ends and unaligned tensors peeled element by element.
+// its start finds its place.  Inside a piece the warps take units of 4 KB in turn (smaller ones where there are too few of
+// those for all warps); 4 KB are 8 vectors of 16 bytes per lane, all in flight at once, with ragged ends and unaligned tensors peeled element by element.
 //
 //   k_grad_norm    sums of squares: per (CTA, worker) one binary64 partial sum in scratch.  CTA b and worker w meet in
 //                  slot b + w: along the sequence b and w never decrease and one of them grows from one meeting to
@@ -39,6 +39,7 @@ struct Table {
     const int64_t* begin;     // [n_tensors + 1]
     const int32_t* first;     // [N + 1]
     int n_tensors, N, grid;
+    int unit;                 // elements
     long long total;          // elements
     long long piece;          // elements of one CTA's piece, a multiple of the unit
     float max_norm;
@@ -217,7 +218,7 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
 }
 
 template <int EB> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_grad_norm(const Table p) {
-    constexpr int U = kUnitBytes / EB;
+    const int U = p.unit;
     __shared__ double sh[kWarps];
     combo_step::pdl_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_finish(const Table p) {
 }
 
 template <int EB> __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_grad_scale(const Table p) {
-    constexpr int U = kUnitBytes / EB;
+    const int U = p.unit;
     __shared__ double sh[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r0 = min(p.piece * blockIdx.x, p.total), r1 = min(r0 + p.piece, p.total);
@@ -385,11 +386,14 @@ combo_status norm_impl(const void* const* tensors, void* const* out, const int64
     p.norm = norm_out;
     p.coef = coef_out;
     p.partial = static_cast<double*>(scratch);
-    const long long unit = kUnitBytes / elem_bytes;
-    const long long units = (total + unit - 1) / unit;
-    // one unit for each warp, until every SM holds two CTAs; then longer pieces
-    long long grid = (units + kWarps - 1) / kWarps;
+    // one unit for each warp, the larger the unit the better, until every SM holds its CTAs; then longer pieces.
+    // Units of 512 bytes keep a warp to few tensors where there are many small ones.
     const long long most = (long long)sms * kCtasPerSm < kMaxGrid ? (long long)sms * kCtasPerSm : kMaxGrid;
+    long long unit = 512 / elem_bytes;
+    while (unit * elem_bytes < kUnitBytes && total > unit * kWarps * most) unit *= 2;
+    p.unit = (int)unit;
+    const long long units = (total + unit - 1) / unit;
+    long long grid = (units + kWarps - 1) / kWarps;
     if (grid > most) grid = most;
     if (grid < 1) grid = 1;
     p.piece = (units + grid - 1) / grid * unit;

@@ -643,26 +643,27 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
 #pragma unroll
                     for (int e = 0; e < 32; ++e) turn[MODE == kGradWeight ? lane * 33 + e : e * 33 + lane] = __uint_as_float(v[e]);
                     __syncwarp();
-                    // a lane stores 16 bytes, neighbours what lies beside it
-                    constexpr int kLane = 16 / OB, kPerLine = 32 / kLane;
+                    // out(line, col) is the result at (row0 + line, col0 + col)
+                    const long long row0 = MODE == kGradWeight ? (long long)i : x.row0 + c0, row_end = MODE == kGradWeight ? (long long)q.p.I : x.row1;
+                    const int col0 = MODE == kGradWeight ? x.j0 + c0 : i, col_end = MODE == kGradWeight ? q.p.J : q.p.I;
+                    if (q.p.c_vec && col0 + 32 <= col_end) {
+                        // a lane stores 16 bytes, neighbours what lies beside it
+                        constexpr int kLane = 16 / OB, kPerLine = 32 / kLane;
 #pragma unroll
-                    for (int e = 0; e < kPerLine; ++e) {
-                        const int line = e * (32 / kPerLine) + lane / kPerLine, col = lane % kPerLine * kLane;
-                        float o[kLane];
+                        for (int e = 0; e < kPerLine; ++e) {
+                            const int line = e * (32 / kPerLine) + lane / kPerLine, col = lane % kPerLine * kLane;
+                            float o[kLane];
 #pragma unroll
-                        for (int f = 0; f < kLane; ++f) o[f] = turn[line * 33 + col + f];
-                        const long long row = MODE == kGradWeight ? i + line : x.row0 + c0 + line;
-                        const int at = MODE == kGradWeight ? x.j0 + c0 + col : i + col, end = MODE == kGradWeight ? q.p.J : q.p.I;
-                        if (row < (MODE == kGradWeight ? (long long)q.p.I : x.row1)) {
-                            unsigned char* to = c + (row * q.p.c_pitch + at) * OB;
-                            if (q.p.c_vec && at + kLane <= end) {
-                                *reinterpret_cast<uint4*>(to) = Elem<OB>::pack(o);
-                            } else {
-#pragma unroll
-                                for (int f = 0; f < kLane; ++f)
-                                    if (at + f < end) Elem<OB>::put(to + f * OB, o[f]);
-                            }
+                            for (int f = 0; f < kLane; ++f) o[f] = turn[line * 33 + col + f];
+                            if (row0 + line < row_end)
+                                *reinterpret_cast<uint4*>(c + ((row0 + line) * q.p.c_pitch + col0 + col) * OB) = Elem<OB>::pack(o);
                         }
+                    } else if (col0 + lane < col_end) {
+                        // off 16-byte boundaries, or at the end of the lines: a line a store
+                        unsigned char* to = c + (row0 * q.p.c_pitch + col0 + lane) * OB;
+                        const int lines = (int)min(row_end - row0, 32LL);
+#pragma unroll 8
+                        for (int line = 0; line < lines; ++line, to += q.p.c_pitch * OB) Elem<OB>::put(to, turn[line * 33 + lane]);
                     }
                     __syncwarp();
                 }
