@@ -50,60 +50,64 @@ __device__ __forceinline__ void rows_of(const Product& p, int w, long long& r0, 
 }
 
 // ---------------------------------------------------------------- binary32 multiply-adds
-// float operands: 128 x 128 outputs for a block of 256 threads, 8 x 8 each, 16 values of r at a time through two shared-
-// memory stages; the next stage's loads are in registers while this one's products are formed.  Any pitch and alignment.
-constexpr int kFT = 128, kFK = 16, kFThreads = 256;
+// float operands: FT x FT outputs for a block of 256 threads, 128 with 8 x 8 each or 64 with 4 x 4, 16 values of r at a time
+// through two shared-memory stages; the next stage's loads are in registers while this one's products are formed.  Any
+// pitch and alignment.
+constexpr int kFK = 16, kFThreads = 256;
 constexpr int kFPad = 4;
 
-// Eight neighbouring elements of one line; those at or beyond `left` are zero.
-__device__ __forceinline__ void load8(const unsigned char* q, int left, bool vec, float (&v)[8]) {
-    if (vec && left >= 8) {
-        const uint4 a = *reinterpret_cast<const uint4*>(q), b = *reinterpret_cast<const uint4*>(q + 16);
-        float x[4], y[4];
-        Elem<4>::unpack(a, x);
-        Elem<4>::unpack(b, y);
+// N neighbouring elements of one line; those at or beyond `left` are zero.
+template <int N> __device__ __forceinline__ void load_some(const unsigned char* q, int left, bool vec, float (&v)[N]) {
+    if (vec && left >= N) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = x[i]; v[4 + i] = y[i]; }
+        for (int i = 0; i < N; i += 4) {
+            float x[4];
+            Elem<4>::unpack(*reinterpret_cast<const uint4*>(q + i * 4), x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i + k] = x[k];
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<4>::get(q + i * 4) : 0.0f;
+        for (int i = 0; i < N; ++i) v[i] = i < left ? Elem<4>::get(q + i * 4) : 0.0f;
     }
 }
 
-// A thread's share of a 128 x 16 operand tile.  ALONG_R: r is contiguous; else the tile index is.
-template <bool ALONG_R>
+// A thread's share, N = FT / 16 neighbours, of an FT x 16 operand tile.  ALONG_R: r is contiguous; else the tile index is.
+template <bool ALONG_R, int N>
 __device__ __forceinline__ void load_part(const unsigned char* base, long long pitch, long long i0, long long i_end, long long r0,
-                                          long long r_end, bool vec, float (&v)[8]) {
+                                          long long r_end, bool vec, float (&v)[N]) {
+    constexpr int kLine = 16 / N;                // threads for a line along r
     const int t = threadIdx.x;
-    const long long i = i0 + (ALONG_R ? t >> 1 : (t & 15) * 8), r = r0 + (ALONG_R ? (t & 1) * 8 : t >> 4);
+    const long long i = i0 + (ALONG_R ? t / kLine : (t & 15) * N), r = r0 + (ALONG_R ? t % kLine * N : t >> 4);
     const long long left = ALONG_R ? (i < i_end ? r_end - r : 0) : (r < r_end ? i_end - i : 0);
-    const int n = (int)min(max(left, 0LL), 8LL);
-    load8(base + (ALONG_R ? i * pitch + r : r * pitch + i) * 4, n, vec, v);
+    load_some<N>(base + (ALONG_R ? i * pitch + r : r * pitch + i) * 4, (int)min(max(left, 0LL), (long long)N), vec, v);
 }
 
-template <bool ALONG_R> __device__ __forceinline__ void store_part(float (*s)[kFT + kFPad], const float (&v)[8]) {
+template <bool ALONG_R, int N> __device__ __forceinline__ void store_part(float (*s)[N * 16 + kFPad], const float (&v)[N]) {
+    constexpr int kLine = 16 / N;
     const int t = threadIdx.x;
     if (ALONG_R) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s[(t & 1) * 8 + k][t >> 1] = v[k];
+        for (int k = 0; k < N; ++k) s[t % kLine * N + k][t / kLine] = v[k];
     } else {
-        float4* d = reinterpret_cast<float4*>(&s[t >> 4][(t & 15) * 8]);
-        d[0] = make_float4(v[0], v[1], v[2], v[3]);
-        d[1] = make_float4(v[4], v[5], v[6], v[7]);
+        float4* d = reinterpret_cast<float4*>(&s[t >> 4][(t & 15) * N]);
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) d[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
     }
 }
 
-template <int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const Product p) {
+template <int MODE, int FT> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const Product p) {
+    constexpr int N = FT / 16, H = FT / 64;      // of a thread: elements of an operand tile; lots of 4 rows and of 4 columns
     constexpr bool A_R = MODE != kGradWeight, B_R = MODE == kForward;
-    __shared__ __align__(16) float sa[2][kFK][kFT + kFPad];
-    __shared__ __align__(16) float sb[2][kFK][kFT + kFPad];
+    __shared__ __align__(16) float sa[2][kFK][FT + kFPad];
+    __shared__ __align__(16) float sb[2][kFK][FT + kFPad];
     const int t = threadIdx.x;
     int w = 0;
     long long i0, i1, r0 = 0, r1 = p.R;
-    const long long j0 = (long long)blockIdx.x * kFT;
+    const long long j0 = (long long)blockIdx.x * FT;
     if (MODE == kGradWeight) {
         w = blockIdx.z;
-        i0 = (long long)blockIdx.y * kFT;
+        i0 = (long long)blockIdx.y * FT;
         i1 = p.I;
         rows_of(p, w, r0, r1);
     } else {
@@ -114,7 +118,7 @@ template <int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const 
             __shared__ int tiles[kFThreads];
             long long a = 0, b = 0;
             if (w0 + t < p.N) rows_of(p, w0 + t, a, b);
-            tiles[t] = (int)((b - a + kFT - 1) / kFT);
+            tiles[t] = (int)((b - a + FT - 1) / FT);
             __syncthreads();
             for (int k = 0; k < kFThreads && w0 + k < p.N; ++k) {
                 if (blockIdx.y < before + tiles[k]) { w = w0 + k; found = true; break; }
@@ -124,17 +128,17 @@ template <int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const 
         }
         if (!found) return;
         rows_of(p, w, i0, i1);
-        i0 += ((long long)blockIdx.y - before) * kFT;
+        i0 += ((long long)blockIdx.y - before) * FT;
     }
     const unsigned char* a = p.a;
     const unsigned char* b = MODE == kGradWeight ? p.b : p.b + w * p.stride * 4;
-    f32x2 acc[8][4];
+    f32x2 acc[4 * H][2 * H];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4 * H; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+        for (int j = 0; j < 2 * H; ++j) acc[i][j] = 0;
     const int ti = t >> 4, tj = t & 15;
-    float va[8], vb[8];
+    float va[N], vb[N];
     int s = 0;
     if (r0 < r1) {
         load_part<A_R>(a, p.a_pitch, i0, i1, r0, r1, p.a_vec, va);
@@ -151,17 +155,20 @@ template <int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const 
         }
 #pragma unroll
         for (int k = 0; k < kFK; ++k) {
-            const float4 x0 = *reinterpret_cast<const float4*>(&sa[s][k][ti * 4]);
-            const float4 x1 = *reinterpret_cast<const float4*>(&sa[s][k][64 + ti * 4]);
-            const ulonglong2 y0 = *reinterpret_cast<const ulonglong2*>(&sb[s][k][tj * 4]);
-            const ulonglong2 y1 = *reinterpret_cast<const ulonglong2*>(&sb[s][k][64 + tj * 4]);
-            const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-            const f32x2 y[4] = {y0.x, y0.y, y1.x, y1.y};
+            float xs[4 * H];
+            f32x2 ys[2 * H];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const f32x2 xx = pair(x[i], x[i]);
+            for (int h = 0; h < H; ++h) {
+                const float4 x = *reinterpret_cast<const float4*>(&sa[s][k][h * 64 + ti * 4]);
+                const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&sb[s][k][h * 64 + tj * 4]);
+                xs[4 * h] = x.x; xs[4 * h + 1] = x.y; xs[4 * h + 2] = x.z; xs[4 * h + 3] = x.w;
+                ys[2 * h] = y.x; ys[2 * h + 1] = y.y;
+            }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fma2(xx, y[j], acc[i][j]);
+            for (int i = 0; i < 4 * H; ++i) {
+                const f32x2 xx = pair(xs[i], xs[i]);
+#pragma unroll
+                for (int j = 0; j < 2 * H; ++j) acc[i][j] = fma2(xx, ys[j], acc[i][j]);
             }
         }
         if (more) {
@@ -173,11 +180,11 @@ template <int MODE> __global__ void __launch_bounds__(kFThreads, 2) k_fma(const 
     }
     unsigned char* c = MODE == kGradWeight ? p.c + w * p.stride * 4 : p.c;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4 * H; ++i) {
         const long long row = i0 + (i >> 2) * 64 + ti * 4 + (i & 3);
         if (row >= i1) continue;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
             const long long col = j0 + h * 64 + tj * 4;
             unsigned char* q = c + (row * p.c_pitch + col) * 4;
             const float v[4] = {lo_of(acc[i][2 * h]), hi_of(acc[i][2 * h]), lo_of(acc[i][2 * h + 1]), hi_of(acc[i][2 * h + 1])};
@@ -688,17 +695,17 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
 }
 
 // ---------------------------------------------------------------- host
-cudaError_t launch_fma(const Product& p, int mode, cudaStream_t st) {
-    const unsigned cols = (unsigned)((p.J + kFT - 1) / kFT);
+template <int FT> cudaError_t launch_fma(const Product& p, int mode, cudaStream_t st) {
+    const unsigned cols = (unsigned)((p.J + FT - 1) / FT);
     if (mode == kGradWeight) {
-        const dim3 grid(cols, (unsigned)((p.I + kFT - 1) / kFT), (unsigned)p.N);
-        k_fma<kGradWeight><<<grid, kFThreads, 0, st>>>(p);
+        const dim3 grid(cols, (unsigned)((p.I + FT - 1) / FT), (unsigned)p.N);
+        k_fma<kGradWeight, FT><<<grid, kFThreads, 0, st>>>(p);
     } else {
         // every worker adds less than one tile to those its rows fill
-        const long long tiles = p.M / kFT + (p.N < p.M ? p.N : p.M);
+        const long long tiles = p.M / FT + (p.N < p.M ? p.N : p.M);
         const dim3 grid(cols, (unsigned)(tiles < 1 ? 1 : tiles));
-        if (mode == kForward) k_fma<kForward><<<grid, kFThreads, 0, st>>>(p);
-        else k_fma<kGradInput><<<grid, kFThreads, 0, st>>>(p);
+        if (mode == kForward) k_fma<kForward, FT><<<grid, kFThreads, 0, st>>>(p);
+        else k_fma<kGradInput, FT><<<grid, kFThreads, 0, st>>>(p);
     }
     return cudaGetLastError();
 }
@@ -876,7 +883,12 @@ combo_status product(int mode, const void* rows1, int64_t pitch1, const void* ro
         if (heights * widths * N >= sms / 2) return launch_tc<2, false>(t, mode, out_bytes, sms, smem, st);
         return launch_tc<1, false>(t, mode, out_bytes, sms, smem, st);
     }
-    const cudaError_t e = launch_fma(p, mode, st);
+    // Tiles of 128 read shared memory half as often; those of 64 serve where 128 leave SMs idle or most of their rows.
+    // Measured (128 / 64): 14 tiles of 128 (7 x 94 rows, 305 -> 144) 44 / 21 us, 64 (8 x 200, 512 -> 512) 58 / 43, 128 whole
+    // ones (gradient of the weights, 512 x 512) 25 / 31, 2304 (32 x 1046, 512 -> 1000) 778 / 1106; 16 x 1 row 107 / 77.
+    const long long mean = mode == kGradWeight ? p.I : (M + N - 1) / N;
+    const bool narrow = (mean + 127) / 128 * ((p.J + 127) / 128) * N * 2 <= sms || mean <= 64;
+    const cudaError_t e = narrow && M <= (1 << 21) ? launch_fma<64>(p, mode, st) : launch_fma<128>(p, mode, st);
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "grouped product launch");
 }
 
