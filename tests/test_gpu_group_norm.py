@@ -208,6 +208,9 @@ SHAPES = [
     ([3, 0, 2], 1500, 512, 32, 0, 0),              # streamed for its size, chunks of unequal length
     ([2, 1], 1300, 1026, 18, 2, 0),                # the same, 57 channels a group, no whole vectors
     ([2], 700, 2304, 9, 8, 8),                     # more vectors than threads in a block
+    ([1, 1], 3001, 128, 32, 0, 0),                 # streamed, 4 channels a group
+    ([2], 7000, 64, 32, 8, 0),                     # streamed, 2 channels a group
+    ([1, 0, 2], 5000, 24, 8, 0, 0),                # streamed, 3 channels a group
 ]
 
 

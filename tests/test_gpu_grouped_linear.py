@@ -126,11 +126,12 @@ def test_larger(types):
     run_all([500, 1100, 0, 731], 520, 776, *types, seed=3)
 
 
+@pytest.mark.parametrize("widths", [(72, 88), (71, 89)])
 @pytest.mark.parametrize("types", TYPES)
-def test_nan_stays_with_its_row_and_worker(types):
+def test_nan_stays_with_its_row_and_worker(types, widths):
     dtype, odt = types
     g = torch.Generator().manual_seed(5)
-    counts, n_in, n_out = [70, 60, 130], 72, 88
+    counts, (n_in, n_out) = [70, 60, 130], widths
     begin = begin_of(counts)
     _, x = rows_array(260, n_in, n_in, dtype, g)
     _, dy = rows_array(260, n_out, n_out, dtype, g)
