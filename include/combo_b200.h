@@ -459,6 +459,13 @@ combo_status combo_device_status(void);
  * CTA (short inputs). */
 int combo_last_kernel_path(void);
 
+/* Which kernels the last combo_grouped_linear* or combo_group_norm* call on this
+ * thread launched: 0 none; products: 1 multiply-adds (float), 2 tensor cores, one
+ * CTA a tile, 3 tensor cores, a pair of CTAs a tile, 4 tensor cores, operands brought
+ * by threads (bases, pitches or strides off 16 bytes); group norm: 5 slabs resident in
+ * shared memory, 6 streamed in two passes. */
+int combo_last_step_path(void);
+
 /* Forces a path for the following calls on this thread: 0 automatic (default),
  * 1 direct gather (blocks taken worker-fastest, so that the gather's re-reads
  * are served by L2), 2 staged with persistent CTAs (falls back to direct where

@@ -15,6 +15,7 @@ _lib = None
 
 COMBO_OK = 0
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+STEP_NONE, STEP_MULTIPLY_ADD, STEP_TENSOR, STEP_TENSOR_PAIRS, STEP_TENSOR_THREADS, STEP_RESIDENT, STEP_STREAMED = range(7)
 PATH_AUTO, PATH_DIRECT, PATH_STAGED, PATH_TILE, PATH_DIRECT_NAIVE = 0, 1, 2, 5, 6
 
 
@@ -69,6 +70,7 @@ def load():
         "combo_debug_dead_wait": [vp],
         "combo_device_status": [],
         "combo_last_kernel_path": [],
+        "combo_last_step_path": [],
         "combo_version": [],
     }
     for name, args in sigs.items():
@@ -433,6 +435,11 @@ def combo_device_status():
 
 def combo_last_kernel_path() -> int:
     return load().combo_last_kernel_path()
+
+
+def combo_last_step_path() -> int:
+    """Which kernels the last product or group norm call on this thread launched (STEP_*)."""
+    return load().combo_last_step_path()
 
 
 def combo_set_kernel_path(path: int) -> None:

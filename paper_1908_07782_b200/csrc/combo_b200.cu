@@ -20,6 +20,7 @@ using combo::AggParams;
 
 thread_local char t_cuda_err[256] = "";
 thread_local int t_last_path = 0;
+thread_local int t_last_step_path = 0;
 thread_local int t_force_path = 0;
 thread_local int t_tile = 0;
 thread_local int t_stages = 0;
@@ -864,6 +865,8 @@ namespace combo_host {
 
 combo_status fail(cudaError_t e, const char* what) { return cuda_fail(e, what); }
 
+void set_step_path(StepPath path) { t_last_step_path = path; }
+
 combo_status device(int* sms, int* smem_optin) {
     DeviceInfo* dev = nullptr;
     combo_status rc = device_info(&dev);
@@ -1233,6 +1236,8 @@ combo_status combo_device_status(void) {
 }
 
 int combo_last_kernel_path(void) { return t_last_path; }
+
+int combo_last_step_path(void) { return t_last_step_path; }
 
 void combo_set_kernel_path(int path) { t_force_path = (path == 1 || path == 2 || path == 3 || path == 5 || path == 6) ? path : 0; }
 

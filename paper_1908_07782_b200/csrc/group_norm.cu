@@ -1062,6 +1062,7 @@ Kernels pick(int eb, bool back, const Plan& plan, int act) {
 cudaError_t launch(const NormParams& p, const Plan& plan, int eb, bool back, int act, int smem_optin, cudaStream_t st) {
     static uint64_t allowed[2][48];
     const Kernels k = pick(eb, back, plan, act);
+    combo_host::set_step_path(plan.res ? combo_host::kPathResident : combo_host::kPathStreamed);
     cudaError_t e = combo_host::allow_smem(k.first, smem_optin, &allowed[0][k.number]);
     if (e != cudaSuccess) return e;
     k.first<<<(unsigned)plan.grid, kThreads, plan.smem, st>>>(p);

@@ -696,6 +696,7 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
 
 // ---------------------------------------------------------------- host
 template <int FT> cudaError_t launch_fma(const Product& p, int mode, cudaStream_t st) {
+    combo_host::set_step_path(combo_host::kPathMultiplyAdd);
     const unsigned cols = (unsigned)((p.J + FT - 1) / FT);
     if (mode == kGradWeight) {
         const dim3 grid(cols, (unsigned)((p.I + FT - 1) / FT), (unsigned)p.N);
@@ -752,6 +753,7 @@ template <int CG, int MODE, int OB, bool THREADS> cudaError_t launch_tc_inst(con
 
 template <int CG, bool THREADS> combo_status launch_tc(const Product& p, int mode, int out_bytes, int sms, int smem_optin, cudaStream_t st) {
     TcParams q = {p, 256, 0, 0, 0, 0};
+    combo_host::set_step_path(THREADS ? combo_host::kPathTensorThreads : CG == 2 ? combo_host::kPathTensorPairs : combo_host::kPathTensor);
     // the height is W's (forward: n_out, rows' gradient: n_in) or n_out; see the table above
     const long long mt = (p.I + 128 * CG - 1) / (128 * CG);
     long long tiles;

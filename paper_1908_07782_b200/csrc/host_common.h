@@ -13,6 +13,9 @@ namespace combo_host {
 combo_status fail(cudaError_t e, const char* what);
 // The current device's SM count and largest shared memory of a block; COMBO_ERR_UNSUPPORTED unless it is 10.x.
 combo_status device(int* sms, int* smem_optin);
+// What combo_last_step_path() answers on this thread.
+enum StepPath { kPathNone = 0, kPathMultiplyAdd = 1, kPathTensor = 2, kPathTensorPairs = 3, kPathTensorThreads = 4, kPathResident = 5, kPathStreamed = 6 };
+void set_step_path(StepPath path);
 // Status word of the grouped products' kernels (see combo_device_status): reads it, and clears it if it is set.
 cudaError_t grouped_linear_status(int* code);
 // cuTensorMapEncodeTiled without interleaving, out-of-bounds elements read as zero; false (and a text for
