@@ -20,7 +20,9 @@
 //
 // Forward statistics: each thread takes mean and M2 (sum of squared deviations from its own mean) of its positions,
 // for each run of channels of its vector that lie in one group, and these are merged by counts: sum of n_i * mean_i for
-// the mean, M2_i + n_i (mean_i - mean)^2 for M2.  Nothing is cancelled, whatever the size of the mean.
+// the mean, M2_i + n_i (mean_i - mean)^2 for M2.  No large squares are subtracted: a large mean costs what its own
+// rounding to binary32 does, two or three units of its last place.  (Resident: two passes.  Streamed: one pass about a pivot
+// that follows the mean, so that a first position, or a first chunk, far from all others costs nothing either.)
 //
 // z is formed in the roundings of the formula as written (no FMA), in both directions alike: a value that the forward
 // pass clipped at zero is a value whose gradient the backward pass drops.
@@ -624,9 +626,10 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads, kStreamC
     const unsigned char* x = p.x + (b * p.L + at.l0 + at.trow) * xp + (long long)at.c0 * EB;
     const int n = at.positions(at.trow);
     for (int col = at.tcol; col < at.nv; col += at.cstep) {
-        // sums of the distances from a channel's first value and of their squares: mean and M2 of the thread's few
-        // positions by one pass (the first value lies among them, so the squares do not outgrow what they measure)
-        f32x2 pivot[P], s[P], q[P];
+        // sums of the distances from a pivot and of their squares, one pass; the pivot is a channel's first value, and the mean
+        // of all positions so far each time their number has doubled.  Those behind a pivot are then never more than those
+        // it is the mean of, and s * s / count takes at most half of q away (7/8 of the first batch's)
+        f32x2 pivot[P], s[P], q[P];              // the pivot negated
         const unsigned char* from = x + col * VB;
         if (n > 0) Ln::widen(*reinterpret_cast<const typename Ln::Raw*>(from), pivot);
 #pragma unroll
@@ -644,8 +647,20 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads, kStreamC
                 q[i] = fma2(d, d, q[i]);
             }
         };
+        // the pivot becomes the mean of the first `count` positions, q their M2
+        const auto move = [&](int count) {
+            const float inv = 1.0f / (float)max(count, 1);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const f32x2 off = mul2(s[i], pair(inv, inv));
+                q[i] = fma2(neg2(s[i]), off, q[i]);
+                pivot[i] = add2(pivot[i], neg2(off));
+                s[i] = 0;
+            }
+        };
         Batch<EB, VEC, kBatch> v, next;          // the next ones are under way while these are added
         next.load(from, step, n);
+        int mark = kBatch;
         for (int k = 0; k < n; k += kBatch) {
             v = next;
             from += kBatch * step;
@@ -653,20 +668,19 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads, kStreamC
             if (n - k >= kBatch) {
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) take(v.raw[j]);
+                if (k + kBatch == mark) {
+                    move(mark);
+                    mark *= 2;
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j)
                     if (j < n - k) take(v.raw[j]);
             }
         }
-        // (negated) mean and M2 of each channel, then of each run: equal counts merge as means and half squared distances
-        const float inv = 1.0f / (float)max(n, 1);
-        f32x2 m[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            m[i] = fma2(s[i], pair(-inv, -inv), pivot[i]);
-            q[i] = fma2(neg2(s[i]), mul2(s[i], pair(inv, inv)), q[i]);
-        }
+        // mean and M2 of each channel, then of each run: equal counts merge as means and half squared distances
+        move(n);
+        f32x2(&m)[P] = pivot;
         Ln::merge(m, q, at.sub, (float)n);
         store_runs<Ln>(stat + at.trow * (at.cb / at.sub) + col * V / at.sub, at.sub, m, q);
     }
@@ -676,19 +690,22 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads, kStreamC
     });
 }
 
-// Adds what the sample's chunks left for each of the block's groups, groups side by side and a group's chunks in lots:
-// acc = add(chunk's pair, first chunk's pair, chunk, acc), then done(group, sums, first chunk's pair).  The block.
-template <typename At, typename A, typename D>
-__device__ __forceinline__ void gather_chunks(const NormParams& p, const At& at, float2* lots, A add, D done) {
+// What the sample's chunks left for each of the block's groups, groups side by side and a group's chunks in lots; the block.
+// Backward: their sums, done(group, sums).
+template <typename At, typename D>
+__device__ __forceinline__ void gather_chunks(const NormParams& p, const At& at, float2* lots, D done) {
     const int parts = max(kThreads / at.ng, 1), part = (int)threadIdx.x / at.ng;
     const float2* e = p.part + at.lot * p.chunks * p.G + at.g0;
     if (part < parts)
         for (int g = (int)threadIdx.x - part * at.ng; g < at.ng; g += kThreads) {
-            const float2 v0 = e[g];
             float2 acc = make_float2(0.0f, 0.0f);
 #pragma unroll 8
-            for (int k = part; k < p.chunks; k += parts) acc = add(e[(long long)k * p.G + g], v0, k, acc);
-            if (parts == 1) done(g, acc, v0);
+            for (int k = part; k < p.chunks; k += parts) {
+                const float2 v = e[(long long)k * p.G + g];
+                acc.x += v.x;
+                acc.y += v.y;
+            }
+            if (parts == 1) done(g, acc);
             else lots[part * at.ng + g] = acc;
         }
     if (parts == 1) return;
@@ -696,7 +713,68 @@ __device__ __forceinline__ void gather_chunks(const NormParams& p, const At& at,
     for (int g = threadIdx.x; g < at.ng; g += kThreads) {
         float2 s = lots[g];
         for (int r = 1; r < parts; ++r) { s.x += lots[r * at.ng + g].x; s.y += lots[r * at.ng + g].y; }
-        done(g, s, e[g]);
+        done(g, s);
+    }
+}
+// Forward: their means and M2 merged by counts, done(group, mean, M2).  A lot is taken as k_norm_sums takes positions, about a
+// pivot that moves to the mean each time the lot's chunks have doubled; then the lots about the mean of all.
+template <typename At, typename D>
+__device__ __forceinline__ void merge_chunks(const NormParams& p, const At& at, float2* lots, D done) {
+    const int parts = min(max(kThreads / at.ng, 1), p.chunks), part = (int)threadIdx.x / at.ng;
+    const float2* e = p.part + at.lot * p.chunks * p.G + at.g0;
+    const float whole = (float)((long long)p.Lc * p.Cg), last = (float)((long long)(p.L - (p.chunks - 1) * p.Lc) * p.Cg);
+    const auto count = [&](int r) {              // values in lot r
+        const int n = (p.chunks - 1 - r) / parts + 1;
+        return (p.chunks - 1 - r) % parts == 0 ? fmaf((float)(n - 1), whole, last) : (float)n * whole;
+    };
+    if (part < parts)
+        for (int g = (int)threadIdx.x - part * at.ng; g < at.ng; g += kThreads) {
+            float pivot = 0.0f, s = 0.0f, q = 0.0f, values = 0.0f;
+            const auto move = [&]() {
+                const float off = s / values;
+                q = fmaf(-s, off, q);
+                pivot += off;
+                s = 0.0f;
+            };
+            int mark = 8;
+            for (int k = part, taken = 0; k < p.chunks; k += 8 * parts) {
+                float2 v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (k + j * parts < p.chunks) v[j] = e[(long long)(k + j * parts) * p.G + g];
+                if (taken == 0) pivot = v[0].x;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (k + j * parts < p.chunks) {
+                        const float n = k + j * parts == p.chunks - 1 ? last : whole, d = v[j].x - pivot;
+                        s = fmaf(n, d, s);
+                        q += fmaf(n * d, d, v[j].y);
+                        values += n;
+                    }
+                taken += 8;
+                if (taken == mark) {
+                    move();
+                    mark *= 2;
+                }
+            }
+            move();
+            if (parts == 1) done(g, pivot, q);
+            else lots[part * at.ng + g] = make_float2(pivot, q);
+        }
+    if (parts == 1) return;
+    __syncthreads();
+    const float total = (float)((long long)p.L * p.Cg);
+    for (int g = threadIdx.x; g < at.ng; g += kThreads) {
+        const float first = lots[g].x;
+        float s = 0.0f, q = 0.0f;
+        for (int r = 1; r < parts; ++r) s = fmaf(count(r), lots[r * at.ng + g].x - first, s);
+        const float m = first + s / total;
+        for (int r = 0; r < parts; ++r) {
+            const float2 v = lots[r * at.ng + g];
+            const float d = v.x - m;
+            q += fmaf(count(r) * d, d, v.y);
+        }
+        done(g, m, q);
     }
 }
 
@@ -717,14 +795,8 @@ template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads,
     if (at.tcol < at.nv) next.load(x + at.tcol * VB, step, n);
     load_params(p, worker_of(p, b), at.c0, at.cb, ga_s, be_s);
     combo_step::pdl_wait();
-    // the chunks' pairs merged by counts, about the first chunk's mean
-    gather_chunks(p, at, lots, [&](float2 v, float2 v0, int k, float2 acc) {
-        const float cnt = (float)((long long)min(p.Lc, p.L - k * p.Lc) * p.Cg), d = v.x - v0.x;
-        return make_float2(fmaf(cnt, d, acc.x), acc.y + fmaf(cnt * d, d, v.y));
-    }, [&](int g, float2 s, float2 v0) {
-        const float total = (float)((long long)p.L * p.Cg), off = s.x / total;
-        const float around = fmaf(-s.x, off, s.y);       // about the mean; below zero by rounding alone
-        const float m = v0.x + off, rs = 1.0f / sqrtf((around < 0.0f ? 0.0f : around) / total + p.eps);
+    merge_chunks(p, at, lots, [&](int g, float m, float q) {
+        const float rs = 1.0f / sqrtf((q < 0.0f ? 0.0f : q) / (float)((long long)p.L * p.Cg) + p.eps);     // below zero by rounding alone
         fin[g] = make_float2(m, rs);
         if (at.chunk == 0) {
             if (p.mean) p.mean[b * p.G + at.g0 + g] = m;
@@ -906,8 +978,7 @@ template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads,
     load_params(p, worker_of(p, b), at.c0, at.cb, ga_s, be_s);
     combo_step::pdl_wait();
     const float inv = 1.0f / (float)((long long)p.L * p.Cg);
-    gather_chunks(p, at, lots, [](float2 v, float2, int, float2 acc) { return make_float2(acc.x + v.x, acc.y + v.y); },
-                  [&](int g, float2 s, float2) { fin[g] = make_float2(s.x * inv, s.y * inv); });
+    gather_chunks(p, at, lots, [&](int g, float2 s) { fin[g] = make_float2(s.x * inv, s.y * inv); });
     __syncthreads();
     for (int col = at.tcol; col < at.nv; col += at.cstep) {
         f32x2 m[P], rs[P], ga[P], be[P], m1[P], m2[P];
