@@ -430,8 +430,9 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
  * elem_bytes (of the inputs) / out_bytes: 4 / 4 float; 2 / 2 and 2 / 4 bfloat16 in,
  * bfloat16 or float out.  float: multiply-adds in binary32, in the order of the sum.
  * bfloat16: exact products, summed in binary32 by the tensor cores, which truncate at every
- * addition of 16 products (about 1e-6 of the result's size for sums over 1000).  The result is
- * rounded once.  Outputs must not overlap inputs.  A NaN or infinity reaches the results that
+ * addition of 16 products: about 1e-6 of the sum of the magnitudes for sums over 1000, 8e-6 over
+ * 4096; longer sums are cut into parts of 4096 that are added with rounding, so it stays at that.
+ * The result is rounded once.  Outputs must not overlap inputs.  A NaN or infinity reaches the results that
  * its row and its worker's weights enter, no others.  Results do not change from run to run.
  * Fastest where all bases, pitches and strides are multiples of 16 bytes.
  */

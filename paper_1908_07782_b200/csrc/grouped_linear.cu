@@ -214,6 +214,13 @@ template <int MODE, int FT> __global__ void __launch_bounds__(kFThreads, 2) k_fm
 // each, so that the next tile's products run meanwhile), turn them through shared memory and store them.  The last rows
 // of a worker in the gradient of the weights: what the load brought beyond them is zeroed in shared memory before the
 // products see it, by a warp of its own in a stage of its own (another worker's NaN would not vanish by being multiplied with zero).
+//
+// The tensor cores truncate each addition of 16 products to the accumulator, towards zero: over terms of one sign the
+// error grows faster than their number, 8e-7 of the sum after 1000 terms, 8e-6 after 4096, 3e-4 after 65536.  A sum of more
+// than kPartSteps stages is therefore cut into parts of that many, formed one after another in the first accumulator and
+// added with rounding, by the warps that take results, to the second one, which such a tile has to itself: 8e-6 whatever the
+// length.  Measured (whole / in parts): gradient of the weights 1024 x 1024 into floats, 4 x 16384 rows 135 / 138 us, 16 x 5000
+// 138 / 156; forward 16 x 500 rows, 8192 -> 1024: 139 / 148.  Parts of 2048 would leave 2e-6 and catch sums of 4096.
 using namespace combo_tc;
 
 __device__ int g_linear_status;              // 0, or the site of the first wait that gave up
@@ -230,6 +237,7 @@ constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kOperandA = 128 * kStep * 2;   // bytes of the height's operand in a stage
 constexpr int kRowBoxes = 4;                 // boxes of 32, 64, 128 or 256 rows of X or dY
 constexpr int kMaxStages = 8;
+constexpr int kPartSteps = 64;               // stages of r that the tensor cores sum by themselves: 4096 values
 constexpr int kTurn = 32 * 33 * 4;           // bytes in which an epilogue warp turns 32 x 32 outputs
 constexpr int kTmemColumns = 512;
 constexpr int kStaticSmem = 1024;           // room for the kernel's barriers
@@ -311,6 +319,22 @@ template <int CG, int MODE> struct Tiles {
         }
         t += stride;
         return true;
+    }
+};
+
+// Whose turn it is of the two accumulators, alike in the warp that issues products and in those that take results.  Tiles take
+// them in turn; one whose sum is cut into parts takes both, and the tile behind it waits for the first.
+struct Turns {
+    uint32_t buf = 0, uses = 0;              // the tile's accumulator (its first); bit b: whether that of accumulator b is odd
+    // parts of the tile's sum (none where no row is summed)
+    __device__ __forceinline__ int begin(const Tile& x) {
+        if (x.steps > kPartSteps) buf = 0;
+        return (x.steps + kPartSteps - 1) / kPartSteps;
+    }
+    __device__ __forceinline__ uint32_t parity(int part) const { return (uses >> buf ^ (uint32_t)part) & 1u; }
+    __device__ __forceinline__ void end(int parts) {
+        uses ^= (uint32_t)(parts & 1) << buf;
+        buf = parts == 0 ? buf : parts == 1 ? buf ^ 1u : 0u;
     }
 };
 
@@ -548,18 +572,18 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
         // ------------------------------------------------------------ products, by one thread of the leader
         if (rank == 0) {
             Tiles<CG, MODE> tiles(q, first);
-            uint32_t done = 0, accs = 0, tails = 0;
+            uint32_t done = 0, tails = 0;
+            Turns turns;
             bool ok = true;
             while (tiles.next(x, stride)) {
                 if (x.steps == 0) continue;
-                const uint32_t buf = accs & 1u;
+                const int parts = turns.begin(x);
+                const uint32_t buf = turns.buf;
                 const int rest = MODE == kGradWeight ? (int)((x.row1 - x.row0) % kStep) : 0;
                 const int plain = !THREADS && rest % 16 != 0 ? x.steps - 1 : x.steps;
                 if (elect()) {
                     const uint32_t d = tmem + buf * 256, kind = product_kind(128 * CG, x.n, A_R, B_R);
                     uint32_t s = done % q.stages, ph = done / q.stages & 1u;
-                    ok = mbar_wait(acc_empty(buf), (accs >> 1 & 1u) ^ 1u, dead_v) || give_up(44);
-                    tc_fence_after();
                     const auto issue = [&](uint32_t a, int n16, bool add) {
                         const uint64_t da = operand(a, A_R, 64 * kStep * 2), db = operand(a + kOperandA, B_R, 64 * kStep * 2);
 #pragma unroll
@@ -567,30 +591,35 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
                             if (MODE != kGradWeight || c < n16)
                                 mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, add || c > 0);
                     };
-                    for (int k = 0; k < plain && ok; ++k) {
-                        if (!mbar_wait(full(s), ph, dead_v)) { ok = give_up(45); break; }
+                    for (int part = 0; part < parts && ok; ++part) {
+                        const int k0 = part * kPartSteps, k1 = min(k0 + kPartSteps, x.steps);
+                        if (!mbar_wait(acc_empty(buf), turns.parity(part) ^ 1u, dead_v)) { ok = give_up(44); break; }
                         tc_fence_after();
-                        issue(smem + s * q.stage_bytes, k + 1 == x.steps && rest ? (rest + 15) / 16 : kStep / 16, k > 0);
-                        mma_commit<CG>(empty(s));
-                        if (++s == q.stages) { s = 0; ph ^= 1u; }
-                    }
-                    if (MODE == kGradWeight && plain < x.steps && ok) {
-                        // zeros that threads of both CTAs have written
-                        if (CG == 1 ? mbar_wait(tail_ready, tails & 1u, dead_v) : mbar_wait_cluster(tail_ready, tails & 1u, dead_v)) {
+                        for (int k = k0; k < min(k1, plain); ++k) {
+                            if (!mbar_wait(full(s), ph, dead_v)) { ok = give_up(45); break; }
                             tc_fence_after();
-                            issue(tail_at, (rest + 15) / 16, plain > 0);
-                            mma_commit<CG>(tail_empty);
-                        } else {
-                            ok = give_up(46);
+                            issue(smem + s * q.stage_bytes, k + 1 == x.steps && rest ? (rest + 15) / 16 : kStep / 16, k > k0);
+                            mma_commit<CG>(empty(s));
+                            if (++s == q.stages) { s = 0; ph ^= 1u; }
                         }
+                        if (MODE == kGradWeight && plain < k1 && ok) {
+                            // zeros that threads of both CTAs have written
+                            if (CG == 1 ? mbar_wait(tail_ready, tails & 1u, dead_v) : mbar_wait_cluster(tail_ready, tails & 1u, dead_v)) {
+                                tc_fence_after();
+                                issue(tail_at, (rest + 15) / 16, plain > k0);
+                                mma_commit<CG>(tail_empty);
+                            } else {
+                                ok = give_up(46);
+                            }
+                        }
+                        if (ok) mma_commit<CG>(acc_full(buf));
                     }
-                    if (ok) mma_commit<CG>(acc_full(buf));
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 done += plain;
                 if (plain < x.steps) ++tails;
-                ++accs;
+                turns.end(parts);
             }
             if (!ok) *dead_v = 1;
         }
@@ -620,32 +649,44 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
         Tiles<CG, MODE> tiles(q, first);
         const int quarter = warp & 3;        // a warp reads the 32 lanes of TMEM that its number allows
         float* turn = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + (q.stages + (MODE == kGradWeight && !THREADS ? 1 : 0)) * q.stage_bytes + quarter * kTurn);
-        uint32_t accs = 0;
+        Turns turns;
         bool ok = true;
         while (tiles.next(x, stride)) {
-            const uint32_t buf = accs & 1u;
             const int i = x.i0 + rank * 128 + quarter * 32;
             const bool any = x.steps > 0;
-            if (any) {
-                ok = mbar_wait(acc_full(buf), accs >> 1 & 1u, dead_v) || give_up(47);
+            const int parts = turns.begin(x);
+            const uint32_t buf = turns.buf, lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+            const int columns = i < q.p.I ? MODE == kGradWeight ? min(x.n, q.p.J - x.j0) : (int)(x.row1 - x.row0) : 0;
+            const auto release = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(CG == 1 ? acc_empty(buf) : at_leader(acc_empty(buf)));
+            };
+            for (int part = 0; part < parts; ++part) {
+                ok = mbar_wait(acc_full(buf), turns.parity(part), dead_v) || give_up(47);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_fence_after();
+                if (parts == 1) break;
+                for (int c0 = 0; c0 < columns; c0 += 16) tmem_fold16(lanes + c0, lanes + 256 + c0, part > 0);
+                tmem_store_wait();
+                // the last part's accumulator goes with the sums, which the next tile but one may overwrite
+                if (part + 1 < parts) release();
             }
+            if (!ok) break;
             unsigned char* c = MODE == kGradWeight ? q.p.c + x.w * q.p.stride * OB : q.p.c;
-            const int wide = MODE == kGradWeight ? min(x.n, q.p.J - x.j0) : (int)(x.row1 - x.row0);
-            if (i < q.p.I) {
+            if (columns > 0) {
                 // lots of 32 columns; the next lot's load is under way while this one is stored
-                const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16);
+                const uint32_t acc = lanes + (parts > 1 ? 256 : buf * 256);
                 uint32_t next[32];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) next[e] = 0u;
                 if (any) tmem_load32(acc, next);
-                for (int c0 = 0; c0 < wide; c0 += 32) {
+                for (int c0 = 0; c0 < columns; c0 += 32) {
                     uint32_t v[32];
                     if (any) tmem_load_wait(next);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = next[e];
-                    if (any && c0 + 32 < wide) tmem_load32(acc + c0 + 32, next);
+                    if (any && c0 + 32 < columns) tmem_load32(acc + c0 + 32, next);
                     // 33 floats to a line: neither the writes nor the reads meet on a bank
 #pragma unroll
                     for (int e = 0; e < 32; ++e) turn[MODE == kGradWeight ? lane * 33 + e : e * 33 + lane] = __uint_as_float(v[e]);
@@ -675,12 +716,8 @@ __global__ void __launch_bounds__(tc_threads(THREADS), 1) k_tc(const TcParams q,
                     __syncwarp();
                 }
             }
-            if (any) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(CG == 1 ? acc_empty(buf) : at_leader(acc_empty(buf)));
-                ++accs;
-            }
+            if (any) release();
+            turns.end(parts);
         }
         if (!ok) *dead_v = 1;
     }
