@@ -257,6 +257,45 @@ def _bytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+_SIZES = {torch.float32: 4, torch.bfloat16: 2}
+_MAX_WORKERS = 8192
+
+
+def _refuse(name: str, what: str):
+    raise ValueError("%s: %s" % (name, what))
+
+
+def _on_gpu(name, *tensors):
+    """Refuses what is not on the current GPU: a kernel cannot read the host's memory, and what it is given are addresses."""
+    at = None
+    for t in tensors:
+        if t is not None:
+            d = t.get_device()
+            if d != at:
+                if at is not None or d < 0 or d != _device():
+                    _refuse(name, "all tensors must be on the current GPU, got one on %s" % t.device)
+                at = d
+
+
+def _short(t, dtype, least) -> bool:
+    return t is not None and (t.dtype is not dtype or t.numel() < least or not t.is_contiguous())
+
+
+def _lists(name, tensors, out, begin, first, n_tensors, N, norm_out, coef_out, scratch):
+    """Types, lengths and places of a table of tensors and of what is written per worker.  (None and counts out of range are
+    left to the library's own refusal.)"""
+    n, w = (n_tensors, N) if n_tensors >= 0 and 1 <= N <= _MAX_WORKERS else (-1, -1)
+    if _short(tensors, torch.int64, n) or _short(out, torch.int64, n):
+        _refuse(name, "tensors and out must be int64 addresses, %d in a row" % n)
+    if _short(begin, torch.int64, n + 1):
+        _refuse(name, "begin must be int64, %d in a row" % (n + 1))
+    if _short(first, torch.int32, w + 1):
+        _refuse(name, "first must be int32, %d in a row" % (w + 1))
+    if _short(norm_out, torch.float32, w) or _short(coef_out, torch.float32, w):
+        _refuse(name, "norm_out and coef_out must be float32, %d in a row" % w)
+    _on_gpu(name, tensors, out, begin, first, norm_out, coef_out, scratch)
+
+
 def combo_grad_scratch_bytes(N: int) -> int:
     return int(load().combo_grad_scratch_bytes(N))
 
@@ -266,6 +305,7 @@ def combo_grad_norm(tensors, begin, first, n_tensors, N, total, elem_bytes, max_
     """Norm of every worker's gradient over its tensors, and the coefficient that clips it
     to ``max_norm`` (float32 [N] each, device).  ``tensors``: device int64 addresses;
     ``begin``: device int64 [n_tensors + 1] positions; ``first``: device int32 [N + 1]."""
+    _lists("combo_grad_norm", tensors, None, begin, first, n_tensors, N, norm_out, coef_out, scratch)
     _check(load().combo_grad_norm(_ptr(tensors), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes, max_norm,
                                   _ptr(norm_out), _ptr(coef_out), _ptr(scratch), _bytes(scratch), _stream(stream)),
            "combo_grad_norm")
@@ -276,6 +316,7 @@ def combo_grad_clip(tensors, out, begin, first, n_tensors, N, total, elem_bytes,
                     stream=None):
     """combo_grad_norm, and every tensor times its worker's coefficient, written to the
     addresses in ``out`` (device int64; may be ``tensors``)."""
+    _lists("combo_grad_clip", tensors, out, begin, first, n_tensors, N, norm_out, coef_out, scratch)
     _check(load().combo_grad_clip(_ptr(tensors), _ptr(out), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes,
                                   max_norm, _ptr(norm_out), _ptr(coef_out), _ptr(scratch), _bytes(scratch),
                                   _stream(stream)), "combo_grad_clip")
@@ -285,17 +326,11 @@ def combo_grad_clip(tensors, out, begin, first, n_tensors, N, total, elem_bytes,
 def combo_check_tensors(tensors, begin, first, n_tensors, N, total, elem_bytes, stream=None) -> int:
     """0 when the table is as combo_grad_norm wants it, else 1 + a bad tensor, or
     1 + n_tensors + a bad worker."""
+    _lists("combo_check_tensors", tensors, None, begin, first, n_tensors, N, None, None, None)
     flag = torch.zeros(1, dtype=torch.int32, device=begin.device)
     _check(load().combo_check_tensors(_ptr(tensors), _ptr(begin), _ptr(first), n_tensors, N, total, elem_bytes,
                                       _stream(stream), _ptr(flag)), "combo_check_tensors")
     return int(flag.item())
-
-
-_SIZES = {torch.float32: 4, torch.bfloat16: 2}
-
-
-def _refuse(name: str, what: str):
-    raise ValueError("%s: %s" % (name, what))
 
 
 def _pitch(shape, stride, name, arg) -> int:
@@ -349,10 +384,11 @@ def combo_group_norm(x, y, gamma, beta, begin, groups, eps, act, mean, rstd, scr
     name = "combo_group_norm"
     size, N, param_size, param_pitch = _norm_args(name, x, (y,), gamma, beta, begin, (mean, rstd), groups)
     B, L, C = shape = x.shape
-    _check(load().combo_group_norm(x.data_ptr(), _pitch(shape, x.stride(), name, "x"), y.data_ptr(),
-                                   _pitch(shape, y.stride(), name, "y"), size, _ptr(gamma), _ptr(beta), param_size,
-                                   param_pitch, _ptr(begin), N, B, L, C, groups, eps, act, _ptr(mean), _ptr(rstd),
-                                   _ptr(scratch), _bytes(scratch), _stream(stream)), name)
+    xp, yp = _pitch(shape, x.stride(), name, "x"), _pitch(shape, y.stride(), name, "y")
+    _on_gpu(name, x, y, gamma, beta, begin, mean, rstd, scratch)
+    _check(load().combo_group_norm(x.data_ptr(), xp, y.data_ptr(), yp, size, _ptr(gamma), _ptr(beta), param_size, param_pitch,
+                                   _ptr(begin), N, B, L, C, groups, eps, act, _ptr(mean), _ptr(rstd), _ptr(scratch),
+                                   _bytes(scratch), _stream(stream)), name)
     return y
 
 
@@ -374,9 +410,10 @@ def combo_group_norm_backward(dy, x, dx, gamma, beta, begin, groups, act, mean, 
         grad_pitch = _rows(dgamma.shape, dgamma.stride(), name, "dgamma")
         if grad_pitch != _rows(dbeta.shape, dbeta.stride(), name, "dbeta"):
             _refuse(name, "dgamma and dbeta must have one pitch")
+    dyp, xp, dxp = (_pitch(shape, t.stride(), name, arg) for t, arg in ((dy, "dy"), (x, "x"), (dx, "dx")))
+    _on_gpu(name, dy, x, dx, gamma, beta, begin, mean, rstd, dgamma, dbeta, scratch)
     _check(load().combo_group_norm_backward(
-        dy.data_ptr(), _pitch(shape, dy.stride(), name, "dy"), x.data_ptr(), _pitch(shape, x.stride(), name, "x"),
-        dx.data_ptr(), _pitch(shape, dx.stride(), name, "dx"), size, _ptr(gamma), _ptr(beta), param_size, param_pitch,
+        dy.data_ptr(), dyp, x.data_ptr(), xp, dx.data_ptr(), dxp, size, _ptr(gamma), _ptr(beta), param_size, param_pitch,
         _ptr(begin), N, B, L, C, groups, act, _ptr(mean), _ptr(rstd), _ptr(dgamma), _ptr(dbeta), grad_pitch,
         _ptr(scratch), _bytes(scratch), _stream(stream)), name)
     return dx
@@ -396,8 +433,9 @@ def _product_args(name, a, b, weights, begin, a_width, b_width, same):
         _refuse(name, "weights: a row's elements must be neighbours")
     if same[0].dtype != same[1].dtype or a.dtype not in _SIZES or b.dtype not in _SIZES or weights.dtype not in _SIZES:
         _refuse(name, "types are float32 and bfloat16, one for both inputs")
-    return (N, M, n_in, n_out, _rows(a.shape, a.stride(), name, "rows"), _rows(b.shape, b.stride(), name, "rows"),
-            stride[1] if n_out > 1 else n_in, stride[0] if N > 1 else 0)
+    pitches = _rows(a.shape, a.stride(), name, "rows"), _rows(b.shape, b.stride(), name, "rows")
+    _on_gpu(name, a, b, weights, begin)
+    return (N, M, n_in, n_out, *pitches, stride[1] if n_out > 1 else n_in, stride[0] if N > 1 else 0)
 
 
 def combo_grouped_linear(x, w, y, begin, stream=None):
