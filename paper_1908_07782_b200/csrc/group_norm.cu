@@ -1044,6 +1044,7 @@ constexpr long long kChunk = 8 * 1024;   // streamed: least elements of a chunk
 // 24.8 / 21.5; backward, bfloat16, 784 of 128 (two slabs of 100 KB) 13.6 / 9.4, 14.6 / 10.6, 15.3 / 12.6.
 constexpr long long kResidentBytes = 8ll << 20;
 constexpr unsigned long long kMostSlab = 112 * 1024;
+constexpr int kMostCtas = 512;                  // streamed: most chunks of all samples together, where there are more than samples
 constexpr int kMaxChannels = COMBO_NORM_MAX_CHANNELS;   // of a block of groups: bounds the tables in shared memory (40 bytes each)
 constexpr int kShortSample = 32;                // positions under which a CTA of the backward pass takes several samples
 
@@ -1054,10 +1055,13 @@ struct Plan {
 };
 
 int samples_per_cta(int L) { return L >= kShortSample ? 1 : (kShortSample + L - 1) / L; }
-// most chunks of a sample
-int chunks_of(int64_t L, int64_t C) {
-    const int64_t n = (L * C + kChunk - 1) / kChunk;
-    return (int)(n < L ? n : L);
+// Most chunks of a sample: of kChunk elements at least, a position at least, and no more in all than a device runs at once (444
+// CTAs on 148 SMs), which bounds the scratch memory by the samples and channels, whatever the length.
+int chunks_of(int64_t B, int64_t L, int64_t C) {
+    int64_t n = (L * C + kChunk - 1) / kChunk;
+    if (n > L) n = L;
+    if (n > kMostCtas / B) n = kMostCtas / B;
+    return (int)(n < 1 ? 1 : n);
 }
 
 // Tables and blocks of groups for one way; false where its shared memory does not suffice.
@@ -1083,7 +1087,7 @@ bool layout(NormParams& p, Plan& plan, int eb, bool vec, bool res, bool back, in
     p.ns = res && back ? samples_per_cta(p.L) : 1;
     p.chunks = 1;
     if (!res) {                                  // as many as have all CTAs on the device at once, where that is enough of them
-        const long long slots = (long long)sms * kStreamCtas / (p.B * p.nblk), most = chunks_of(p.L, p.C);
+        const long long slots = (long long)sms * kStreamCtas / (p.B * p.nblk), most = chunks_of(p.B, p.L, p.C);
         p.chunks = (int)(slots < 1 ? 1 : slots < most ? slots : most);
     }
     p.Lc = (p.L + p.chunks - 1) / p.chunks;
@@ -1158,7 +1162,7 @@ cudaError_t launch(const NormParams& p, const Plan& plan, int eb, bool back, int
 }
 
 // Scratch: sums per chunk and group, then (backward) per chunk and channel
-size_t part_bytes(int64_t B, int64_t L, int64_t C, int groups) { return ((size_t)B * chunks_of(L, C) * groups * 8 + 127) / 128 * 128; }
+size_t part_bytes(int64_t B, int64_t L, int64_t C, int groups) { return ((size_t)B * chunks_of(B, L, C) * groups * 8 + 127) / 128 * 128; }
 
 // What forward and backward ask alike.
 combo_status check_shape(int elem_bytes, int param_bytes, const void* gamma, const void* beta, int64_t param_pitch,
@@ -1199,7 +1203,7 @@ size_t combo_group_norm_scratch_bytes(int64_t B, int64_t L, int64_t C, int group
     if (B < 0 || L < 1 || C < 1 || L > (1 << 28) || C > (1 << 20) || B > (1LL << 40) / L / C || groups < 1 || groups > C)
         return 0;
     const int64_t n = B < 1 ? 1 : B;
-    return part_bytes(n, L, C, groups) + (size_t)n * chunks_of(L, C) * C * sizeof(float2);
+    return part_bytes(n, L, C, groups) + (size_t)n * chunks_of(n, L, C) * C * sizeof(float2);
 }
 
 combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y_pitch, int elem_bytes, const void* gamma,
