@@ -372,7 +372,8 @@ combo_status combo_check_tensors(const void* const* d_tensors, const int64_t* d_
  *
  * x, y, dy, dx: elem_bytes 4 = float or 2 = bfloat16, aligned to it; positions lie
  * `..._pitch` >= C elements apart, samples L pitches.  y may be x, and dx may be x or
- * dy, with the same pitch; other overlaps are refused.  gamma, beta: param_bytes 4 or
+ * dy, with the same pitch; other overlaps are refused (arrays of one pitch whose channels
+ * lie beside each other, views of one wider array, do not overlap).  gamma, beta: param_bytes 4 or
  * 2, worker w's at + w * param_pitch elements -- a flat [N][P] array is given by its
  * first vector's place and pitch P --; both NULL for 1 and 0.  d_begin: device
  * int64[N + 1], worker w's samples are d_begin[w] .. d_begin[w+1] - 1 (ascending,
@@ -432,7 +433,8 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
  * bfloat16: exact products, summed in binary32 by the tensor cores, which truncate at every
  * addition of 16 products: about 1e-6 of the sum of the magnitudes for sums over 1000, 8e-6 over
  * 4096; longer sums are cut into parts of 4096 that are added with rounding, so it stays at that.
- * The result is rounded once.  Outputs must not overlap inputs.  A NaN or infinity reaches the results that
+ * The result is rounded once.  Outputs must not overlap inputs (rows of one pitch may lie
+ * beside each other in a wider array).  A NaN or infinity reaches the results that
  * its row and its worker's weights enter, no others.  Results do not change from run to run.
  * Fastest where all bases, pitches and strides are multiples of 16 bytes.
  */

@@ -1184,11 +1184,12 @@ combo_status check_shape(int elem_bytes, int param_bytes, const void* gamma, con
 bool array_ok(const void* p, int64_t pitch, int64_t C, int eb) {
     return p && combo_host::aligned_to(p, eb) && pitch >= C && pitch <= (1LL << 40) / C;
 }
-size_t extent(int64_t B, int64_t L, int64_t C, int64_t pitch, int eb) { return B < 1 ? 0 : (size_t)((B * L - 1) * pitch + C) * eb; }
 bool vec_ok(const void* p, int64_t pitch, int eb) { return combo_host::aligned_to(p, 16) && pitch * eb % 16 == 0; }
 // an output may be an input, element for element; it may not overlap it in any other way
-bool clash(const void* out, int64_t out_pitch, size_t out_n, const void* in, int64_t in_pitch, size_t in_n) {
-    return combo_host::overlap(out, out_n, in, in_n) && !(out == in && out_pitch == in_pitch);
+bool clash(const void* out, int64_t out_pitch, const void* in, int64_t in_pitch, int64_t positions, int64_t C, int eb) {
+    if (out == in && (out_pitch == in_pitch || positions == 1)) return false;
+    const size_t width = (size_t)C * eb;
+    return combo_host::overlap(combo_host::Rows{out, positions, width, (size_t)out_pitch * eb}, combo_host::Rows{in, positions, width, (size_t)in_pitch * eb});
 }
 
 bool scratch_ok(const void* scratch, size_t bytes, int64_t B, int64_t L, int64_t C, int groups) {
@@ -1216,8 +1217,7 @@ combo_status combo_group_norm(const void* x, int64_t x_pitch, void* y, int64_t y
     if (B == 0) return COMBO_OK;
     if (!array_ok(x, x_pitch, C, elem_bytes) || !array_ok(y, y_pitch, C, elem_bytes)) return COMBO_ERR_INVALID_ARG;
     if (!combo_host::aligned_to(mean_out, 4) || !combo_host::aligned_to(rstd_out, 4)) return COMBO_ERR_INVALID_ARG;
-    if (clash(y, y_pitch, extent(B, L, C, y_pitch, elem_bytes), x, x_pitch, extent(B, L, C, x_pitch, elem_bytes)))
-        return COMBO_ERR_ALIAS;
+    if (clash(y, y_pitch, x, x_pitch, B * L, C, elem_bytes)) return COMBO_ERR_ALIAS;
     int sms = 0, smem = 0;
     if ((rc = combo_host::device(&sms, &smem)) != COMBO_OK) return rc;
     NormParams p = {};
@@ -1280,9 +1280,7 @@ combo_status combo_group_norm_backward(const void* dy, int64_t dy_pitch, const v
             !array_ok(dx, dx_pitch, C, elem_bytes) || !mean || !rstd)
             return COMBO_ERR_INVALID_ARG;
         if (!combo_host::aligned_to(mean, 4) || !combo_host::aligned_to(rstd, 4)) return COMBO_ERR_INVALID_ARG;
-        const size_t n = extent(B, L, C, dx_pitch, elem_bytes);
-        if (clash(dx, dx_pitch, n, x, x_pitch, extent(B, L, C, x_pitch, elem_bytes)) ||
-            clash(dx, dx_pitch, n, dy, dy_pitch, extent(B, L, C, dy_pitch, elem_bytes)))
+        if (clash(dx, dx_pitch, x, x_pitch, B * L, C, elem_bytes) || clash(dx, dx_pitch, dy, dy_pitch, B * L, C, elem_bytes))
             return COMBO_ERR_ALIAS;
     }
     if ((rc = combo_host::device(&sms, &smem)) != COMBO_OK) return rc;

@@ -846,9 +846,6 @@ bool vec_ok(const void* p, int64_t pitch, int64_t stride, int eb) {
     return combo_host::aligned_to(p, 16) && pitch * eb % 16 == 0 && stride * eb % 16 == 0;
 }
 
-// rows, each `width` elements, `pitch` apart
-size_t extent(int64_t rows, int64_t width, int64_t pitch, int eb) { return rows < 1 ? 0 : (size_t)((rows - 1) * pitch + width) * eb; }
-
 // Checks and launches one of the three.
 combo_status product(int mode, const void* rows1, int64_t pitch1, const void* rows2, int64_t pitch2, const void* weights,
                      int64_t w_pitch, int64_t w_stride, int elem_bytes, int out_bytes, const int64_t* begin, int N, int64_t M,
@@ -870,13 +867,11 @@ combo_status product(int mode, const void* rows1, int64_t pitch1, const void* ro
         return COMBO_ERR_INVALID_ARG;
     if (N > 1 && (w_stride < (n_out - 1) * w_pitch + n_in || w_stride > (1LL << 44) / N)) return COMBO_ERR_INVALID_ARG;
     if (N == 1) w_stride = 0;
-    const size_t n1 = extent(M, width1, pitch1, elem_bytes), n2 = extent(M, width2, pitch2, eb2);
+    const combo_host::Rows r1 = {rows1, M, (size_t)width1 * elem_bytes, (size_t)pitch1 * elem_bytes};
+    const combo_host::Rows r2 = {rows2, M, (size_t)width2 * eb2, (size_t)pitch2 * eb2};
     const size_t nw = ((size_t)(N - 1) * w_stride + (n_out - 1) * w_pitch + n_in) * ebw;
-    const void* out = mode == kGradWeight ? weights : rows2;
-    const size_t nout = mode == kGradWeight ? nw : n2;
-    if (combo_host::overlap(out, nout, rows1, n1) ||
-        combo_host::overlap(out, nout, mode == kGradWeight ? rows2 : weights, mode == kGradWeight ? n2 : nw))
-        return COMBO_ERR_ALIAS;
+    const auto in_weights = [&](const combo_host::Rows& r) { return combo_host::overlap(weights, nw, r.p, r.extent()); };
+    if (mode == kGradWeight ? in_weights(r1) || in_weights(r2) : combo_host::overlap(r2, r1) || in_weights(r2)) return COMBO_ERR_ALIAS;
     int sms = 0, smem = 0;
     combo_status rc = combo_host::device(&sms, &smem);
     if (rc != COMBO_OK) return rc;

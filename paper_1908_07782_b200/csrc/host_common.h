@@ -32,6 +32,23 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return na && nb && x < y + nb && y < x + na;
 }
 
+// Rows of `width` bytes, `pitch` apart, and whether two such arrays share a byte.  Views of one wider array (equal pitches) lie
+// beside each other where their columns do; other arrays are taken to share what their extents share.
+struct Rows {
+    const void* p;
+    int64_t n;
+    size_t width, pitch;
+    size_t extent() const { return n < 1 ? 0 : (size_t)(n - 1) * pitch + width; }
+};
+inline bool overlap(const Rows& a, const Rows& b) {
+    if (!overlap(a.p, a.extent(), b.p, b.extent())) return false;
+    const size_t pitch = a.n > 1 ? a.pitch : b.pitch;
+    if (b.n > 1 && b.pitch != pitch) return true;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    const size_t off = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;      // of b's columns behind the start of a's
+    return off < a.width || off + b.width > pitch;
+}
+
 // Lets `kern` use up to `bytes` of dynamic shared memory, once per kernel and device: `done` is the kernel's own word
 // of device bits (asking the driver costs as much as a launch).
 template <typename K> inline cudaError_t allow_smem(K kern, int bytes, uint64_t* done) {
