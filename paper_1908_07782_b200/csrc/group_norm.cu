@@ -5,7 +5,7 @@
 //   dz = dy * act'(z),  dgamma_w = sum dz * h,  dbeta_w = sum dz,  t = dz * gamma_w
 //   dx = rstd * (t - mean(t) - h * mean(t * h))
 //
-// Bound by HBM: forward 1 read and 1 write of x, backward 2 reads and 1 write.  Two ways, by a rule on sizes (choose()):
+// Bound by HBM: forward 1 read and 1 write of x, backward 2 reads and 1 write.  Two ways, by a rule on sizes (resident()):
 //
 //   resident   small inputs and short samples, one launch: a CTA brings the slab of a (sample, block of whole groups) into
 //              shared memory, reduces it and writes the result from there.  Every thread works on the vectors it loaded
@@ -1038,12 +1038,13 @@ template <int EB, bool VEC, int ACT> __global__ void __launch_bounds__(kThreads,
 constexpr int kRowBytes = 128;                  // resident: least bytes of a position that a block of groups takes,
 constexpr int kSlabBytes = 8 * 1024;            // and of a slab
 constexpr long long kChunk = 8 * 1024;   // streamed: least elements of a chunk
-// Resident up to 8 MB and for slabs of up to 112 KB.  Measured (resident / streamed, 1, 4, 8, 16, 32 MB of input): forward,
-// bfloat16, 196 positions of 256 channels 5.1 / 6.4, 5.9 / 8.0, 6.9 / 9.7, 8.9 / 13.3, 19.4 / 22.8 us; 49 of 512 5.4 / 6.1,
-// 6.8 / 7.8, 12.0 / 9.1, 18.9 / 13.4, 35.8 / 27.9; backward, floats, 196 of 256 7.7 / 8.6, 8.2 / 8.7, 9.8 / 10.5, 11.5 / 13.5,
-// 24.8 / 21.5; backward, bfloat16, 784 of 128 (two slabs of 100 KB) 13.6 / 9.4, 14.6 / 10.6, 15.3 / 12.6.
+// Where the resident way is taken; measured at resident().
 constexpr long long kResidentBytes = 8ll << 20;
-constexpr unsigned long long kMostSlab = 112 * 1024;
+constexpr long long kShortBytes = 32 * 1024;
+constexpr long long kManySamples = 180;         // for each that a CTA takes
+constexpr long long kSamplesPerWorker = 64;
+constexpr int kWorkersAdding = 5;
+constexpr unsigned long long kMostSlab = 112 * 1024;   // 784 positions of 128 channels, bfloat16, two slabs of 100 KB: 13.6 / 9.4 us at 1 MB
 constexpr int kMostCtas = 512;                  // streamed: most chunks of all samples together, where there are more than samples
 constexpr int kMaxChannels = COMBO_NORM_MAX_CHANNELS;   // of a block of groups: bounds the tables in shared memory (40 bytes each)
 constexpr int kShortSample = 32;                // positions under which a CTA of the backward pass takes several samples
@@ -1114,14 +1115,32 @@ bool layout(NormParams& p, Plan& plan, int eb, bool vec, bool res, bool back, in
     return true;
 }
 
-// Resident where everything is small (one launch, no second read) or where a sample is too short to be worth a CTA's
-// tables twice; else streamed.
+// Whether the resident layout in `p` and `plan` is the faster way.  Measured, resident / streamed in us, bfloat16 unless said, 8
+// workers:
+//   forward, samples of up to 32 KB: always (1 position of 1024 channels, 4096 samples 27 / 60; 49 of 64, 1337 19 / 43).
+//   forward, longer ones: while the CTAs are no more than 1.6 times what the device holds at once, up to 8 MB: 49 of 512
+//     channels in 32 groups, 4 MB (0.85 of it) 6.6 / 8.5, 8 MB (1.7) 11.4 / 9.9, floats 8 MB (1.56) 8.4 / 8.9; 49 of 2048, 8 MB
+//     (1.14) 7.3 / 10.3; 196 of 256, 8 MB (0.57) 6.4 / 10.0.
+//   backward, several samples to a CTA (they go through it one after another, 3 to 5 us each): where there are so many that the
+//     streamed way's CTA for each costs more: 1 position of 256 channels, 512 samples 94 / 16, 2048 96 / 41, 8192 102 / 145;
+//     4 of 256, 512 samples 29 / 16, 2048 34 / 41; 8 of 1024, 256 samples 21 / 15, 1024 35 / 42.
+//   backward, others: while the CTAs fit the device at once, up to 8 MB, and the parameters' gradients, which the streamed way
+//     adds beside its second pass, are sums over few samples: 49 of 1024, 8 MB (0.57) 10.3 / 14.9; 49 of 256, 16 MB (1.7)
+//     18.6 / 14.2; for one worker instead of 8: 49 of 256, 42 samples 9.4 / 8.4, 167 18.0 / 13.9.  Samples of up to 16 KB, x and
+//     dy: always where five workers or more share the adding (49 of 64, 1337 samples for 8 workers 27 / 32, for one 78 / 38).
+bool resident(const NormParams& p, const Plan& plan, bool back, long long sample_bytes, int smem_optin, int sms) {
+    if (p.ns > 1) return p.B > kManySamples * p.ns;
+    if (!back && sample_bytes <= kShortBytes) return true;
+    if (back && sample_bytes <= kShortBytes / 2 && p.N >= kWorkersAdding) return true;
+    if (sample_bytes * p.B > kResidentBytes) return false;
+    const long long fit = (smem_optin + 1024) / (long long)(plan.smem + 1024), at_once = sms * (fit < kCtasPerSm ? fit : kCtasPerSm);
+    return back ? plan.grid <= at_once && p.B <= kSamplesPerWorker * p.N : plan.grid * 5 <= at_once * 8;
+}
+
 combo_status choose(NormParams& p, Plan& plan, int eb, bool vec, bool back, int smem_optin, int sms) {
-    const int arrays = back ? 2 : 1;
-    const long long sample = (long long)p.L * p.C * eb * arrays;
-    const bool res = sample * p.B <= kResidentBytes || sample <= 32 * 1024;
+    const long long sample_bytes = (long long)p.L * p.C * eb * (back ? 2 : 1);
     for (int v = vec ? 1 : 0; v >= 0; --v) {
-        if (res && layout(p, plan, eb, v != 0, true, back, smem_optin, sms)) break;
+        if (layout(p, plan, eb, v != 0, true, back, smem_optin, sms) && resident(p, plan, back, sample_bytes, smem_optin, sms)) break;
         if (layout(p, plan, eb, v != 0, false, back, smem_optin, sms)) break;
         if (v == 0) return COMBO_ERR_INVALID_ARG;
     }
