@@ -15,8 +15,9 @@
 //              are taken from the last one back.  A CTA has no phases in which its SM's memory pipe idles, which is worth
 //              more than the second read costs.
 //
-// Measured: forward 37 x 3136 x 256 bfloat16 32 us (18 at the copy rate), backward 98 x 784 x 128 floats 40 us (18) and
-// 123 x 196 x 1024 bfloat16 61 us (23; its three arrays outgrow L2), one sample of 8 workers, 49 x 512, 5 us.
+// Measured: forward 37 x 3136 x 256 bfloat16, ReLU, 33 us (18 at the copy rate), backward 98 x 784 x 128 floats, SiLU, 42 us (18)
+// and 123 x 196 x 1024 bfloat16, ReLU, 61 us (23; its three arrays outgrow L2), one sample of 8 workers, 49 x 512, 5 us.  Far
+// from the copy rate: samples of one or a few positions, backward (1386 x 1 x 256 floats 29 us for 4 MB).
 //
 // Forward statistics: each thread takes mean and M2 (sum of squared deviations from its own mean) of its positions,
 // for each run of channels of its vector that lie in one group, and these are merged by counts: sum of n_i * mean_i for

@@ -11,10 +11,12 @@
 //   gradient, rows    m (ragged)   k           n        A along r, B along j
 //   gradient, weights n            k           m (ragged)   both along i / j
 //
-// Measured (bfloat16 on 16-byte boundaries unless said): forward 16 x 1065 rows, 1024 -> 4096: 117 us, 1220 TFLOP/s of a
-// measured 1675 (burst) or 1385 (sustained); gradient of the weights 16 x 924 rows, 4096 -> 1024, into floats: 112 us, 1080;
-// of the rows 32 x 168, 2048 -> 1000: 45 to 68 us, by where the arrays lie, bound by its 131 MB of weights; one row a worker, 16 x 1024 -> 1024: 8.7 us for
-// 33 MB.  Off 16-byte boundaries 121 to 180 TFLOP/s; floats 46 TFLOP/s, bound by the multiply-add pipe.
+// Measured (bfloat16 on 16-byte boundaries unless said): forward 16 x 1065 rows, 1024 -> 4096: 116 to 122 us in the first hundred
+// calls (1200 TFLOP/s of a measured 1675), 136 to 144 in calls that go on (1020 of 1385), when the power limit has the clock
+// at 1.22 to 1.33 GHz instead of 1.97; gradient of the weights 16 x 924 rows, 4096 -> 1024, into floats: 112 to 118 us (1050),
+// then 130 to 139 (900); of the rows 32 x 168, 2048 -> 1000: 45 to 68 us, by where the arrays lie, bound by its 131 MB of weights;
+// one row a worker, 16 x 1024 -> 1024: 8.7 us for 33 MB.  Off 16-byte boundaries 100 to 180 TFLOP/s; floats 46 TFLOP/s, bound by
+// the multiply-add pipe.
 #include <string.h>
 
 #include "host_common.h"
