@@ -457,6 +457,76 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
                                               int64_t n_in, int64_t n_out, void* stream);
 
 /*
+ * Softmax cross entropy of a linear classifier, grouped by worker: every worker's rows
+ * against its own weights, the logits never kept.
+ *
+ *   z_mv = x_m . W_w,v      lse_m = log sum_v exp z_mv      loss_m = lse_m - z_m,label
+ *
+ * and the gradients of sum_m g_m loss_m:
+ *
+ *   d_mv = (exp(z_mv - lse_m) - [v = label_m]) g_m
+ *   dx_m = sum_v d_mv W_w,v      dW_w,v = sum_m d_mv x_m
+ *
+ * x, w, d_begin and their pitches and strides: as combo_grouped_linear, n_out being the
+ * number of classes.  d_labels: device int64[M]; a row whose label is not in
+ * 0 .. n_out - 1 has none: its loss, lse and dx are 0, and whatever it holds (NaN too)
+ * enters nothing.  Rows of no worker are neither read into a result nor written.
+ * loss_out, lse_out: device float[M].  Backward takes the lse that the forward call wrote,
+ * and row_grad, device float[M], the g_m; NULL stands for every worker's mean, g_m = 1 /
+ * (labelled rows of m's worker).  dx [M][n_in] of x's type; dW as in
+ * combo_grouped_linear_grad_weight, grad_bytes 4 = float or, for bfloat16 inputs, 2 =
+ * bfloat16; written (not added to), zeros for a worker without labelled rows.
+ *
+ * Outputs must not overlap inputs, scratch or one another (x and dx may lie beside each
+ * other in a wider array).  A NaN or infinity reaches the results that its row and its
+ * worker's weights enter, no others.  Results do not change from run to run.
+ *
+ * scratch: device memory of at least combo_grouped_cross_entropy_scratch_bytes bytes
+ * (grad_bytes 0 for the forward call), 256-byte aligned, contents undefined afterwards.
+ */
+size_t combo_grouped_cross_entropy_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes,
+                                                 int grad_bytes);
+combo_status combo_grouped_cross_entropy(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch,
+                                         int64_t w_stride, int elem_bytes, const int64_t* d_labels,
+                                         const int64_t* d_begin, int N, int64_t M, int64_t n_in, int64_t n_out,
+                                         float* loss_out, float* lse_out, void* scratch, size_t scratch_bytes,
+                                         void* stream);
+combo_status combo_grouped_cross_entropy_backward(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch,
+                                                  int64_t w_stride, int elem_bytes, const int64_t* d_labels,
+                                                  const float* lse, const float* row_grad, void* dx,
+                                                  int64_t dx_pitch, void* dw, int64_t dw_pitch, int64_t dw_stride,
+                                                  int grad_bytes, const int64_t* d_begin, int N, int64_t M,
+                                                  int64_t n_in, int64_t n_out, void* scratch,
+                                                  size_t scratch_bytes, void* stream);
+
+/*
+ * Dropout whose mask is a function of counters and is never stored:
+ *
+ *   y = residual + (kept ? x * 65536 / (65536 - T) : 0),   T = p * 65536 rounded
+ *
+ * x, residual (NULL: none), y: [M][n], elem_bytes 4 = float or 2 = bfloat16, rows
+ * `..._pitch` >= n elements apart, worker w's being d_begin[w] .. d_begin[w+1] - 1 (as
+ * above; NULL if N == 1: all rows).  The backward pass is the same call on dy without a
+ * residual.
+ *
+ * kept: with `step` one step of splitmix64 (the output for state z), worker
+ * W = first_worker + w, the element's row r among its worker's and column c,
+ *
+ *   key = step(step(step(seed) ^ (round << 32 | W)) ^ (2^63 | site))
+ *   h = step(key ^ (r * ceil(n / 4) + c / 4)),   kept = (h >> 16 (c % 4)) % 65536 >= T
+ *
+ * so a worker's mask is the same whichever other workers are in the call and whichever GPU
+ * holds it; `site` tells apart the dropouts of one step.  p in 0 .. 1; p = 1 keeps nothing.
+ * Dropped elements are 0 (or the residual) whatever x holds.  binary32 product and sum, each
+ * rounded; rounded once more to bfloat16.  y may be x or residual (same pitch); other
+ * overlaps with y are refused.  n <= 2^32, M * n <= 2^40, first_worker + N <=
+ * COMBO_MAX_WORKERS.
+ */
+combo_status combo_dropout(const void* x, int64_t x_pitch, const void* residual, int64_t residual_pitch, void* y,
+                           int64_t y_pitch, int elem_bytes, const int64_t* d_begin, int N, int64_t M, int64_t n,
+                           float p, uint64_t seed, uint32_t round, uint32_t site, int first_worker, void* stream);
+
+/*
  * Reads and clears the device status word that kernels set when one of their
  * bounded waits gives up.  Synchronises the device.  Returns COMBO_OK or
  * COMBO_ERR_DEVICE_TIMEOUT (or COMBO_ERR_CUDA).

@@ -15,4 +15,6 @@ from .binding import (ComboError, combo_aggregation_divergence, combo_aggregatio
                       combo_group_norm, combo_group_norm_scratch_bytes, combo_group_norm_backward,
                       ACT_NONE, ACT_RELU, ACT_SILU, STEP_NONE, STEP_MULTIPLY_ADD, STEP_TENSOR, STEP_TENSOR_PAIRS,
                       STEP_TENSOR_THREADS, STEP_RESIDENT, STEP_STREAMED,
-                      combo_grouped_linear, combo_grouped_linear_grad_input, combo_grouped_linear_grad_weight)
+                      combo_grouped_linear, combo_grouped_linear_grad_input, combo_grouped_linear_grad_weight,
+                      combo_grouped_cross_entropy, combo_grouped_cross_entropy_backward,
+                      combo_grouped_cross_entropy_scratch_bytes, combo_dropout)

@@ -67,6 +67,10 @@ def load():
         "combo_grouped_linear": [vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, i32, i64, i64, i64, vp],
         "combo_grouped_linear_grad_input": [vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, i32, i64, i64, i64, vp],
         "combo_grouped_linear_grad_weight": [vp, i64, vp, i64, vp, i64, i64, i32, i32, vp, i32, i64, i64, i64, vp],
+        "combo_grouped_cross_entropy": [vp, i64, vp, i64, i64, i32, vp, vp, i32, i64, i64, i64, vp, vp, vp, ctypes.c_size_t, vp],
+        "combo_grouped_cross_entropy_backward": [vp, i64, vp, i64, i64, i32, vp, vp, vp, vp, i64, vp, i64, i64, i32, vp, i32, i64, i64,
+                                                 i64, vp, ctypes.c_size_t, vp],
+        "combo_dropout": [vp, i64, vp, i64, vp, i64, i32, vp, i32, i64, i64, f32, u64, u32, u32, i32, vp],
         "combo_debug_dead_wait": [vp],
         "combo_device_status": [],
         "combo_last_kernel_path": [],
@@ -83,6 +87,8 @@ def load():
     lib.combo_grad_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_group_norm_scratch_bytes.argtypes = [i64, i64, i64, i32]
     lib.combo_group_norm_scratch_bytes.restype = ctypes.c_size_t
+    lib.combo_grouped_cross_entropy_scratch_bytes.argtypes = [i32, i64, i64, i64, i32, i32]
+    lib.combo_grouped_cross_entropy_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_set_kernel_path.argtypes = [i32]
     lib.combo_set_kernel_path.restype = None
     lib.combo_set_tuning.argtypes = [i32, i32]
@@ -468,6 +474,87 @@ def combo_grouped_linear_grad_weight(dy, x, dw, begin, stream=None):
                                                    _SIZES[dy.dtype], _SIZES[dw.dtype], begin.data_ptr(), N, M, n_in, n_out,
                                                    _stream(stream)), name)
     return dw
+
+
+def _loss_args(name, x, w, labels, floats, begin):
+    """What the two cross entropy calls check alike: x [M, n_in], w [N, n_out, n_in], labels [M], `floats` float32 [M] or None."""
+    if len(x.shape) != 2 or len(w.shape) != 3 or x.dtype not in _SIZES or w.dtype != x.dtype:
+        _refuse(name, "x must be [M, n_in] and w [N, n_out, n_in] of one type, float32 or bfloat16")
+    (M, n_in), shape, stride = x.shape, w.shape, w.stride()
+    N, n_out = shape[0], shape[1]
+    if shape[2] != n_in:
+        _refuse(name, "x is %d wide, the weights %d" % (n_in, shape[2]))
+    if n_in > 1 and stride[2] != 1:
+        _refuse(name, "w: a row's elements must be neighbours")
+    if labels.dtype != torch.int64 or labels.numel() != M or not labels.is_contiguous():
+        _refuse(name, "labels must be int64 [M]")
+    for t in floats:
+        if t is not None and (t.dtype != torch.float32 or t.numel() != M or not t.is_contiguous()):
+            _refuse(name, "loss, lse and row_grad must be float32 [M]")
+    if begin.dtype != torch.int64 or begin.numel() != N + 1 or not begin.is_contiguous():
+        _refuse(name, "begin must be int64 [N + 1]")
+    return N, M, n_in, n_out, _rows(x.shape, x.stride(), name, "x"), stride[1] if n_out > 1 else n_in, stride[0] if N > 1 else 0
+
+
+def combo_grouped_cross_entropy_scratch_bytes(N: int, M: int, n_in: int, n_out: int, elem_bytes: int, grad_bytes: int = 0) -> int:
+    """Scratch of combo_grouped_cross_entropy, or, with the size of dw's elements, of its backward call."""
+    return int(load().combo_grouped_cross_entropy_scratch_bytes(N, M, n_in, n_out, elem_bytes, grad_bytes))
+
+
+def combo_grouped_cross_entropy(x, w, labels, loss, lse, begin, scratch, stream=None):
+    """Softmax cross entropy of x[m] W_w^T for every worker w's rows m (``begin``: device int64 [N + 1]), without
+    keeping the logits: x [M, n_in], w [N, n_out, n_in] (a view of flat parameter vectors) of x's type, labels int64
+    [M] (one outside the classes: the row has none); loss and lse (the logits' log-sum-exp, for the backward call)
+    float32 [M]."""
+    name = "combo_grouped_cross_entropy"
+    N, M, n_in, n_out, xp, wp, ws = _loss_args(name, x, w, labels, (loss, lse), begin)
+    _on_gpu(name, x, w, labels, loss, lse, begin, scratch)
+    _check(load().combo_grouped_cross_entropy(x.data_ptr(), xp, w.data_ptr(), wp, ws, _SIZES[x.dtype], labels.data_ptr(),
+                                              begin.data_ptr(), N, M, n_in, n_out, _ptr(loss), _ptr(lse), _ptr(scratch),
+                                              _bytes(scratch), _stream(stream)), name)
+    return loss
+
+
+def combo_grouped_cross_entropy_backward(x, w, labels, lse, row_grad, dx, dw, begin, scratch, stream=None):
+    """Gradients of sum_m row_grad[m] loss[m] (``row_grad`` None: of every worker's mean over its labelled rows): dx like
+    x, dw [N, n_out, n_in] (a view of flat gradient vectors) float32 or x's type, from the forward call's lse."""
+    name = "combo_grouped_cross_entropy_backward"
+    N, M, n_in, n_out, xp, wp, ws = _loss_args(name, x, w, labels, (lse, row_grad), begin)
+    if dx.shape != x.shape or dx.dtype != x.dtype:
+        _refuse(name, "dx must be like x")
+    if dw.shape != w.shape or dw.dtype not in _SIZES or (n_in > 1 and dw.stride(2) != 1):
+        _refuse(name, "dw must be [N, n_out, n_in], float32 or x's type, a row's elements neighbours")
+    dxp, stride = _rows(dx.shape, dx.stride(), name, "dx"), dw.stride()
+    _on_gpu(name, x, w, labels, lse, row_grad, dx, dw, begin, scratch)
+    _check(load().combo_grouped_cross_entropy_backward(
+        x.data_ptr(), xp, w.data_ptr(), wp, ws, _SIZES[x.dtype], labels.data_ptr(), _ptr(lse), _ptr(row_grad), dx.data_ptr(), dxp,
+        dw.data_ptr(), stride[1] if n_out > 1 else n_in, stride[0] if N > 1 else 0, _SIZES[dw.dtype], begin.data_ptr(), N, M, n_in,
+        n_out, _ptr(scratch), _bytes(scratch), _stream(stream)), name)
+    return dx
+
+
+def combo_dropout(x, residual, y, begin, p, seed, rnd, site=0, first_worker=0, stream=None):
+    """y = residual + x with every element dropped with probability p and the others scaled, x, y, residual (or None)
+    [M, n]; the mask follows from (seed, round, site, worker, place among the worker's rows), ``begin``: device int64
+    [N + 1], or None for one worker.  The backward pass is the same call on dy without a residual."""
+    name = "combo_dropout"
+    if len(x.shape) != 2 or x.dtype not in _SIZES:
+        _refuse(name, "x must be [M, n], float32 or bfloat16")
+    for t in (residual, y):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            _refuse(name, "y and residual must be like x")
+    if begin is not None and (begin.dtype != torch.int64 or begin.numel() < 2 or not begin.is_contiguous()):
+        _refuse(name, "begin must be int64 [N + 1]")
+    if not (0 <= seed < 1 << 64 and 0 <= rnd < 1 << 32 and 0 <= site < 1 << 32):
+        _refuse(name, "seed has 64 bits, round and site 32")
+    shape = x.shape
+    xp, yp = _rows(shape, x.stride(), name, "x"), _rows(shape, y.stride(), name, "y")
+    rp = 0 if residual is None else _rows(shape, residual.stride(), name, "residual")
+    _on_gpu(name, x, residual, y, begin)
+    _check(load().combo_dropout(x.data_ptr(), xp, _ptr(residual), rp, y.data_ptr(), yp, _SIZES[x.dtype], _ptr(begin),
+                                1 if begin is None else begin.numel() - 1, shape[0], shape[1], p, seed, rnd, site, first_worker,
+                                _stream(stream)), name)
+    return y
 
 
 def combo_device_status():

@@ -1,0 +1,201 @@
+"""combo_grouped_cross_entropy and its backward call against the definitions in 64 bits."""
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import paper_1908_07782_b200 as combo  # noqa: E402
+from loss_util import DEV, U, Case  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = [(F32, F32), (BF16, BF16), (BF16, F32)]
+IDS = ["f32", "bf16", "bf16-f32"]
+
+SHAPES = {
+    # the smallest, one class, one input
+    "one": dict(counts=[1], n_in=1, n_out=1),
+    "one class": dict(counts=[3, 2], n_in=9, n_out=1),
+    "one input": dict(counts=[5, 4], n_in=1, n_out=7),
+    # small classifiers, workers without rows, rows of no worker
+    "classifier": dict(counts=[1] * 8, n_in=256, n_out=10),
+    "ragged": dict(counts=[7, 0, 20, 1], n_in=33, n_out=13, lead=3, behind=2, mean=False),
+    "masked": dict(counts=[40, 9, 0, 64], n_in=64, n_out=21, keep=0.3),
+    # larger than a tile in each direction, odd widths
+    "wide": dict(counts=[130, 300], n_in=200, n_out=700),
+    "odd": dict(counts=[129, 65, 0, 257], n_in=77, n_out=301, keep=0.6, mean=False),
+    "classes": dict(counts=[70, 3], n_in=136, n_out=2500),
+    "long": dict(counts=[1100], n_in=520, n_out=513, keep=0.9),
+    "deep": dict(counts=[66], n_in=2300, n_out=260),
+    "many workers": dict(counts=[k % 4 for k in range(300)], n_in=72, n_out=300),
+    # places and pitches: 16-byte ones that are not dense, and others
+    "pitches": dict(counts=[33, 140], n_in=128, n_out=384, xp=8, wp=16, gap=64),
+    "off 16 bytes": dict(counts=[33, 140], n_in=128, n_out=384, xp=3, wp=1, gap=5, skew=1),
+}
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_values_and_gradients(shape, types):
+    c = Case(dtype=types[0], out=types[1], seed=len(shape), **SHAPES[shape])
+    c.forward()
+    c.check_forward()
+    lse = c.exact_lse()
+    outside = c.dx[~c.inside].clone()
+    c.backward(lse)
+    c.check_backward(lse)
+    assert torch.equal(c.dx[~c.inside], outside)
+    # nothing between the rows, nor between the workers' weights
+    for buf, t in ((c.dx_buf, c.dx), (c.dw_buf, c.dw)):
+        assert int((~buf.isnan()).sum()) == t.numel()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_row_has_a_label(dtype):
+    c = Case([5, 0, 70], 40, 300, dtype, keep=0.0)
+    c.forward()
+    assert (c.loss == 0).all() and (c.lse == 0).all()
+    c.backward(c.lse)
+    assert (c.dx == 0).all() and (c.dw == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_rows(dtype):
+    c = Case([0, 0], 40, 300, dtype)
+    c.forward()
+    c.backward(c.lse)
+    assert (c.dw == 0).all()
+
+
+@pytest.mark.parametrize("n_out", [20, 600])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_logits(dtype, n_out):
+    """Logits of a thousand and more: only differences are exponentiated."""
+    c = Case([40, 130], 64, n_out, dtype, spread=400.0)
+    c.forward()
+    c.check_forward()
+    assert float(c.lse.max()) > 500
+    lse = c.lse.clone()
+    c.backward(lse)
+    c.check_backward(lse)
+
+
+@pytest.mark.parametrize("n_out", [12, 520])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_nan_and_infinity_stay_in_their_row_and_worker(dtype, n_out):
+    c = Case([20, 150, 9], 48, n_out, dtype)
+    good = Case([20, 150, 9], 48, n_out, dtype)
+    for k in (c, good):
+        k.forward()
+    good.backward(good.lse)
+    c.x[25, 3] = float("nan")
+    c.x[120, 5] = float("inf")
+    c.w[2, 7, 1] = float("nan")
+    c.forward()
+    bad = torch.zeros(c.M, dtype=torch.bool, device=DEV)
+    bad[[25, 120]] = True
+    bad[170:] = True
+    assert c.loss[bad].isnan().all() and torch.equal(c.loss[~bad], good.loss[~bad])
+    c.backward(c.lse)
+    assert c.dx[bad].isnan().any(1).all() and torch.equal(c.dx[~bad], good.dx[~bad])
+    assert torch.equal(c.dw[0], good.dw[0]) and c.dw[1].isnan().any() and c.dw[2].isnan().any()
+
+
+def test_a_class_at_minus_infinity_is_none():
+    """Weights of -inf against a positive input: the class has probability zero."""
+    c = Case([30], 16, 400, BF16)
+    c.x[:, 0] = 1.0
+    c.w[0, 399, 0] = float("-inf")
+    c.labels[:] = 5
+    c.forward()
+    w = c.w[0, :399].double()
+    want = torch.logsumexp(c.x.double() @ w.T, 1)
+    assert (c.lse.double() - want).abs().max() < 1e-4
+    assert not c.loss.isnan().any()
+
+
+@pytest.mark.parametrize("counts,n_in,n_out", [([6, 0, 9], 24, 11), ([40, 130], 96, 520)])
+def test_gradients_against_differences(counts, n_in, n_out):
+    c = Case(counts, n_in, n_out, F32, mean=False, keep=0.7)
+    c.forward()
+    c.backward(c.lse)
+    g = torch.Generator().manual_seed(3)
+    ux, uw = torch.randn(c.M, n_in, generator=g).to(DEV), torch.randn(c.w.shape, generator=g).to(DEV) / n_in ** 0.5
+    x0, w0, h = c.x.clone(), c.w.clone(), 2.0 ** -7
+    for dx, dw in ((ux, None), (None, uw)):
+        losses = []
+        for sign in (1, -1):
+            c.x.copy_(x0 if dx is None else x0 + sign * h * dx)
+            c.w.copy_(w0 if dw is None else w0 + sign * h * dw)
+            c.forward()
+            losses.append(c.loss.double())
+        c.x.copy_(x0)
+        c.w.copy_(w0)
+        got = ((losses[0] - losses[1]) * c.row_grad.double() * c.has).sum() / (2 * h)
+        want = (c.dx.double() * dx.double())[c.has].sum() if dw is None else (c.dw.double() * dw.double()).sum()
+        # the third derivative of a log-sum-exp is a third central moment, R^3 q (1 - q) (1 - 2 q) for two values R apart, at most
+        # R^3 / (6 sqrt(3)) over the range R of the logits' change; float inputs moved by h are off by half a unit; the losses'
+        # own error
+        tol = 0.0
+        for w in range(c.N):
+            rows, x, wt, z, dz = c.logits(w)
+            if len(rows):
+                move = dx[rows].double() @ wt.T if dw is None else x @ dw[w].double().T
+                spread = move.max(1).values - move.min(1).values
+                error = 4 * dz.max(1).values + (200 + c.V / 8) * U * 2
+                tol += float((c.row_grad[rows].double().abs() * (h * h / 6 * spread ** 3 / (6 * 3 ** 0.5) + error / h)).sum())
+        assert abs(float(got - want)) <= tol and tol < 0.25 * abs(float(want)) + 1.0
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_same_bits_from_run_to_run_and_from_a_graph(types):
+    c = Case([300, 20, 0, 410], 136, 1000, types[0], types[1], keep=0.8)
+    f, b = c.scratch(False), c.scratch(True)
+    c.forward(f)
+    c.backward(c.lse, b)
+    first = [t.clone() for t in (c.loss, c.lse, c.dx, c.dw)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            c.forward(f)
+            c.backward(c.lse, b)
+    for _ in range(3):
+        for t in (c.loss, c.lse, c.dx, c.dw):
+            t.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, k) for t, k in zip((c.loss, c.lse, c.dx, c.dw), first))
+
+
+def test_two_calls_at_once():
+    a, b = Case([500, 300], 264, 1500, BF16, seed=1), Case([200, 610], 264, 1500, BF16, seed=2)
+    for c in (a, b):
+        c.forward()
+        c.backward(c.lse)
+    torch.cuda.synchronize()
+    want = [t.clone() for c in (a, b) for t in (c.loss, c.dx, c.dw)]
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    pa, pb = [(c.scratch(False), c.scratch(True)) for c in (a, b)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s, p in ((a, sa, pa), (b, sb, pb)):
+            with torch.cuda.stream(s):
+                c.forward(p[0])
+                c.backward(c.lse, p[1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, k) for t, k in zip([t for c in (a, b) for t in (c.loss, c.dx, c.dw)], want))
+
+
+def test_a_view_beside_the_input():
+    """x and dx as columns of one array."""
+    c = Case([40, 30], 32, 300, F32)
+    c.backward(c.exact_lse())
+    want = c.dx.clone()
+    wide = torch.zeros(c.M, 64, device=DEV)
+    wide[:, :32] = c.x
+    combo.combo_grouped_cross_entropy_backward(wide[:, :32], c.w, c.labels, c.exact_lse(), None, wide[:, 32:], c.dw, c.begin, c.scratch(True))
+    assert torch.equal(wide[:, 32:], want)
