@@ -16,7 +16,7 @@ HEADERS = {
     "group_norm.cu": ("host_common.h", "step_common.cuh"),
     "grouped_linear.cu": ("host_common.h", "step_common.cuh", "tensor_core.cuh"),
     "grad_clip.cu": ("host_common.h", "step_common.cuh"),
-    "cross_entropy.cu": ("host_common.h", "step_common.cuh"),
+    "cross_entropy.cu": ("host_common.h", "step_common.cuh", "tensor_core.cuh", "cross_entropy_tensor.cuh"),
     "dropout.cu": ("host_common.h", "step_common.cuh"),
 }
 SOURCES = [os.path.join(CSRC, f) for f in HEADERS]

@@ -1228,6 +1228,9 @@ combo_status combo_device_status(void) {
         return COMBO_ERR_DEVICE_TIMEOUT;
     }
     if ((e = combo_host::grouped_linear_status(&v)) != cudaSuccess) return cuda_fail(e, "grouped product status");
+    int u = 0;
+    if ((e = combo_host::cross_entropy_status(&u)) != cudaSuccess) return cuda_fail(e, "cross entropy status");
+    if (v == 0) v = u;
     if (v != 0) {
         snprintf(t_cuda_err, sizeof(t_cuda_err), "bounded wait gave up at site %d", v);
         return COMBO_ERR_DEVICE_TIMEOUT;

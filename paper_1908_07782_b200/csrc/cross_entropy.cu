@@ -6,6 +6,7 @@
 
 #include "host_common.h"
 #include "step_common.cuh"
+#include "cross_entropy_tensor.cuh"
 
 namespace {
 
@@ -291,6 +292,255 @@ template <int EB, bool VEC> cudaError_t launch_few(const Loss& p, int grad_bytes
     return cudaGetLastError();
 }
 
+// ---------------------------------------------------------------- packing of rows and weights for the tensor cores
+using namespace combo_loss;
+
+// Where things lie in scratch.
+struct Packed {
+    int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 1]; [cap]; [cap]
+    float *lse, *g, *own;                                      // [cap]
+    unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][piece][kp]; of [cap][d_pitch]
+    float2* part;
+    float* dx;
+    long long cap;
+    int kp, height;                                            // inputs, up to a multiple of 64; rows of a tile
+};
+
+constexpr int kCountThreads = 1024, kCountRows = 8;
+
+// A worker's labelled rows, in order: how many, and which.  The others' results are zeros.
+__global__ void __launch_bounds__(kCountThreads) k_count(const Loss p, const Packed s) {
+    __shared__ int sums[33];
+    const int w = blockIdx.x, t = threadIdx.x, lane = t & 31;
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
+    long long r0, r1;
+    rows_of(p, w, r0, r1);
+    int before = 0;
+    for (long long i0 = r0; i0 < r1; i0 += kCountThreads * kCountRows) {
+        const long long i = i0 + t * kCountRows;
+        unsigned has = 0;
+#pragma unroll
+        for (int e = 0; e < kCountRows; ++e) {
+            const int64_t label = i + e < r1 ? p.labels[i + e] : -1;
+            has |= (unsigned)(label >= 0 && label < p.V) << e;
+        }
+        const int mine = __popc(has);
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) sums[t >> 5] = upto;
+        __syncthreads();
+        if (t < 32) {
+            const int v = sums[t];
+            int u = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int k = __shfl_up_sync(0xffffffffu, u, o);
+                if (lane >= o) u += k;
+            }
+            sums[t] = u - v;
+            if (t == 31) sums[32] = u;
+        }
+        __syncthreads();
+        int at = before + sums[t >> 5] + upto - mine;
+#pragma unroll
+        for (int e = 0; e < kCountRows; ++e) {
+            if (has >> e & 1u) {
+                s.list[r0 + at++] = (int)(i + e);
+            } else if (i + e < r1) {
+                if (p.loss) p.loss[i + e] = p.lse[i + e] = 0.0f;
+                else s.pos[i + e] = -1;
+            }
+        }
+        before += sums[32];
+        __syncthreads();
+    }
+    if (t == 0) s.count[w] = before;
+}
+
+// Eight neighbours of a line of `left` elements, zeros behind.
+template <int EB> __device__ __forceinline__ void load8(const unsigned char* q, int left, bool vec, float (&v)[8]) {
+    if (vec && left >= 8) {
+        if constexpr (EB == 2) {
+            Elem<2>::unpack(*reinterpret_cast<const uint4*>(q), v);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 f = *reinterpret_cast<const float4*>(q + h * 16);
+                v[4 * h] = f.x; v[4 * h + 1] = f.y; v[4 * h + 2] = f.z; v[4 * h + 3] = f.w;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? Elem<EB>::get(q + e * EB) : 0.0f;
+    }
+}
+// Writes them as bfloat16 planes: each holds what the ones before leave, rounded; towards zero where rounding would overflow.
+template <int PLANES> __device__ __forceinline__ void store_planes(unsigned short* to, long long plane, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {
+        uint32_t o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e] = combo_step::pack_bf16(v[2 * e], v[2 * e + 1]);
+            if (PLANES > 1) {
+                if (fabsf(v[2 * e]) > 3.3895314e38f && fabsf(v[2 * e]) <= 3.4028235e38f) o[e] = (o[e] & 0xffff0000u) | __float_as_uint(v[2 * e]) >> 16;
+                if (fabsf(v[2 * e + 1]) > 3.3895314e38f && fabsf(v[2 * e + 1]) <= 3.4028235e38f) o[e] = (o[e] & 0xffffu) | (__float_as_uint(v[2 * e + 1]) & 0xffff0000u);
+                v[2 * e] -= combo_step::widen_lo(o[e]);
+                v[2 * e + 1] -= combo_step::widen_hi(o[e]);
+            }
+        }
+        *reinterpret_cast<uint4*>(to + k * plane) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+constexpr int kPackRows = 16;
+
+// Packs the labelled rows, kPackRows to a CTA; the first CTA leaves the tables of where the workers' rows lie.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss p, const Packed s, int vec) {
+    __shared__ int begins[COMBO_MAX_WORKERS + 1];              // packed rows
+    __shared__ int sums[kThreads + 1];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
+    const int per = (p.N + kThreads - 1) / kThreads;
+    const auto scan = [&](int unit, int* to, int scale) {      // ascending sums of ceil(count / unit) * scale
+        int mine = 0;
+        for (int w = t * per; w < min((t + 1) * per, p.N); ++w) mine += (s.count[w] + unit - 1) / unit;
+        sums[t] = mine;
+        __syncthreads();
+        for (int o = 1; o < kThreads; o <<= 1) {
+            const int v = t >= o ? sums[t - o] : 0;
+            __syncthreads();
+            sums[t] += v;
+            __syncthreads();
+        }
+        int at = sums[t] - mine;
+        for (int w = t * per; w < min((t + 1) * per, p.N); ++w) {
+            to[w] = at * scale;
+            at += (s.count[w] + unit - 1) / unit;
+        }
+        if (t == kThreads - 1) to[p.N] = sums[t] * scale;
+        __syncthreads();
+    };
+    scan(kStep, begins, kStep);
+    if (blockIdx.x == 0) {
+        for (int w = t; w <= p.N; w += kThreads) s.row0[w] = begins[w];
+        scan(s.height, s.tiles, 1);
+    }
+    const int total = begins[p.N];
+    for (int j = blockIdx.x * kPackRows + warp; j < min((int)(blockIdx.x + 1) * kPackRows, total); j += kWarps) {
+        int lo = 0, hi = p.N - 1;                              // the last w with begins[w] <= j
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (begins[mid] <= j) lo = mid;
+            else hi = mid - 1;
+        }
+        long long r0, r1;
+        rows_of(p, lo, r0, r1);
+        const int rank = j - begins[lo], count = s.count[lo];
+        const int from = rank < count ? s.list[r0 + rank] : -1;
+        if (lane == 0) {
+            s.src[j] = from;
+            s.label[j] = from >= 0 ? (int)p.labels[from] : -1;
+            if (!p.loss && from >= 0) {
+                s.pos[from] = j;
+                s.lse[j] = p.lse_in[from];
+                s.g[j] = p.row_grad ? p.row_grad[from] : 1.0f / (float)count;
+            }
+        }
+        unsigned short* to = s.x + (long long)j * s.kp;
+        for (int k = lane * 8; k < s.kp; k += 256) {
+            float v[8];
+            load8<EB>(p.x + (from * p.x_pitch + k) * EB, from >= 0 ? p.K - k : 0, vec, v);
+            store_planes<EB == 4 ? 3 : 1>(to + k, s.cap * s.kp, v);
+        }
+    }
+}
+
+// The weights of `classes` classes from v0 on as planes, zeros where there are none.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Loss p, unsigned short* out, int v0, int classes, int kp, int vec) {
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
+    const int lots = kp / 8;
+    const long long all = (long long)p.N * classes * lots;
+    for (long long o = blockIdx.x * (long long)kThreads + threadIdx.x; o < all; o += (long long)gridDim.x * kThreads) {
+        const long long line = o / lots;
+        const int k = (int)(o - line * lots) * 8, w = (int)(line / classes), v = v0 + (int)(line - (long long)w * classes);
+        float f[8];
+        load8<EB>(p.w + (w * p.w_stride + v * p.w_pitch + k) * EB, v < p.V ? p.K - k : 0, vec, f);
+        store_planes<EB == 4 ? 3 : 1>(out + o * 8, all * 8, f);
+    }
+}
+
+// A row's log-sum-exp from its pieces, 32 rows to a CTA, and its loss.
+__global__ void __launch_bounds__(kThreads) k_finish(const Loss p, const Packed s, int pieces) {
+    __shared__ float sm[2][kWarps][32];
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
+    const int from = j < s.row0[p.N] ? s.src[j] : -1;
+    float m = -INFINITY, sum = 0.0f;
+    if (from >= 0) {
+#pragma unroll 4
+        for (int i = warp; i < pieces; i += kWarps) {
+            const float2 v = s.part[i * s.cap + j];
+            join(m, sum, v.x, v.y);
+        }
+    }
+    sm[0][warp][lane] = m;
+    sm[1][warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && from >= 0) {
+        for (int k = 1; k < kWarps; ++k) join(m, sum, sm[0][k][lane], sm[1][k][lane]);
+        const float lse = m + logf(sum);
+        p.lse[from] = lse;
+        p.loss[from] = lse - s.own[j];
+    }
+}
+
+// The rows' gradients to their places: the parts of the sums added up, zeros for rows without a label.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const Loss p, const Packed s, const Pass q, int vec) {
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
+    const int splits = splits_of(q), lots = s.kp / 8;
+    const long long total = q.row0[q.N], a = min(max((long long)p.begin[0], 0LL), p.M), b = min(max((long long)p.begin[p.N], a), p.M);
+    for (long long o = blockIdx.x * (long long)kThreads + threadIdx.x; o < (b - a) * lots; o += (long long)gridDim.x * kThreads) {
+        const long long row = o / lots, m = a + row;
+        const int k = (int)(o - row * lots) * 8, left = p.K - k;
+        if (left <= 0) continue;
+        const int j = s.pos[m];
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = 0.0f;
+        if (j >= 0) {
+            for (int i = 0; i < splits; ++i) {
+                uint32_t v[8];
+                load32(q.dx + (i * total + j) * q.dx_pitch + k, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(v[e]);
+            }
+        }
+        unsigned char* to = p.dx + (m * p.dx_pitch + k) * EB;
+        if (vec && left >= 8) {
+            if constexpr (EB == 2) {
+                *reinterpret_cast<uint4*>(to) = Elem<2>::pack(f);
+            } else {
+                reinterpret_cast<float4*>(to)[0] = make_float4(f[0], f[1], f[2], f[3]);
+                reinterpret_cast<float4*>(to)[1] = make_float4(f[4], f[5], f[6], f[7]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) Elem<EB>::put(to + e * EB, f[e]);
+        }
+    }
+}
+
 // ---------------------------------------------------------------- host
 bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int grad_bytes) {
     return (elem_bytes == 2 || elem_bytes == 4) && (grad_bytes == 0 || grad_bytes == 4 || (grad_bytes == 2 && elem_bytes == 2)) && N >= 1 &&
@@ -298,16 +548,228 @@ bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int
            n_out <= COMBO_LINEAR_MAX_WIDTH;
 }
 
-size_t scratch_needed(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int grad_bytes) {
-    (void)N; (void)n_in; (void)elem_bytes;
-    return 256 + (grad_bytes ? (size_t)M * n_out * 4 : 0);
+constexpr int kSms = 148;
+constexpr size_t kPieceBytes = 256u << 20;       // aimed at for a piece of classes: d, and the weights' planes
+
+// How a call is computed, by its sizes alone.
+struct Plan {
+    bool few;
+    int cg, planes, d_planes, kp;                // of x and w; of d
+    int v_width, k_width, unit;                  // tiles along the classes, along the inputs; pieces are multiples of `unit`
+    long long cap;
+    size_t x, part, dx, region, room, total;     // places in scratch; bytes of the region for pieces
+};
+
+size_t up(size_t n, size_t unit) { return (n + unit - 1) / unit * unit; }
+
+int even_width(int64_t n, int most, int unit) {
+    const int64_t tiles = (n + most - 1) / most;
+    return (int)up((size_t)((n + tiles - 1) / tiles), unit);
+}
+
+// Bytes of a piece of so many classes.
+size_t piece_bytes(const Plan& a, int N, size_t classes, bool back, bool direct) {
+    return (back ? up(classes * a.cap * a.d_planes * 2, 256) : 0) + (direct ? 0 : up(classes * N * a.kp * a.planes * 2, 256));
+}
+
+Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_bytes) {
+    Plan a = {};
+    const bool back = grad_bytes != 0;
+    a.few = M == 0 || (V * K <= (1 << 17) && M * V <= (1 << 24));
+    if (a.few) {
+        a.total = 256 + (back ? (size_t)M * V * 4 : 0);
+        return a;
+    }
+    a.cg = M / N > 128 ? 2 : 1;
+    a.planes = elem_bytes == 4 ? 3 : 1;
+    a.d_planes = elem_bytes == 4 ? 3 : grad_bytes == 4 ? 2 : 1;
+    a.kp = (int)up(K, 64);
+    const int most = a.planes == 3 && a.cg == 1 ? 128 : 256;
+    a.v_width = even_width(V, most, 64 * a.cg);
+    a.k_width = even_width(K, most, 64 * a.cg);
+    if (V > 1024) a.v_width = most;
+    a.unit = a.v_width;
+    a.cap = (long long)up(M + 63 * (N < M ? N : M), 64);
+    const size_t cap = (size_t)a.cap;
+    size_t at = up((size_t)N * 4, 256) + 2 * up((size_t)M * 4, 256) + 2 * up((size_t)(N + 1) * 4, 256) + 5 * up(cap * 4, 256);
+    a.x = at;
+    at += up(cap * a.kp * a.planes * 2, 256);
+    a.part = at;
+    if (!back) {
+        at += up(2 * up(V, a.v_width) / a.v_width * cap * 8, 256);
+    } else {
+        const size_t wt = up(K, a.k_width) / a.k_width, split_rows = (size_t)kMaxTurns * (kSms / a.cg) / wt * 128 * a.cg;
+        a.dx = at;
+        at += up((cap > split_rows ? cap : split_rows) * wt * a.k_width * 4, 256);
+    }
+    a.region = at;
+    const size_t whole = piece_bytes(a, N, up(V, a.unit), back, false), least = piece_bytes(a, N, a.unit, back, false);
+    a.room = whole < kPieceBytes ? whole : least > kPieceBytes ? least : kPieceBytes;
+    a.total = at + a.room;
+    return a;
+}
+
+bool map_of(CUtensorMap* map, void* base, int rank, const long long* dims, const long long* strides) {
+    cuuint64_t d[4], s[3];
+    const cuuint32_t box[4] = {kStep, 64, 1, 1}, ones[4] = {1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
+    for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * 2;
+    return combo_host::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, base, d, s, box, ones, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass q, const Maps& maps, long long tiles, int sms, int smem_optin, cudaStream_t st) {
+    static uint64_t allowed;
+    auto kern = k_loss<CG, MODE, PA, PB, OB>;
+    const int turn = MODE == kWeights && !q.vec ? kOutWarps * kTurn : 0, most = smem_optin - kStaticSmem;
+    q.stage_bytes = (PA * 2 + PB * (q.width / CG / 64)) * kBlock;
+    q.stages = (most - 1024 - turn) / q.stage_bytes;
+    if (q.stages > kMaxStages) q.stages = kMaxStages;
+    cudaError_t e = combo_host::allow_smem(kern, most, &allowed);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles < sms / CG ? tiles : sms / CG) * CG);
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = 1024 + (size_t)q.stages * q.stage_bytes + turn;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, q, maps);
+}
+
+// EB: bytes of the inputs; GB: of dW (0: forward).
+template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Loss& p, unsigned char* scratch, int sms, int smem_optin, cudaStream_t st) {
+    constexpr int P = EB == 4 ? 3 : 1, D = EB == 4 ? 3 : GB == 4 ? 2 : 1;
+    constexpr bool kBack = GB != 0;
+    const auto vec_ok = [](const void* b, long long pitch, long long stride, int eb) {
+        return combo_host::aligned_to(b, 16) && pitch * eb % 16 == 0 && stride * eb % 16 == 0;
+    };
+    Packed s = {};
+    s.cap = a.cap;
+    s.kp = a.kp;
+    s.height = 128 * CG;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { unsigned char* r = scratch + at; at += up(bytes, 256); return r; };
+    const size_t cap = (size_t)a.cap;
+    s.count = reinterpret_cast<int*>(take((size_t)p.N * 4));
+    s.list = reinterpret_cast<int*>(take((size_t)p.M * 4));
+    s.pos = reinterpret_cast<int*>(take((size_t)p.M * 4));
+    s.row0 = reinterpret_cast<int*>(take((size_t)(p.N + 1) * 4));
+    s.tiles = reinterpret_cast<int*>(take((size_t)(p.N + 1) * 4));
+    s.src = reinterpret_cast<int*>(take(cap * 4));
+    s.label = reinterpret_cast<int*>(take(cap * 4));
+    s.lse = reinterpret_cast<float*>(take(cap * 4));
+    s.g = reinterpret_cast<float*>(take(cap * 4));
+    s.own = reinterpret_cast<float*>(take(cap * 4));
+    s.x = reinterpret_cast<unsigned short*>(scratch + a.x);
+    s.part = reinterpret_cast<float2*>(scratch + a.part);
+    s.dx = reinterpret_cast<float*>(scratch + a.dx);
+
+    // bfloat16 weights on 16-byte boundaries are read where they lie
+    const bool w_vec = vec_ok(p.w, p.w_pitch, p.w_stride, EB), direct = EB == 2 && w_vec && p.w_pitch < (1LL << 36) && p.w_stride < (1LL << 36);
+    int piece = (int)up(p.V, a.unit);
+    if (!(direct && !kBack))
+        while (piece > a.unit && piece_bytes(a, p.N, piece, kBack, direct) > a.room) piece = (int)up(piece / 2, a.unit);
+    s.d = reinterpret_cast<unsigned short*>(scratch + a.region);
+    s.w = s.d + (kBack ? up((size_t)piece * cap * D * 2, 256) / 2 : 0);
+
+    cudaError_t e = combo_host::launch_after(k_count, dim3(p.N), dim3(kCountThreads), 0, st, p, s);
+    if (e != cudaSuccess) return e;
+    e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((cap + kPackRows - 1) / kPackRows)), dim3(kThreads), 0, st, p, s,
+                                 (int)vec_ok(p.x, p.x_pitch, 0, EB));
+    if (e != cudaSuccess) return e;
+
+    CUtensorMap mx, mw, md;
+    const long long xd[3] = {a.kp, a.cap, P}, xs[2] = {a.kp, a.cap * a.kp};
+    const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : piece, p.N, direct ? 1 : P};
+    const long long lines = (long long)piece * a.kp;
+    const long long ws[3] = {direct ? p.w_pitch : a.kp, direct ? (p.N > 1 ? p.w_stride : 8) : lines, direct ? 8 : lines * p.N};
+    const long long dd[3] = {piece, a.cap, D}, ds[2] = {piece, a.cap * piece};
+    if (!map_of(&mx, s.x, 3, xd, xs) || !map_of(&mw, direct ? const_cast<unsigned char*>(p.w) : reinterpret_cast<unsigned char*>(s.w), 4, wd, ws) ||
+        (kBack && !map_of(&md, s.d, 3, dd, ds)))
+        return cudaErrorInvalidValue;
+
+    Pass q = {};
+    q.row0 = s.row0;
+    q.tiles = s.tiles;
+    q.N = p.N;
+    q.V = p.V;
+    q.K = p.K;
+    q.clusters = kSms / CG;
+    q.row_cap = a.cap;
+    q.d_pitch = piece;
+    q.d_plane = a.cap * piece;
+    q.label = s.label;
+    q.lse = s.lse;
+    q.g = s.g;
+    q.part = s.part;
+    q.own = s.own;
+    q.d = s.d;
+    q.dx = s.dx;
+    q.dw = p.dw;
+    q.dw_pitch = p.dw_pitch;
+    q.dw_stride = p.dw_stride;
+    q.part_steps = EB == 4 ? 1 : 16;
+    const int kt = (p.K + a.k_width - 1) / a.k_width;
+    q.dx_pitch = kt * a.k_width;
+    q.split_steps = (int)(piece < up(p.V, 64) ? piece : up(p.V, 64)) / kStep;
+    const long long row_tiles = p.M / s.height + (p.N < p.M ? p.N : p.M);          // at most
+    for (int v0 = 0; v0 < p.V; v0 += piece) {
+        const int classes = p.V - v0 < piece ? p.V - v0 : piece;
+        if (!direct) {
+            const long long lots = (long long)p.N * piece * a.kp / 8, grid = (lots + kThreads - 1) / kThreads;
+            e = combo_host::launch_after(k_planes<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s.w, v0, piece, a.kp, (int)w_vec);
+            if (e != cudaSuccess) return e;
+        }
+        q.v0 = v0;
+        q.v_end = v0 + classes;
+        q.w_row = direct ? v0 : 0;
+        q.width = a.v_width;
+        q.wt = (classes + a.v_width - 1) / a.v_width;
+        q.steps = a.kp / kStep;
+        const Maps logits_of = {mx, mw};
+        e = kBack ? launch_loss<CG, kGrad, P, P, D>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
+                  : launch_loss<CG, kStats, P, P, 1>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
+        if (e != cudaSuccess) return e;
+        if constexpr (kBack) {
+            q.width = a.k_width;
+            q.wt = kt;
+            q.steps = (classes + kStep - 1) / kStep;
+            q.add = v0 > 0;
+            // bfloat16 rows take the first plane of d: the others are below their rounding
+            e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
+            if (e != cudaSuccess) return e;
+            q.ht = (classes + s.height - 1) / s.height;
+            q.vec = vec_ok(p.dw, p.dw_pitch, p.dw_stride, GB) && p.K * GB % 16 == 0
+                        ? combo_host::aligned_to(p.dw, 32) && p.dw_pitch * GB % 32 == 0 && p.dw_stride * GB % 32 == 0 ? 32 : 16
+                        : 0;
+            e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{md, mx}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    if (!kBack) return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(kThreads), 0, st, p, s, 2 * ((p.V + a.v_width - 1) / a.v_width));
+    q.width = a.k_width;
+    q.wt = kt;
+    const long long lots = (long long)p.M * a.kp / 8, grid = (lots + kThreads - 1) / kThreads;
+    return combo_host::launch_after(k_rows_out<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s, q,
+                                    (int)vec_ok(p.dx, p.dx_pitch, 0, EB));
+}
+
+template <int CG> cudaError_t launch_tensor(const Plan& a, const Loss& p, int elem_bytes, int grad_bytes, void* scratch, int sms, int smem_optin, cudaStream_t st) {
+    unsigned char* b = static_cast<unsigned char*>(scratch);
+    if (elem_bytes == 4) return grad_bytes ? run_tensor<CG, 4, 4>(a, p, b, sms, smem_optin, st) : run_tensor<CG, 4, 0>(a, p, b, sms, smem_optin, st);
+    if (grad_bytes == 4) return run_tensor<CG, 2, 4>(a, p, b, sms, smem_optin, st);
+    return grad_bytes ? run_tensor<CG, 2, 2>(a, p, b, sms, smem_optin, st) : run_tensor<CG, 2, 0>(a, p, b, sms, smem_optin, st);
 }
 
 combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in, int64_t n_out, void* scratch, size_t scratch_bytes, void* stream) {
     if (!sizes_ok(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes)) return COMBO_ERR_INVALID_ARG;
     const bool back = grad_bytes != 0;
     if (!p.begin || !combo_host::aligned_to(p.begin, 8)) return COMBO_ERR_INVALID_ARG;
-    if (!scratch || !combo_host::aligned_to(scratch, 256) || scratch_bytes < scratch_needed(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes))
+    if (!scratch || !combo_host::aligned_to(scratch, 256) || scratch_bytes < plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes).total)
         return COMBO_ERR_INVALID_ARG;
     if (p.M > 0) {
         if (!p.x || !p.labels || p.x_pitch < n_in || p.x_pitch > (1LL << 40) / p.M) return COMBO_ERR_INVALID_ARG;
@@ -345,13 +807,19 @@ combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in,
     if (p.M == 0 && !back) return COMBO_OK;
     p.K = (int)n_in;
     p.V = (int)n_out;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e;
+    const Plan plan = plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes);
+    if (!plan.few) {
+        e = plan.cg == 2 ? launch_tensor<2>(plan, p, elem_bytes, grad_bytes, scratch, sms, smem, st)
+                         : launch_tensor<1>(plan, p, elem_bytes, grad_bytes, scratch, sms, smem, st);
+        return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "cross entropy launch");
+    }
     p.d = static_cast<float*>(scratch);
     const auto vec_ok = [&](const void* a, int64_t pitch, int64_t stride) {
         return combo_host::aligned_to(a, 16) && pitch * elem_bytes % 16 == 0 && stride * elem_bytes % 16 == 0;
     };
     const bool vec = vec_ok(p.x, p.x_pitch, 0) && vec_ok(p.w, p.w_pitch, p.w_stride);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
     if (elem_bytes == 4) e = vec ? launch_few<4, true>(p, grad_bytes, st) : launch_few<4, false>(p, grad_bytes, st);
     else e = vec ? launch_few<2, true>(p, grad_bytes, st) : launch_few<2, false>(p, grad_bytes, st);
     return e == cudaSuccess ? COMBO_OK : combo_host::fail(e, "cross entropy launch");
@@ -359,10 +827,21 @@ combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in,
 
 }  // namespace
 
+namespace combo_host {
+
+cudaError_t cross_entropy_status(int* code) {
+    const int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(code, combo_loss::g_loss_status, sizeof(int));
+    if (e == cudaSuccess && *code != 0) e = cudaMemcpyToSymbol(combo_loss::g_loss_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace combo_host
+
 extern "C" {
 
 size_t combo_grouped_cross_entropy_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int grad_bytes) {
-    return sizes_ok(N, M, n_in, n_out, elem_bytes, grad_bytes) ? scratch_needed(N, M, n_in, n_out, elem_bytes, grad_bytes) : 0;
+    return sizes_ok(N, M, n_in, n_out, elem_bytes, grad_bytes) ? plan_of(N, M, n_in, n_out, elem_bytes, grad_bytes).total : 0;
 }
 
 combo_status combo_grouped_cross_entropy(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch, int64_t w_stride, int elem_bytes,

@@ -18,6 +18,8 @@ enum StepPath { kPathNone = 0, kPathMultiplyAdd = 1, kPathTensor = 2, kPathTenso
 void set_step_path(StepPath path);
 // Status word of the grouped products' kernels (see combo_device_status): reads it, and clears it if it is set.
 cudaError_t grouped_linear_status(int* code);
+// The same of the cross entropy's kernels.
+cudaError_t cross_entropy_status(int* code);
 // cuTensorMapEncodeTiled without interleaving, out-of-bounds elements read as zero; false (and a text for
 // combo_last_cuda_error()) if it is missing or refuses.
 bool encode_tiled(CUtensorMap* map, CUtensorMapDataType type, int rank, void* base, const cuuint64_t* dims, const cuuint64_t* strides,
