@@ -297,7 +297,7 @@ using namespace combo_loss;
 
 // Where things lie in scratch.
 struct Packed {
-    int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 1]; [cap]; [cap]
+    int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 1]; [cap]: forward the row, backward the worker; [cap]
     float *lse, *g, *own;                                      // [cap]
     unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][piece][kp]; of [cap][d_pitch]
     float2* part;
@@ -402,8 +402,8 @@ constexpr int kPackRows = 16;
 
 // Packs the labelled rows, kPackRows to a CTA; the first CTA leaves the tables of where the workers' rows lie.
 template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss p, const Packed s, int vec) {
-    __shared__ int begins[COMBO_MAX_WORKERS + 1];              // packed rows
-    __shared__ int sums[kThreads + 1];
+    extern __shared__ int begins[];                            // packed rows [N + 1]
+    __shared__ int sums[kWarps];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     combo_step::pdl_release();
     combo_step::pdl_wait();
@@ -411,20 +411,23 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
     const auto scan = [&](int unit, int* to, int scale) {      // ascending sums of ceil(count / unit) * scale
         int mine = 0;
         for (int w = t * per; w < min((t + 1) * per, p.N); ++w) mine += (s.count[w] + unit - 1) / unit;
-        sums[t] = mine;
-        __syncthreads();
-        for (int o = 1; o < kThreads; o <<= 1) {
-            const int v = t >= o ? sums[t - o] : 0;
-            __syncthreads();
-            sums[t] += v;
-            __syncthreads();
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
         }
-        int at = sums[t] - mine;
+        __syncthreads();
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+        int at = upto - mine;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) at += k < warp ? sums[k] : 0;
         for (int w = t * per; w < min((t + 1) * per, p.N); ++w) {
             to[w] = at * scale;
             at += (s.count[w] + unit - 1) / unit;
         }
-        if (t == kThreads - 1) to[p.N] = sums[t] * scale;
+        if (t == kThreads - 1) to[p.N] = at * scale;
         __syncthreads();
     };
     scan(kStep, begins, kStep);
@@ -445,7 +448,7 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
         const int rank = j - begins[lo], count = s.count[lo];
         const int from = rank < count ? s.list[r0 + rank] : -1;
         if (lane == 0) {
-            s.src[j] = from;
+            s.src[j] = p.loss ? from : lo;
             s.label[j] = from >= 0 ? (int)p.labels[from] : -1;
             if (!p.loss && from >= 0) {
                 s.pos[from] = j;
@@ -477,34 +480,51 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Los
     }
 }
 
-// A row's log-sum-exp from its pieces, 32 rows to a CTA, and its loss.
-__global__ void __launch_bounds__(kThreads) k_finish(const Loss p, const Packed s, int pieces) {
-    __shared__ float sm[2][kWarps][32];
+// A row's log-sum-exp from its pieces, 32 rows to a CTA, and its loss: a thread takes eight pieces at a time, so that their loads
+// and exponentials do not wait for one another.
+constexpr int kFinishWarps = 32;
+__global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, const Packed s, int pieces) {
+    __shared__ float sm[2][kFinishWarps][32];
     combo_step::pdl_release();
     combo_step::pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
-    const int from = j < s.row0[p.N] ? s.src[j] : -1;
+    if (blockIdx.x * 32 >= s.row0[p.N]) return;
+    const int from = s.src[j];
     float m = -INFINITY, sum = 0.0f;
     if (from >= 0) {
-#pragma unroll 4
-        for (int i = warp; i < pieces; i += kWarps) {
-            const float2 v = s.part[i * s.cap + j];
-            join(m, sum, v.x, v.y);
+        for (int i0 = warp; i0 < pieces; i0 += 8 * kFinishWarps) {
+            float2 v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = i0 + e * kFinishWarps < pieces ? s.part[(i0 + e * kFinishWarps) * s.cap + j] : make_float2(-INFINITY, 0.0f);
+            float most = m;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, v[e].x);
+            const float zero = most == -INFINITY ? 0.0f : most;
+            sum *= exp2_fast((m - zero) * kLog2E);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[e].y * exp2_fast((v[e].x - zero) * kLog2E);
+            m = most;
         }
     }
     sm[0][warp][lane] = m;
     sm[1][warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && from >= 0) {
-        for (int k = 1; k < kWarps; ++k) join(m, sum, sm[0][k][lane], sm[1][k][lane]);
-        const float lse = m + logf(sum);
+        float most = -INFINITY;
+#pragma unroll 8
+        for (int k = 0; k < kFinishWarps; ++k) most = fmaxf(most, sm[0][k][lane]);
+        const float zero = most == -INFINITY ? 0.0f : most;
+        sum = 0.0f;
+#pragma unroll 8
+        for (int k = 0; k < kFinishWarps; ++k) sum += sm[1][k][lane] * exp2_fast((sm[0][k][lane] - zero) * kLog2E);
+        const float lse = zero + logf(sum);
         p.lse[from] = lse;
         p.loss[from] = lse - s.own[j];
     }
 }
 
 // The rows' gradients to their places: the parts of the sums added up, zeros for rows without a label.
-template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const Loss p, const Packed s, const Pass q, int vec) {
+template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const Loss p, const Packed s, const Pass q, int vec, int w_vec) {
     combo_step::pdl_release();
     combo_step::pdl_wait();
     const int splits = splits_of(q), lots = s.kp / 8;
@@ -523,6 +543,17 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const L
                 load32(q.dx + (i * total + j) * q.dx_pitch + k, v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(v[e]);
+            }
+            if (EB == 2) {
+                // d of a row's label is most of its gradient: what the plane's rounding left of it comes here
+                float v[8];
+                load8<EB>(p.w + (s.src[j] * p.w_stride + s.label[j] * p.w_pitch + k) * EB, left, w_vec, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = fmaf(s.own[j], v[e], f[e]);
+            }
+            if (!q.scaled) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] *= s.g[j];
             }
         }
         unsigned char* to = p.dx + (m * p.dx_pitch + k) * EB;
@@ -549,7 +580,10 @@ bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int
 }
 
 constexpr int kSms = 148;
-constexpr size_t kPieceBytes = 256u << 20;       // aimed at for a piece of classes: d, and the weights' planes
+#ifndef KPIECE
+#define KPIECE 512
+#endif
+constexpr size_t kPieceBytes = (size_t)KPIECE << 20;       // aimed at for a piece of classes: d, and the weights' planes
 
 // How a call is computed, by its sizes alone.
 struct Plan {
@@ -585,7 +619,7 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     a.d_planes = elem_bytes == 4 ? 3 : grad_bytes == 4 ? 2 : 1;
     a.kp = (int)up(K, 64);
     const int most = a.planes == 3 && a.cg == 1 ? 128 : 256;
-    a.v_width = even_width(V, most, 64 * a.cg);
+    a.v_width = even_width(V, most, 128);
     a.k_width = even_width(K, most, 64 * a.cg);
     if (V > 1024) a.v_width = most;
     a.unit = a.v_width;
@@ -609,9 +643,9 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     return a;
 }
 
-bool map_of(CUtensorMap* map, void* base, int rank, const long long* dims, const long long* strides) {
+bool map_of(CUtensorMap* map, void* base, int rank, const long long* dims, const long long* strides, int rows = 64) {
     cuuint64_t d[4], s[3];
-    const cuuint32_t box[4] = {kStep, 64, 1, 1}, ones[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {kStep, (cuuint32_t)rows, 1, 1}, ones[4] = {1, 1, 1, 1};
     for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
     for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * 2;
     return combo_host::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, base, d, s, box, ones, CU_TENSOR_MAP_SWIZZLE_128B);
@@ -620,7 +654,7 @@ bool map_of(CUtensorMap* map, void* base, int rank, const long long* dims, const
 template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass q, const Maps& maps, long long tiles, int sms, int smem_optin, cudaStream_t st) {
     static uint64_t allowed;
     auto kern = k_loss<CG, MODE, PA, PB, OB>;
-    const int turn = MODE == kWeights && !q.vec ? kOutWarps * kTurn : 0, most = smem_optin - kStaticSmem;
+    const int turn = MODE == kWeights && !q.vec ? kOutWarps * kTurn : MODE == kGrad ? kOutWarps * 2 * kPut : 0, most = smem_optin - kStaticSmem;
     q.stage_bytes = (PA * 2 + PB * (q.width / CG / 64)) * kBlock;
     q.stages = (most - 1024 - turn) / q.stage_bytes;
     if (q.stages > kMaxStages) q.stages = kMaxStages;
@@ -631,12 +665,14 @@ template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass
     cfg.blockDim = dim3(kTcThreads);
     cfg.dynamicSmemBytes = 1024 + (size_t)q.stages * q.stage_bytes + turn;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = CG > 1 ? 1 : 0;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, q, maps);
 }
 
@@ -671,25 +707,25 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     // bfloat16 weights on 16-byte boundaries are read where they lie
     const bool w_vec = vec_ok(p.w, p.w_pitch, p.w_stride, EB), direct = EB == 2 && w_vec && p.w_pitch < (1LL << 36) && p.w_stride < (1LL << 36);
     int piece = (int)up(p.V, a.unit);
-    if (!(direct && !kBack))
-        while (piece > a.unit && piece_bytes(a, p.N, piece, kBack, direct) > a.room) piece = (int)up(piece / 2, a.unit);
+    for (int n = 2; piece > a.unit && !(direct && !kBack) && piece_bytes(a, p.N, piece, kBack, direct) > a.room; ++n)
+        piece = (int)up((p.V + n - 1) / n, a.unit);
     s.d = reinterpret_cast<unsigned short*>(scratch + a.region);
     s.w = s.d + (kBack ? up((size_t)piece * cap * D * 2, 256) / 2 : 0);
 
     cudaError_t e = combo_host::launch_after(k_count, dim3(p.N), dim3(kCountThreads), 0, st, p, s);
     if (e != cudaSuccess) return e;
-    e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((cap + kPackRows - 1) / kPackRows)), dim3(kThreads), 0, st, p, s,
+    e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((cap + kPackRows - 1) / kPackRows)), dim3(kThreads), (size_t)(p.N + 1) * 4, st, p, s,
                                  (int)vec_ok(p.x, p.x_pitch, 0, EB));
     if (e != cudaSuccess) return e;
 
-    CUtensorMap mx, mw, md;
+    CUtensorMap mx, mw, md = {}, put = {};
     const long long xd[3] = {a.kp, a.cap, P}, xs[2] = {a.kp, a.cap * a.kp};
     const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : piece, p.N, direct ? 1 : P};
     const long long lines = (long long)piece * a.kp;
     const long long ws[3] = {direct ? p.w_pitch : a.kp, direct ? (p.N > 1 ? p.w_stride : 8) : lines, direct ? 8 : lines * p.N};
     const long long dd[3] = {piece, a.cap, D}, ds[2] = {piece, a.cap * piece};
     if (!map_of(&mx, s.x, 3, xd, xs) || !map_of(&mw, direct ? const_cast<unsigned char*>(p.w) : reinterpret_cast<unsigned char*>(s.w), 4, wd, ws) ||
-        (kBack && !map_of(&md, s.d, 3, dd, ds)))
+        (kBack && !(map_of(&md, s.d, 3, dd, ds) && map_of(&put, s.d, 3, dd, ds, 32))))
         return cudaErrorInvalidValue;
 
     Pass q = {};
@@ -700,14 +736,13 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.K = p.K;
     q.clusters = kSms / CG;
     q.row_cap = a.cap;
-    q.d_pitch = piece;
-    q.d_plane = a.cap * piece;
+    q.count = s.count;
+    q.scaled = p.row_grad != nullptr;
     q.label = s.label;
     q.lse = s.lse;
     q.g = s.g;
     q.part = s.part;
     q.own = s.own;
-    q.d = s.d;
     q.dx = s.dx;
     q.dw = p.dw;
     q.dw_pitch = p.dw_pitch;
@@ -730,7 +765,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.width = a.v_width;
         q.wt = (classes + a.v_width - 1) / a.v_width;
         q.steps = a.kp / kStep;
-        const Maps logits_of = {mx, mw};
+        const Maps logits_of = {mx, mw, put};
         e = kBack ? launch_loss<CG, kGrad, P, P, D>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
                   : launch_loss<CG, kStats, P, P, 1>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
         if (e != cudaSuccess) return e;
@@ -740,22 +775,22 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
             q.steps = (classes + kStep - 1) / kStep;
             q.add = v0 > 0;
             // bfloat16 rows take the first plane of d: the others are below their rounding
-            e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
+            e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw, put}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
             if (e != cudaSuccess) return e;
             q.ht = (classes + s.height - 1) / s.height;
             q.vec = vec_ok(p.dw, p.dw_pitch, p.dw_stride, GB) && p.K * GB % 16 == 0
                         ? combo_host::aligned_to(p.dw, 32) && p.dw_pitch * GB % 32 == 0 && p.dw_stride * GB % 32 == 0 ? 32 : 16
                         : 0;
-            e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{md, mx}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
+            e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{md, mx, put}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
             if (e != cudaSuccess) return e;
         }
     }
-    if (!kBack) return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(kThreads), 0, st, p, s, 2 * ((p.V + a.v_width - 1) / a.v_width));
+    if (!kBack) return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(kFinishWarps * 32), 0, st, p, s, 2 * ((p.V + a.v_width - 1) / a.v_width));
     q.width = a.k_width;
     q.wt = kt;
     const long long lots = (long long)p.M * a.kp / 8, grid = (lots + kThreads - 1) / kThreads;
     return combo_host::launch_after(k_rows_out<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s, q,
-                                    (int)vec_ok(p.dx, p.dx_pitch, 0, EB));
+                                    (int)vec_ok(p.dx, p.dx_pitch, 0, EB), (int)w_vec);
 }
 
 template <int CG> cudaError_t launch_tensor(const Plan& a, const Loss& p, int elem_bytes, int grad_bytes, void* scratch, int sms, int smem_optin, cudaStream_t st) {

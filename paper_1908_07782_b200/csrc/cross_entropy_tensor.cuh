@@ -26,7 +26,8 @@ constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kBlock = 64 * kStep * 2;       // bytes of a block of 64 x 64
 constexpr int kOutWarps = 8, kFirstOutWarp = 4, kTcThreads = 32 * (kFirstOutWarp + kOutWarps);
 constexpr int kMaxStages = 8;
-constexpr int kTurn = 32 * 33 * 4;           // bytes in which a warp turns 32 x 32 results
+constexpr int kTurn = 32 * 33 * 4;           // weights': bytes in which a warp turns 32 x 32 results
+constexpr int kPut = 32 * 128;               // kGrad: bytes that a warp hands to TMA, 32 rows of 64 values; two such places
 constexpr int kTmemColumns = 512;
 constexpr int kStaticSmem = 1024;
 constexpr float kLog2E = 1.4426950408889634f;
@@ -48,18 +49,19 @@ struct Pass {
     int v_end;                               // weights': behind the piece's last class
     int clusters, split_steps;               // rows': that run at once; a whole piece's stages
     int add, vec;                            // rows': whether sums are there already; weights': bytes that a store may take at once
-    long long row_cap, d_pitch, dx_pitch, d_plane;
+    int scaled;                              // whether d holds the rows' factors g; else the weights' gradients are divided by `count`
+    long long row_cap, dx_pitch;
     const int* label;                        // of packed rows; -1 behind a worker's last
     const float *lse, *g;
+    const int* count;                        // labelled rows of a worker
     float2* part;                            // [2 tiles of classes][row_cap]
-    float* own;                              // a row's logit of its label
-    unsigned short* d;                       // [planes][row_cap][d_pitch]
+    float* own;                              // a row's logit of its label; kGrad: what the first plane of d leaves of its d
     float* dx;                               // [splits][rows][dx_pitch]
     unsigned char* dw;
     long long dw_pitch, dw_stride;
 };
 struct alignas(64) Maps {
-    CUtensorMap a, b;
+    CUtensorMap a, b, d;                     // d: kGrad's results, [planes][row_cap][piece], 32 rows to a box
 };
 
 // Into how many parts the sums over a piece's classes are cut, to have work for all CTAs where rows are few: the number with the
@@ -178,6 +180,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
         prefetch_map(&maps.b);
     }
     if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_at), kTmemColumns);
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
     tc_fence_before();
     __syncthreads();
     if (CG == 2) {
@@ -291,13 +295,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
         Walk<CG, MODE> walk(q, first);
         const int quarter = warp & 3, half = (warp - kFirstOutWarp) >> 2, columns = q.width / 2;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * columns;
-        uint32_t turn = 0;
+        uint32_t turn = 0, puts = 0;
+        const uint32_t put = smem + q.stages * q.stage_bytes + (warp - kFirstOutWarp) * 2 * kPut;
         bool ok = true;
         while (walk.next(x, stride)) {
             const int parts = (x.steps + q.part_steps - 1) / q.part_steps;
+            const int col = x.c0 + half * columns;       // the first of the thread's columns
+            const int j = x.row + rank * 128 + quarter * 32 + lane;          // the packed row (weights': none)
+            // workers' rows begin at multiples of 64: a warp's are all this worker's, or another's or nobody's
+            const bool mine = MODE != kWeights && j < x.row_end;
             float acc[128];
 #pragma unroll
             for (int e = 0; e < 128; ++e) acc[e] = 0.0f;
+            if (MODE == kRows && q.add && mine && x.steps > 0) {
+                const float* from = q.dx + ((long long)x.split * q.row0[q.N] + j) * q.dx_pitch + col;
+#pragma unroll
+                for (int c = 0; c < 128; c += 8) {
+                    if (c < columns) {
+                        uint32_t o[8];
+                        load32(from + c, o);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[c + e] = __uint_as_float(o[e]);
+                    }
+                }
+            }
             for (int part = 0; part < parts; ++part) {
                 const uint32_t n = turn + part, buf = n & 1u;
                 ok = mbar_wait(acc_full(buf), n >> 1 & 1u, dead_v) || give_up(54);
@@ -319,8 +340,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
             }
             if (!ok) break;
             turn += parts;
-            const int col = x.c0 + half * columns;       // the first of the thread's columns
             if constexpr (MODE == kWeights) {
+                if (!q.scaled) {
+                    const float scale = parts > 0 ? 1.0f / (float)q.count[x.w] : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 128; ++e) acc[e] *= scale;
+                }
                 const int v = q.v0 + x.h0 + rank * 128 + quarter * 32 + lane;
                 if (q.vec) {
                     if (v < q.v_end) {
@@ -361,23 +386,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                     }
                 }
             } else {
-                const int j = x.row + rank * 128 + quarter * 32 + lane;
-                const bool mine = j < x.row_end;         // else another worker's, or nobody's
+                if (!mine) continue;
                 if constexpr (MODE == kStats) {
-                    const int left = q.V - (q.v0 + col); // classes that there are
-                    float m = -INFINITY;
+                    // classes that are not there
+                    const int left = q.V - (q.v0 + col);
+                    if (left < columns) {
 #pragma unroll
-                    for (int e = 0; e < 128; ++e)
-                        if (e < columns && e < left) m = fmaxf(m, acc[e]);
-                    const float zero = m == -INFINITY ? 0.0f : m;
-                    float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 128; e += 2) {
-                        if (e < columns && e < left) s0 += exp2_fast((acc[e] - zero) * kLog2E);
-                        if (e + 1 < columns && e + 1 < left) s1 += exp2_fast((acc[e + 1] - zero) * kLog2E);
+                        for (int e = 0; e < 128; ++e)
+                            if (e >= left) acc[e] = -INFINITY;
                     }
-                    if (mine) q.part[((q.v0 + col) / columns) * q.row_cap + j] = make_float2(m, s0 + s1);
-                    const int at = mine ? q.label[j] - q.v0 - col : -1;
+                    float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        if (c < columns) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) most[e & 3] = fmaxf(most[e & 3], acc[c + e]);
+                        }
+                    }
+                    const float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), zero = m == -INFINITY ? 0.0f : m;
+                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        if (c < columns) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) sum[e & 3] += exp2_fast((acc[c + e] - zero) * kLog2E);
+                        }
+                    }
+                    q.part[((q.v0 + col) / columns) * q.row_cap + j] = make_float2(m, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                    const int at = q.label[j] - q.v0 - col;
                     if (__any_sync(0xffffffffu, at >= 0 && at < columns)) {
                         float z = 0.0f;
 #pragma unroll
@@ -386,67 +422,95 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                         if (at >= 0 && at < columns) q.own[j] = z;
                     }
                 } else if constexpr (MODE == kGrad) {
-                    const int left = q.V - (q.v0 + col);
-                    const int label = mine ? q.label[j] : -1;
-                    const float lse = label >= 0 ? q.lse[j] : 0.0f, g = label >= 0 ? q.g[j] : 0.0f;
+                    const int left = q.v_end - (q.v0 + col), label = q.label[j];
+                    const float lse = label >= 0 ? q.lse[j] : 0.0f;
                     const int at = label - q.v0 - col;
-                    const bool any = __any_sync(0xffffffffu, label >= 0 && at >= 0 && at < columns);
 #pragma unroll
-                    for (int e = 0; e < 128; ++e)
-                        if (e < columns) acc[e] = exp2_fast((acc[e] - lse) * kLog2E);
+                    for (int c = 0; c < 128; c += 32) {
+                        if (c < columns) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) acc[c + e] = exp2_fast((acc[c + e] - lse) * kLog2E);
+                        }
+                    }
+                    const bool here = label >= 0 && at >= 0 && at < columns;
+                    const bool any = __any_sync(0xffffffffu, here);
                     if (any) {
 #pragma unroll
                         for (int e = 0; e < 128; ++e)
                             if (e == at) acc[e] -= 1.0f;
                     }
+                    if (q.scaled) {
+                        const float g = label >= 0 ? q.g[j] : 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 128; ++e) acc[e] *= g;
+                    }
                     // rows without a label and classes that are not there: 0, whatever the product is
+                    if (left < columns) {
 #pragma unroll
-                    for (int e = 0; e < 128; ++e)
-                        if (e < columns) acc[e] = label >= 0 && e < left ? acc[e] * g : 0.0f;
-                    if (mine) {
-                        unsigned short* to = q.d + (long long)j * q.d_pitch + col;
+                        for (int e = 0; e < 128; ++e)
+                            if (e >= left) acc[e] = 0.0f;
+                    }
+                    if (!__all_sync(0xffffffffu, label >= 0)) {
 #pragma unroll
-                        for (int p = 0; p < OB; ++p) {
+                        for (int e = 0; e < 128; ++e) acc[e] = label >= 0 ? acc[e] : 0.0f;
+                    }
+                    if (any) {
+                        float rest = 0.0f;
 #pragma unroll
-                            for (int c = 0; c < 128; c += 16) {
-                                if (c < columns) {
-                                    uint32_t o[8];
+                        for (int e = 0; e < 128; ++e)
+                            if (e == at) rest = acc[e] - combo_step::widen_lo(combo_step::pack_bf16(acc[e], 0.0f));
+                        if (here) q.own[j] = rest;
+                    }
+                    // 64 columns of a plane at a time, in TMA's order: 16 bytes of a row at (their number xor the row's) of its 128
 #pragma unroll
-                                    for (int e = 0; e < 8; ++e) {
-                                        o[e] = combo_step::pack_bf16(acc[c + 2 * e], acc[c + 2 * e + 1]);
+                    for (int p = 0; p < OB; ++p) {
+#pragma unroll
+                        for (int c = 0; c < 128; c += 64) {
+                            if (c < columns) {
+                                const uint32_t place = put + (puts & 1u) * kPut;
+                                if (elect()) tma_store_wait_read<1>();
+                                __syncwarp();
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) {
+                                    uint32_t o[4];
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        float &lo = acc[c + k * 8 + 2 * e], &hi = acc[c + k * 8 + 2 * e + 1];
+                                        o[e] = combo_step::pack_bf16(lo, hi);
                                         if (p + 1 < OB) {
-                                            acc[c + 2 * e] -= combo_step::widen_lo(o[e]);
-                                            acc[c + 2 * e + 1] -= combo_step::widen_hi(o[e]);
+                                            lo -= combo_step::widen_lo(o[e]);
+                                            hi -= combo_step::widen_hi(o[e]);
                                         }
                                     }
-                                    store32(to + p * q.d_plane + c, o);
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + lane * 128 + ((k ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]),
+                                                 "r"(o[2]), "r"(o[3])
+                                                 : "memory");
                                 }
+                                fence_async();
+                                __syncwarp();
+                                if (elect()) tma_store_3d(&maps.d, place, col + c, j - lane, p);
+                                __syncwarp();
+                                ++puts;
                             }
                         }
                     }
                 } else {
-                    if (mine) {
-                        float* to = q.dx + ((long long)x.split * q.row0[q.N] + j) * q.dx_pitch + col;
-                        if (!q.add || x.steps > 0) {
+                    float* to = q.dx + ((long long)x.split * q.row0[q.N] + j) * q.dx_pitch + col;
+                    if (!q.add || x.steps > 0) {
 #pragma unroll
-                            for (int c = 0; c < 128; c += 8) {
-                                if (c < columns) {
-                                    uint32_t o[8];
-                                    if (q.add) {
-                                        load32(to + c, o);
+                        for (int c = 0; c < 128; c += 8) {
+                            if (c < columns) {
+                                uint32_t o[8];
 #pragma unroll
-                                        for (int e = 0; e < 8; ++e) acc[c + e] += __uint_as_float(o[e]);
-                                    }
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(acc[c + e]);
-                                    store32(to + c, o);
-                                }
+                                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(acc[c + e]);
+                                store32(to + c, o);
                             }
                         }
                     }
                 }
             }
         }
+        if (MODE == kGrad) tma_store_wait();
         if (!ok) *dead_v = 1;
     }
     tc_fence_before();

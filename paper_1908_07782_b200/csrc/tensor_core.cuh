@@ -100,6 +100,15 @@ __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int
                      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(u)
                      : "memory");
 }
+// A box of this CTA's shared memory to global memory; the thread that asked may wait until it has been read (the memory may be
+// used again), or is there.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t from, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(from), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int LEFT> __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // what threads wrote to shared memory becomes visible to the tensor cores and to TMA
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
