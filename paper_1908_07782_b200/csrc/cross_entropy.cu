@@ -299,7 +299,7 @@ using namespace combo_loss;
 struct Packed {
     int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 1]; [cap]: forward the row, backward the worker; [cap]
     float *lse, *g, *own;                                      // [cap]
-    unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][piece][kp]; of [cap][d_pitch]
+    unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][piece][kp]; of [piece / 8][cap][8]
     float2* part;
     float* dx;
     long long cap;
@@ -487,22 +487,22 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, cons
     __shared__ float sm[2][kFinishWarps][32];
     combo_step::pdl_release();
     combo_step::pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, j = blockIdx.x * 32 + lane;
     if (blockIdx.x * 32 >= s.row0[p.N]) return;
     const int from = s.src[j];
     float m = -INFINITY, sum = 0.0f;
     if (from >= 0) {
-        for (int i0 = warp; i0 < pieces; i0 += 8 * kFinishWarps) {
+        for (int i0 = warp; i0 < pieces; i0 += 8 * warps) {
             float2 v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = i0 + e * kFinishWarps < pieces ? s.part[(i0 + e * kFinishWarps) * s.cap + j] : make_float2(-INFINITY, 0.0f);
+            for (int e = 0; e < 8; ++e) v[e] = i0 + e * warps < pieces ? s.part[(i0 + e * warps) * s.cap + j] : make_float2(-INFINITY, 0.0f);
             float most = m;
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = fmaxf(most, v[e].x);
             const float zero = most == -INFINITY ? 0.0f : most;
-            sum *= exp2_fast((m - zero) * kLog2E);
+            sum *= exp2_fast(m - zero);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[e].y * exp2_fast((v[e].x - zero) * kLog2E);
+            for (int e = 0; e < 8; ++e) sum += v[e].y * exp2_fast(v[e].x - zero);
             m = most;
         }
     }
@@ -512,12 +512,12 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, cons
     if (warp == 0 && from >= 0) {
         float most = -INFINITY;
 #pragma unroll 8
-        for (int k = 0; k < kFinishWarps; ++k) most = fmaxf(most, sm[0][k][lane]);
+        for (int k = 0; k < warps; ++k) most = fmaxf(most, sm[0][k][lane]);
         const float zero = most == -INFINITY ? 0.0f : most;
         sum = 0.0f;
 #pragma unroll 8
-        for (int k = 0; k < kFinishWarps; ++k) sum += sm[1][k][lane] * exp2_fast((sm[0][k][lane] - zero) * kLog2E);
-        const float lse = zero + logf(sum);
+        for (int k = 0; k < warps; ++k) sum += sm[1][k][lane] * exp2_fast(sm[0][k][lane] - zero);
+        const float lse = (zero + log2f(sum)) * 0.69314718f;
         p.lse[from] = lse;
         p.loss[from] = lse - s.own[j];
     }
@@ -581,7 +581,7 @@ bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int
 
 constexpr int kSms = 148;
 #ifndef KPIECE
-#define KPIECE 512
+#define KPIECE 1024
 #endif
 constexpr size_t kPieceBytes = (size_t)KPIECE << 20;       // aimed at for a piece of classes: d, and the weights' planes
 
@@ -591,6 +591,7 @@ struct Plan {
     int cg, planes, d_planes, kp;                // of x and w; of d
     int v_width, k_width, unit;                  // tiles along the classes, along the inputs; pieces are multiples of `unit`
     long long cap;
+    long long dx_rows;                           // of the sums for dx, all splits
     size_t x, part, dx, region, room, total;     // places in scratch; bytes of the region for pieces
 };
 
@@ -620,7 +621,7 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     a.kp = (int)up(K, 64);
     const int most = a.planes == 3 && a.cg == 1 ? 128 : 256;
     a.v_width = even_width(V, most, 128);
-    a.k_width = even_width(K, most, 64 * a.cg);
+    a.k_width = even_width(K, most, 128);
     if (V > 1024) a.v_width = most;
     a.unit = a.v_width;
     a.cap = (long long)up(M + 63 * (N < M ? N : M), 64);
@@ -634,7 +635,8 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     } else {
         const size_t wt = up(K, a.k_width) / a.k_width, split_rows = (size_t)kMaxTurns * (kSms / a.cg) / wt * 128 * a.cg;
         a.dx = at;
-        at += up((cap > split_rows ? cap : split_rows) * wt * a.k_width * 4, 256);
+        a.dx_rows = (long long)(cap > split_rows ? cap : split_rows);
+        at += up((size_t)a.dx_rows * wt * a.k_width * 4, 256);
     }
     a.region = at;
     const size_t whole = piece_bytes(a, N, up(V, a.unit), back, false), least = piece_bytes(a, N, a.unit, back, false);
@@ -643,18 +645,20 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     return a;
 }
 
-bool map_of(CUtensorMap* map, void* base, int rank, const long long* dims, const long long* strides, int rows = 64) {
+// Tensor map of elements of eb bytes; boxes of 128 bytes, swizzled, by `rows`, or of `plain` elements without a swizzle.
+bool map_of(CUtensorMap* map, void* base, int eb, int rank, const long long* dims, const long long* strides, int rows, int plain = 0) {
     cuuint64_t d[4], s[3];
-    const cuuint32_t box[4] = {kStep, (cuuint32_t)rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {plain ? (cuuint32_t)plain : 128u / eb, (cuuint32_t)rows, 1, 1}, ones[4] = {1, 1, 1, 1};
     for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
-    for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * 2;
-    return combo_host::encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, base, d, s, box, ones, CU_TENSOR_MAP_SWIZZLE_128B);
+    for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * eb;
+    const CUtensorMapDataType type = eb == 8 ? CU_TENSOR_MAP_DATA_TYPE_UINT64 : eb == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    return combo_host::encode_tiled(map, type, rank, base, d, s, box, ones, plain ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass q, const Maps& maps, long long tiles, int sms, int smem_optin, cudaStream_t st) {
     static uint64_t allowed;
     auto kern = k_loss<CG, MODE, PA, PB, OB>;
-    const int turn = MODE == kWeights && !q.vec ? kOutWarps * kTurn : MODE == kGrad ? kOutWarps * 2 * kPut : 0, most = smem_optin - kStaticSmem;
+    const int turn = MODE == kWeights && !q.vec ? kOutWarps * kTurn : MODE == kRows || MODE == kWeights ? kOutWarps * kPut : 0, most = smem_optin - kStaticSmem;
     q.stage_bytes = (PA * 2 + PB * (q.width / CG / 64)) * kBlock;
     q.stages = (most - 1024 - turn) / q.stage_bytes;
     if (q.stages > kMaxStages) q.stages = kMaxStages;
@@ -718,15 +722,26 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
                                  (int)vec_ok(p.x, p.x_pitch, 0, EB));
     if (e != cudaSuccess) return e;
 
-    CUtensorMap mx, mw, md = {}, put = {};
+    // bfloat16 or floats by whole boxes where 16-byte boundaries allow
+    const bool dw_vec = kBack && vec_ok(p.dw, p.dw_pitch, p.dw_stride, kBack ? GB : 4) && p.dw_pitch < (1LL << 36) && p.dw_stride < (1LL << 36);
+    const int kt = (p.K + a.k_width - 1) / a.k_width;
+    const long long dx_pitch = kt * a.k_width;
+    CUtensorMap mx, mw, md = {}, mdw = {}, out_dx = {}, out_dw = {};
     const long long xd[3] = {a.kp, a.cap, P}, xs[2] = {a.kp, a.cap * a.kp};
     const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : piece, p.N, direct ? 1 : P};
     const long long lines = (long long)piece * a.kp;
     const long long ws[3] = {direct ? p.w_pitch : a.kp, direct ? (p.N > 1 ? p.w_stride : 8) : lines, direct ? 8 : lines * p.N};
-    const long long dd[3] = {piece, a.cap, D}, ds[2] = {piece, a.cap * piece};
-    if (!map_of(&mx, s.x, 3, xd, xs) || !map_of(&mw, direct ? const_cast<unsigned char*>(p.w) : reinterpret_cast<unsigned char*>(s.w), 4, wd, ws) ||
-        (kBack && !(map_of(&md, s.d, 3, dd, ds) && map_of(&put, s.d, 3, dd, ds, 32))))
-        return cudaErrorInvalidValue;
+    // d: eight classes of a row in 16 bytes, rows side by side, so that a warp that writes and a box that is read run along memory;
+    // in 64-bit units, of which a box may have 256
+    const long long dd[3] = {2 * a.cap, piece / 8, D}, ds[2] = {a.cap * 2, a.cap * 2 * (piece / 8)};
+    bool fine = map_of(&mx, s.x, 2, 3, xd, xs, 64) && map_of(&mw, direct ? const_cast<unsigned char*>(p.w) : reinterpret_cast<unsigned char*>(s.w), 2, 4, wd, ws, 64);
+    if (kBack && fine) {
+        const long long rd[3] = {dx_pitch, a.dx_rows, 1}, rs[2] = {dx_pitch, 8};
+        const long long gd[3] = {p.K, p.V, p.N}, gs[2] = {p.dw_pitch, p.N > 1 ? p.dw_stride : 8};
+        fine = map_of(&md, s.d, 8, 3, dd, ds, 8, 256) && map_of(&mdw, s.d, 8, 3, dd, ds, 16, 128) && map_of(&out_dx, s.dx, 4, 3, rd, rs, 32) &&
+               (!dw_vec || map_of(&out_dw, p.dw, kBack ? GB : 4, 3, gd, gs, 32));
+    }
+    if (!fine) return cudaErrorInvalidValue;
 
     Pass q = {};
     q.row0 = s.row0;
@@ -737,6 +752,8 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.clusters = kSms / CG;
     q.row_cap = a.cap;
     q.count = s.count;
+    q.d = reinterpret_cast<unsigned char*>(s.d);
+    q.d_blocks = piece / 8;
     q.scaled = p.row_grad != nullptr;
     q.label = s.label;
     q.lse = s.lse;
@@ -748,8 +765,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.dw_pitch = p.dw_pitch;
     q.dw_stride = p.dw_stride;
     q.part_steps = EB == 4 ? 1 : 16;
-    const int kt = (p.K + a.k_width - 1) / a.k_width;
-    q.dx_pitch = kt * a.k_width;
+    q.dx_pitch = dx_pitch;
     q.split_steps = (int)(piece < up(p.V, 64) ? piece : up(p.V, 64)) / kStep;
     const long long row_tiles = p.M / s.height + (p.N < p.M ? p.N : p.M);          // at most
     for (int v0 = 0; v0 < p.V; v0 += piece) {
@@ -765,7 +781,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.width = a.v_width;
         q.wt = (classes + a.v_width - 1) / a.v_width;
         q.steps = a.kp / kStep;
-        const Maps logits_of = {mx, mw, put};
+        const Maps logits_of = {mx, mw, mw};
         e = kBack ? launch_loss<CG, kGrad, P, P, D>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
                   : launch_loss<CG, kStats, P, P, 1>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
         if (e != cudaSuccess) return e;
@@ -775,17 +791,18 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
             q.steps = (classes + kStep - 1) / kStep;
             q.add = v0 > 0;
             // bfloat16 rows take the first plane of d: the others are below their rounding
-            e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw, put}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
+            e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw, out_dx}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
             if (e != cudaSuccess) return e;
             q.ht = (classes + s.height - 1) / s.height;
-            q.vec = vec_ok(p.dw, p.dw_pitch, p.dw_stride, GB) && p.K * GB % 16 == 0
-                        ? combo_host::aligned_to(p.dw, 32) && p.dw_pitch * GB % 32 == 0 && p.dw_stride * GB % 32 == 0 ? 32 : 16
-                        : 0;
-            e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{md, mx, put}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
+            q.vec = dw_vec;
+            e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{mdw, mx, out_dw}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
             if (e != cudaSuccess) return e;
         }
     }
-    if (!kBack) return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(kFinishWarps * 32), 0, st, p, s, 2 * ((p.V + a.v_width - 1) / a.v_width));
+    if (!kBack) {
+        const int pieces = 2 * ((p.V + a.v_width - 1) / a.v_width), warps = pieces >= 8 * kFinishWarps ? kFinishWarps : pieces / 8 < 4 ? 4 : pieces / 8;
+        return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(warps * 32), 0, st, p, s, pieces);
+    }
     q.width = a.k_width;
     q.wt = kt;
     const long long lots = (long long)p.M * a.kp / 8, grid = (lots + kThreads - 1) / kThreads;

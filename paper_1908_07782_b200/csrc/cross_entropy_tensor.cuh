@@ -19,15 +19,23 @@
 namespace combo_loss {
 
 using namespace combo_tc;
+using combo_step::add2;
+using combo_step::f32x2;
+using combo_step::fma2;
+using combo_step::hi_of;
+using combo_step::lo_of;
+using combo_step::mul2;
+using combo_step::neg2;
+using combo_step::pair;
 
 enum Mode { kStats = 0, kGrad = 1, kRows = 2, kWeights = 3 };
 
 constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kBlock = 64 * kStep * 2;       // bytes of a block of 64 x 64
-constexpr int kOutWarps = 8, kFirstOutWarp = 4, kTcThreads = 32 * (kFirstOutWarp + kOutWarps);
+constexpr int kOutWarps = 8, kFirstOutWarp = 4, kCols = 1024 / kOutWarps, kTcThreads = 32 * (kFirstOutWarp + kOutWarps);
 constexpr int kMaxStages = 8;
 constexpr int kTurn = 32 * 33 * 4;           // weights': bytes in which a warp turns 32 x 32 results
-constexpr int kPut = 32 * 128;               // kGrad: bytes that a warp hands to TMA, 32 rows of 64 values; two such places
+constexpr int kPut = 32 * 128;               // bytes that a warp hands to TMA: 32 rows of 128
 constexpr int kTmemColumns = 512;
 constexpr int kStaticSmem = 1024;
 constexpr float kLog2E = 1.4426950408889634f;
@@ -48,9 +56,12 @@ struct Pass {
     int v0, w_row;                           // the piece's first class, and where the map of the weights has it
     int v_end;                               // weights': behind the piece's last class
     int clusters, split_steps;               // rows': that run at once; a whole piece's stages
-    int add, vec;                            // rows': whether sums are there already; weights': bytes that a store may take at once
+    int add, vec;                            // rows': whether sums are there already; weights': whether TMA may store them
     int scaled;                              // whether d holds the rows' factors g; else the weights' gradients are divided by `count`
-    long long row_cap, dx_pitch;
+    long long row_cap;
+    unsigned char* d;                        // [planes][d_blocks][row_cap] of eight classes in 16 bytes
+    int d_blocks;
+    long long dx_pitch;
     const int* label;                        // of packed rows; -1 behind a worker's last
     const float *lse, *g;
     const int* count;                        // labelled rows of a worker
@@ -61,7 +72,7 @@ struct Pass {
     long long dw_pitch, dw_stride;
 };
 struct alignas(64) Maps {
-    CUtensorMap a, b, d;                     // d: kGrad's results, [planes][row_cap][piece], 32 rows to a box
+    CUtensorMap a, b, out;                   // out: of dx or dW, 32 rows of 128 bytes to a box
 };
 
 // Into how many parts the sums over a piece's classes are cut, to have work for all CTAs where rows are few: the number with the
@@ -84,49 +95,74 @@ struct Tile {
     int step0, steps;
 };
 
-// Walks the tiles t, t + stride, ...; the whole warp.
+// Walks the tiles t, t + stride, ...; the whole warp.  Lanes find 32 tiles at once: the search and the divisions take more than a
+// thousand cycles, and taking them before every tile left the ring of stages short of loads (16 stages a tile: 700 cycles a stage).
 template <int CG, int MODE> struct Walk {
     const Pass& q;
-    int t, lane, w0, mult, splits, upto;     // upto: tiles up to the lane's worker, that one with it
-    __device__ __forceinline__ Walk(const Pass& q_, int first) : q(q_), t(first) {
+    int t, stride, lane, at, splits;
+    int w, row, rows, code, high;            // the lane's tile; w < 0: none
+    __device__ __forceinline__ Walk(const Pass& q_, int first, int stride_) : q(q_), t(first), stride(stride_) {
         lane = threadIdx.x & 31;
         splits = MODE == kRows ? splits_of(q) : 1;
-        mult = q.wt * splits;
-        w0 = 0;
-        if (MODE != kWeights) lot();
+        at = 32;
     }
-    __device__ __forceinline__ void lot() { upto = q.tiles[min(w0 + lane + 1, q.N)] * mult; }
-    __device__ __forceinline__ bool next(Tile& x, int stride) {
+    __device__ __forceinline__ void find() {
+        const int mine = t + lane * stride;
+        w = -1;
+        row = rows = code = high = 0;
         if (MODE == kWeights) {
             const int per = q.wt * q.ht;
-            if (t >= per * q.N) return false;
-            x.w = t / per;
-            const int k = t - x.w * per;
-            x.c0 = k % q.wt * q.width;
-            x.h0 = k / q.wt * 128 * CG;
-            x.row = q.row0[x.w];
-            x.row_end = q.row0[x.w + 1];
-            x.split = x.step0 = 0;
-            x.steps = (x.row_end - x.row) / kStep;
-        } else {
-            unsigned m;
-            while (!(m = __ballot_sync(0xffffffffu, upto > t))) {
-                w0 += 32;
-                if (w0 >= q.N) return false;
-                lot();
+            if (mine < per * q.N) {
+                w = mine / per;
+                const int k = mine - w * per;
+                high = k / q.wt;
+                code = k - high * q.wt;
+                row = q.row0[w];
+                rows = q.row0[w + 1] - row;
             }
-            x.w = w0 + __ffs(m) - 1;
-            const int before = q.tiles[x.w], mine = q.tiles[x.w + 1] - before, at = t - before * mult, rest = at / mine;
-            x.split = rest / q.wt;
-            x.c0 = (rest - x.split * q.wt) * q.width;
-            x.h0 = 0;
-            x.row = q.row0[x.w] + (at - rest * mine) * 128 * CG;
-            x.row_end = q.row0[x.w + 1];
-            const int per = MODE == kRows ? (q.steps + splits - 1) / splits : q.steps;
+        } else {
+            const int mult = q.wt * splits;
+            int lo = 0, hi = q.N;            // the last w with so many tiles before it
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (q.tiles[mid] * mult <= mine) lo = mid;
+                else hi = mid - 1;
+            }
+            if (lo < q.N) {
+                w = lo;
+                const int before = q.tiles[w], tiles = q.tiles[w + 1] - before, k = mine - before * mult, rest = k / tiles;
+                row = (k - rest * tiles) * 128 * CG;
+                rows = q.row0[w + 1] - q.row0[w] - row;
+                row += q.row0[w];
+                code = rest;
+            }
+        }
+        t += 32 * stride;
+        at = 0;
+    }
+    __device__ __forceinline__ bool next(Tile& x) {
+        if (at == 32) find();
+        x.w = __shfl_sync(0xffffffffu, w, at);
+        if (x.w < 0) return false;
+        x.row = __shfl_sync(0xffffffffu, row, at);
+        const int n = __shfl_sync(0xffffffffu, rows, at), c = __shfl_sync(0xffffffffu, code, at);
+        x.row_end = x.row + n;
+        x.h0 = x.split = x.step0 = 0;
+        x.steps = q.steps;
+        if (MODE == kWeights) {
+            x.h0 = __shfl_sync(0xffffffffu, high, at) * 128 * CG;
+            x.c0 = c * q.width;
+            x.steps = n / kStep;
+        } else if (MODE == kRows) {
+            x.split = c / q.wt;
+            x.c0 = (c - x.split * q.wt) * q.width;
+            const int per = (q.steps + splits - 1) / splits;
             x.step0 = min(x.split * per, q.steps);
             x.steps = min(per, q.steps - x.step0);
+        } else {
+            x.c0 = c * q.width;
         }
-        t += stride;
+        ++at;
         return true;
     }
 };
@@ -136,16 +172,33 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void store32(void* to, const uint32_t (&v)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
-                 "r"(v[5]), "r"(v[6]), "r"(v[7])
-                 : "memory");
-}
 __device__ __forceinline__ void load32(const void* from, uint32_t (&v)[8]) {
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "l"(from)
                  : "memory");
+}
+
+// A warp's columns c .. of acc, 128 bytes of a lane's row, into shared memory in TMA's order (16 bytes of a row at their number xor
+// the row's), and on from there by `hand`, which one thread calls.
+template <int EB, typename F> __device__ __forceinline__ void put_box(uint32_t put, const f32x2 (&acc)[kCols / 2], int c, int lane, F hand) {
+    if (elect()) tma_store_wait_read();
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        uint32_t o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x2 v = acc[(EB == 4 ? (c + k * 4 + e) / 2 : (c + k * 8) / 2 + e) % (kCols / 2)];
+            o[e] = EB == 4 ? __float_as_uint(e & 1 ? hi_of(v) : lo_of(v)) : combo_step::pack_bf16(lo_of(v), hi_of(v));
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + lane * 128 + ((k ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                     : "memory");
+    }
+    fence_async();
+    __syncwarp();
+    if (elect()) hand();
+    __syncwarp();
 }
 
 // PA, PB: planes of the height's and the width's operand.  OB: weights': bytes of a result; kGrad: planes of d.
@@ -202,10 +255,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
         const int planes = op == 0 ? PA : PB, blocks = op == 0 ? 2 : blocks_b;
         const uint32_t bytes = (uint32_t)(planes * blocks) * kBlock, offset = op == 0 ? 0u : (uint32_t)PA * 2 * kBlock;
         const uint32_t bar_leader = CG == 1 ? full(0) : at_leader(full(0));
-        Walk<CG, MODE> walk(q, first);
+        Walk<CG, MODE> walk(q, first, stride);
         uint32_t done = 0;
         bool ok = true;
-        while (walk.next(x, stride)) {
+        while (walk.next(x)) {
             uint32_t s = done % q.stages, ph = done / q.stages & 1u;
             if (elect()) {
                 // along the operand's own index; a step goes along r
@@ -215,19 +268,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                     if (rank == 0) mbar_arrive_expect(full(s), bytes * CG);
                     uint32_t to = smem + s * q.stage_bytes + offset;
                     const int r = (x.step0 + k) * kStep, bar = bar_leader + 8 * s;
-                    for (int p = 0; p < planes; ++p)
+                    for (int p = 0; p < planes; ++p) {
+                        if (op == 0 && (MODE == kRows || MODE == kWeights)) {
+                            // d: both blocks at once
+                            if (MODE == kRows) tma_3d<CG>(to, map, 2 * own, r / 8, p, bar);
+                            else tma_3d<CG>(to, map, 2 * (x.row + r), own / 8, p, bar);
+                            to += 2 * kBlock;
+                            continue;
+                        }
                         for (int b = 0; b < blocks; ++b, to += kBlock) {
                             const int i = own + b * 64;
-                            if (MODE == kStats || MODE == kGrad) {
-                                if (op == 0) tma_3d<CG>(to, map, r, i, p, bar);
-                                else tma_4d<CG>(to, map, r, q.w_row + i, x.w, p, bar);
-                            } else if (MODE == kRows) {
-                                if (op == 0) tma_3d<CG>(to, map, r, i, p, bar);
-                                else tma_4d<CG>(to, map, i, q.w_row + r, x.w, p, bar);
-                            } else {
-                                tma_3d<CG>(to, map, i, x.row + r, p, bar);
-                            }
+                            if (op == 0) tma_3d<CG>(to, map, r, i, p, bar);
+                            else if (MODE == kRows) tma_4d<CG>(to, map, i, q.w_row + r, x.w, p, bar);
+                            else if (MODE == kWeights) tma_3d<CG>(to, map, i, x.row + r, p, bar);
+                            else tma_4d<CG>(to, map, r, q.w_row + i, x.w, p, bar);
                         }
+                    }
                     if (++s == (uint32_t)q.stages) { s = 0; ph ^= 1u; }
                 }
             }
@@ -246,11 +302,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
     } else if (warp == 1) {
         // ------------------------------------------------------------ products, by one thread of the leader
         if (rank == 0) {
-            Walk<CG, MODE> walk(q, first);
+            Walk<CG, MODE> walk(q, first, stride);
             uint32_t done = 0, turn = 0;     // stages; parts, which take the two accumulators in turn
             bool ok = true;
             const uint32_t kind = product_kind(128 * CG, q.width, A_R, B_R);
-            while (walk.next(x, stride)) {
+            while (walk.next(x)) {
                 const int parts = (x.steps + q.part_steps - 1) / q.part_steps;
                 if (elect()) {
                     uint32_t s = done % q.stages, ph = done / q.stages & 1u;
@@ -270,10 +326,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                                 for (int pa = 0; pa <= sum; ++pa) {
                                     const int pb = sum - pa;
                                     if (pa >= PA || pb >= PB) continue;
-                                    const uint64_t da = operand(a0 + pa * 2 * kBlock, A_R, kBlock), db = operand(b0 + pb * blocks_b * kBlock, B_R, kBlock);
+                                    const uint32_t a = a0 + pa * 2 * kBlock;
+                                    const uint64_t da = MODE == kRows ? operand_plain(a, 128 * 16, 128) : MODE == kWeights ? operand_plain(a, 128, 64 * 16) : operand(a, true, 0);
+                                    const uint64_t db = operand(b0 + pb * blocks_b * kBlock, B_R, kBlock);
+                                    constexpr uint32_t kStepA = MODE == kRows ? 2 * 128 * 16 : MODE == kWeights ? 2 * 128 : step16(true);
 #pragma unroll
                                     for (int c = 0; c < kStep / 16; ++c) {
-                                        mma<CG>(d, da + (uint64_t)(c * step16(A_R) >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, add);
+                                        mma<CG>(d, da + (uint64_t)(c * kStepA >> 4), db + (uint64_t)(c * step16(B_R) >> 4), kind, add);
                                         add = true;
                                     }
                                 }
@@ -291,47 +350,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
             if (!ok) *dead_v = 1;
         }
     } else if (warp >= kFirstOutWarp) {
-        // ------------------------------------------------------------ results: four warps for either half of the columns
-        Walk<CG, MODE> walk(q, first);
-        const int quarter = warp & 3, half = (warp - kFirstOutWarp) >> 2, columns = q.width / 2;
-        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * columns;
-        uint32_t turn = 0, puts = 0;
-        const uint32_t put = smem + q.stages * q.stage_bytes + (warp - kFirstOutWarp) * 2 * kPut;
+        // ------------------------------------------------------------ results: a warp's quarter of the rows by its part of the columns
+        Walk<CG, MODE> walk(q, first, stride);
+        const int quarter = warp & 3, share = (warp - kFirstOutWarp) >> 2, columns = q.width / (kOutWarps / 4);
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + share * columns;
+        uint32_t turn = 0;
+        const uint32_t put = smem + q.stages * q.stage_bytes + (warp - kFirstOutWarp) * kPut;
         bool ok = true;
-        while (walk.next(x, stride)) {
+        while (walk.next(x)) {
             const int parts = (x.steps + q.part_steps - 1) / q.part_steps;
-            const int col = x.c0 + half * columns;       // the first of the thread's columns
+            const int col = x.c0 + share * columns;      // the first of the thread's columns
             const int j = x.row + rank * 128 + quarter * 32 + lane;          // the packed row (weights': none)
             // workers' rows begin at multiples of 64: a warp's are all this worker's, or another's or nobody's
             const bool mine = MODE != kWeights && j < x.row_end;
-            float acc[128];
+            f32x2 acc[kCols / 2];                        // pairs of columns
 #pragma unroll
-            for (int e = 0; e < 128; ++e) acc[e] = 0.0f;
-            if (MODE == kRows && q.add && mine && x.steps > 0) {
-                const float* from = q.dx + ((long long)x.split * q.row0[q.N] + j) * q.dx_pitch + col;
-#pragma unroll
-                for (int c = 0; c < 128; c += 8) {
-                    if (c < columns) {
-                        uint32_t o[8];
-                        load32(from + c, o);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[c + e] = __uint_as_float(o[e]);
-                    }
-                }
-            }
+            for (int e = 0; e < kCols / 2; ++e) acc[e] = 0;
             for (int part = 0; part < parts; ++part) {
                 const uint32_t n = turn + part, buf = n & 1u;
                 ok = mbar_wait(acc_full(buf), n >> 1 & 1u, dead_v) || give_up(54);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < 128; c += 16) {
+                for (int c = 0; c < kCols; c += 16) {
                     if (c < columns) {
                         uint32_t v[16];
                         tmem_load16(lanes + buf * 256 + c, v);
                         tmem_load_wait(v);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[c + e] += __uint_as_float(v[e]);
+                        for (int e = 0; e < 8; ++e) acc[c / 2 + e] = add2(acc[c / 2 + e], pair(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])));
                     }
                 }
                 tc_fence_before();
@@ -344,43 +391,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                 if (!q.scaled) {
                     const float scale = parts > 0 ? 1.0f / (float)q.count[x.w] : 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 128; ++e) acc[e] *= scale;
+                    for (int e = 0; e < kCols / 2; ++e) acc[e] = mul2(acc[e], pair(scale, scale));
                 }
-                const int v = q.v0 + x.h0 + rank * 128 + quarter * 32 + lane;
+                const int v = q.v0 + x.h0 + rank * 128 + quarter * 32;
+                if (v >= q.v_end) continue;
                 if (q.vec) {
-                    if (v < q.v_end) {
-                        unsigned char* to = q.dw + (x.w * q.dw_stride + v * q.dw_pitch + col) * OB;
-                        constexpr int kLane = 32 / OB;   // 32 bytes a store, or 16
 #pragma unroll
-                        for (int c = 0; c < 128; c += kLane) {
-                            if (c < columns) {
-                                uint32_t o[8];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    o[e] = OB == 4 ? __float_as_uint(acc[c + (OB == 4 ? e : 0)]) : combo_step::pack_bf16(acc[c + (OB == 4 ? 0 : 2 * e)], acc[c + (OB == 4 ? 0 : 2 * e + 1)]);
-                                if (col + c + kLane <= q.K && q.vec == 32) {
-                                    store32(to + c * OB, o);
-                                } else if (col + c < q.K) {
-                                    // K is a multiple of what 16 bytes hold
-                                    *reinterpret_cast<uint4*>(to + c * OB) = make_uint4(o[0], o[1], o[2], o[3]);
-                                    if (col + c + kLane / 2 < q.K) *reinterpret_cast<uint4*>(to + c * OB + 16) = make_uint4(o[4], o[5], o[6], o[7]);
-                                }
-                            }
-                        }
-                    }
+                    for (int c = 0; c < kCols; c += 128 / OB)
+                        if (c < columns && col + c < q.K) put_box<OB>(put, acc, c, lane, [&] { tma_store_3d(&maps.out, put, col + c, v, x.w); });
                 } else {
                     // off 16-byte boundaries: lots of 32 x 32 are turned and stored a line at a time
                     float* turned = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + q.stages * q.stage_bytes + (warp - kFirstOutWarp) * kTurn);
-                    const int base = q.v0 + x.h0 + rank * 128 + quarter * 32, lines = min(q.v_end - base, 32);
+                    const int lines = min(q.v_end - v, 32);
 #pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
+                    for (int c = 0; c < kCols; c += 32) {
                         if (c < columns) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) turned[lane * 33 + e] = acc[c + e];
+                            for (int e = 0; e < 16; ++e) {
+                                turned[lane * 33 + 2 * e] = lo_of(acc[c / 2 + e]);
+                                turned[lane * 33 + 2 * e + 1] = hi_of(acc[c / 2 + e]);
+                            }
                             __syncwarp();
-                            if (col + c + lane < q.K)
+                            if (c + lane < columns && col + c + lane < q.K)
                                 for (int line = 0; line < lines; ++line)
-                                    combo_step::Elem<OB>::put(q.dw + (x.w * q.dw_stride + (base + line) * q.dw_pitch + col + c + lane) * OB, turned[line * 33 + lane]);
+                                    combo_step::Elem<OB>::put(q.dw + (x.w * q.dw_stride + (v + line) * q.dw_pitch + col + c + lane) * OB, turned[line * 33 + lane]);
                             __syncwarp();
                         }
                     }
@@ -392,125 +426,107 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                     const int left = q.V - (q.v0 + col);
                     if (left < columns) {
 #pragma unroll
-                        for (int e = 0; e < 128; ++e)
-                            if (e >= left) acc[e] = -INFINITY;
+                        for (int e = 0; e < kCols; e += 2)
+                            acc[e / 2] = pair(e < left ? lo_of(acc[e / 2]) : -INFINITY, e + 1 < left ? hi_of(acc[e / 2]) : -INFINITY);
                     }
                     float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
+                    for (int c = 0; c < kCols; c += 32) {
                         if (c < columns) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) most[e & 3] = fmaxf(most[e & 3], acc[c + e]);
+                            for (int e = 0; e < 16; ++e) most[e & 3] = fmaxf(most[e & 3], fmaxf(lo_of(acc[c / 2 + e]), hi_of(acc[c / 2 + e])));
                         }
                     }
-                    const float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), zero = m == -INFINITY ? 0.0f : m;
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    // exponents of two against the largest one as it is rounded here, so that its rounding does not enter the sum
+                    const float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * kLog2E, zero = m == -INFINITY ? 0.0f : -m;
+                    f32x2 sum[2] = {0, 0};
 #pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
+                    for (int c = 0; c < kCols; c += 32) {
                         if (c < columns) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) sum[e & 3] += exp2_fast((acc[c + e] - zero) * kLog2E);
+                            for (int e = 0; e < 16; ++e) {
+                                const f32x2 x2 = fma2(acc[c / 2 + e], pair(kLog2E, kLog2E), pair(zero, zero));
+                                sum[e & 1] = add2(sum[e & 1], pair(exp2_fast(lo_of(x2)), exp2_fast(hi_of(x2))));
+                            }
                         }
                     }
-                    q.part[((q.v0 + col) / columns) * q.row_cap + j] = make_float2(m, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                    sum[0] = add2(sum[0], sum[1]);
+                    q.part[((q.v0 + col) / columns) * q.row_cap + j] = make_float2(m, lo_of(sum[0]) + hi_of(sum[0]));
                     const int at = q.label[j] - q.v0 - col;
                     if (__any_sync(0xffffffffu, at >= 0 && at < columns)) {
                         float z = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 128; ++e)
-                            if (e == at) z = acc[e];
+                        for (int e = 0; e < kCols; ++e)
+                            if (e == at) z = e & 1 ? hi_of(acc[e / 2]) : lo_of(acc[e / 2]);
                         if (at >= 0 && at < columns) q.own[j] = z;
                     }
                 } else if constexpr (MODE == kGrad) {
                     const int left = q.v_end - (q.v0 + col), label = q.label[j];
-                    const float lse = label >= 0 ? q.lse[j] : 0.0f;
+                    const float lse = label >= 0 ? -q.lse[j] * kLog2E : 0.0f;
                     const int at = label - q.v0 - col;
+                    const bool here = label >= 0 && at >= 0 && at < columns;
+                    const bool any = __any_sync(0xffffffffu, here), all = __all_sync(0xffffffffu, label >= 0) && left >= columns;
+                    float g = 1.0f;
+                    if (q.scaled) g = label >= 0 ? q.g[j] : 0.0f;
+                    unsigned char* to = q.d + ((long long)(col / 8) * q.row_cap + j) * 16;
+                    float own = 0.0f;                // d of the row's label
+                    // 32 classes at a time, from the logits to their places in scratch: 16 bytes a lane, a warp's side by side
 #pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
+                    for (int c = 0; c < kCols; c += 32) {
                         if (c < columns) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) acc[c + e] = exp2_fast((acc[c + e] - lse) * kLog2E);
-                        }
-                    }
-                    const bool here = label >= 0 && at >= 0 && at < columns;
-                    const bool any = __any_sync(0xffffffffu, here);
-                    if (any) {
+                            for (int e = c / 2; e < c / 2 + 16; ++e) {
+                                const f32x2 x2 = fma2(acc[e], pair(kLog2E, kLog2E), pair(lse, lse));
+                                acc[e] = pair(exp2_fast(lo_of(x2)), exp2_fast(hi_of(x2)));
+                            }
+                            if (any) {
 #pragma unroll
-                        for (int e = 0; e < 128; ++e)
-                            if (e == at) acc[e] -= 1.0f;
-                    }
-                    if (q.scaled) {
-                        const float g = label >= 0 ? q.g[j] : 0.0f;
+                                for (int e = c; e < c + 32; e += 2)
+                                    acc[e / 2] = add2(acc[e / 2], pair(e == at ? -1.0f : 0.0f, e + 1 == at ? -1.0f : 0.0f));
+                            }
+                            if (q.scaled) {
 #pragma unroll
-                        for (int e = 0; e < 128; ++e) acc[e] *= g;
-                    }
-                    // rows without a label and classes that are not there: 0, whatever the product is
-                    if (left < columns) {
+                                for (int e = c / 2; e < c / 2 + 16; ++e) acc[e] = mul2(acc[e], pair(g, g));
+                            }
+                            if (!all) {
+                                // rows without a label and classes that are not there: 0, whatever the product is
 #pragma unroll
-                        for (int e = 0; e < 128; ++e)
-                            if (e >= left) acc[e] = 0.0f;
-                    }
-                    if (!__all_sync(0xffffffffu, label >= 0)) {
+                                for (int e = c; e < c + 32; e += 2)
+                                    acc[e / 2] = pair(label >= 0 && e < left ? lo_of(acc[e / 2]) : 0.0f, label >= 0 && e + 1 < left ? hi_of(acc[e / 2]) : 0.0f);
+                            }
+                            if (any) {
 #pragma unroll
-                        for (int e = 0; e < 128; ++e) acc[e] = label >= 0 ? acc[e] : 0.0f;
-                    }
-                    if (any) {
-                        float rest = 0.0f;
+                                for (int e = c; e < c + 32; ++e)
+                                    if (e == at) own = e & 1 ? hi_of(acc[e / 2]) : lo_of(acc[e / 2]);
+                            }
 #pragma unroll
-                        for (int e = 0; e < 128; ++e)
-                            if (e == at) rest = acc[e] - combo_step::widen_lo(combo_step::pack_bf16(acc[e], 0.0f));
-                        if (here) q.own[j] = rest;
-                    }
-                    // 64 columns of a plane at a time, in TMA's order: 16 bytes of a row at (their number xor the row's) of its 128
+                            for (int p = 0; p < OB; ++p) {
 #pragma unroll
-                    for (int p = 0; p < OB; ++p) {
-#pragma unroll
-                        for (int c = 0; c < 128; c += 64) {
-                            if (c < columns) {
-                                const uint32_t place = put + (puts & 1u) * kPut;
-                                if (elect()) tma_store_wait_read<1>();
-                                __syncwarp();
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) {
+                                for (int k = c; k < c + 32; k += 8) {
                                     uint32_t o[4];
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) {
-                                        float &lo = acc[c + k * 8 + 2 * e], &hi = acc[c + k * 8 + 2 * e + 1];
-                                        o[e] = combo_step::pack_bf16(lo, hi);
-                                        if (p + 1 < OB) {
-                                            lo -= combo_step::widen_lo(o[e]);
-                                            hi -= combo_step::widen_hi(o[e]);
-                                        }
+                                        f32x2& v = acc[k / 2 + e];
+                                        o[e] = combo_step::pack_bf16(lo_of(v), hi_of(v));
+                                        if (p + 1 < OB) v = add2(v, neg2(pair(combo_step::widen_lo(o[e]), combo_step::widen_hi(o[e]))));
                                     }
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + lane * 128 + ((k ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]),
-                                                 "r"(o[2]), "r"(o[3])
-                                                 : "memory");
+                                    *reinterpret_cast<uint4*>(to + ((long long)p * q.d_blocks + k / 8) * q.row_cap * 16) = make_uint4(o[0], o[1], o[2], o[3]);
                                 }
-                                fence_async();
-                                __syncwarp();
-                                if (elect()) tma_store_3d(&maps.d, place, col + c, j - lane, p);
-                                __syncwarp();
-                                ++puts;
                             }
                         }
                     }
+                    if (here) q.own[j] = own - combo_step::widen_lo(combo_step::pack_bf16(own, 0.0f));
                 } else {
-                    float* to = q.dx + ((long long)x.split * q.row0[q.N] + j) * q.dx_pitch + col;
+                    const int y = x.split * q.row0[q.N] + j - lane;
                     if (!q.add || x.steps > 0) {
 #pragma unroll
-                        for (int c = 0; c < 128; c += 8) {
-                            if (c < columns) {
-                                uint32_t o[8];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(acc[c + e]);
-                                store32(to + c, o);
-                            }
-                        }
+                        for (int c = 0; c < kCols; c += 32)
+                            if (c < columns) put_box<4>(put, acc, c, lane, [&] { q.add ? tma_add_3d(&maps.out, put, col + c, y, 0) : tma_store_3d(&maps.out, put, col + c, y, 0); });
                     }
                 }
             }
         }
-        if (MODE == kGrad) tma_store_wait();
+        if (MODE == kRows || MODE == kWeights) tma_store_wait();
         if (!ok) *dead_v = 1;
     }
     tc_fence_before();

@@ -107,7 +107,13 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t fr
                  : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-template <int LEFT> __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+// The same, added to what is there.
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t from, int x, int y, int z) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(from), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // what threads wrote to shared memory becomes visible to the tensor cores and to TMA
@@ -195,6 +201,11 @@ __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::
 __device__ __forceinline__ uint64_t operand(uint32_t addr, bool along_r, uint32_t block) {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)((along_r ? 16u : block) >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 |
            1ull << 46 | 2ull << 61;
+}
+// Shared-memory operand without swizzle: pieces of 8 x 16 bytes, 128 bytes each, `next_r` bytes from one to the next along r,
+// `next_i` along its own index (either index may be the one that 16 bytes run along).
+__device__ __forceinline__ uint64_t operand_plain(uint32_t addr, uint32_t next_r, uint32_t next_i) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(next_r >> 4) << 16 | (uint64_t)(next_i >> 4) << 32 | 1ull << 46;
 }
 // bytes from one step of 16 values of r to the next
 __host__ __device__ constexpr uint32_t step16(bool along_r) { return along_r ? 32u : 2048u; }
