@@ -6,8 +6,9 @@
 // before xor the next word: seed, round | worker, site, place; one draw of 64 bits serves four neighbours of a row.  A place counts
 // within the worker's own rows, so a worker's mask does not depend on the other workers or on which GPU holds it.
 //
-// Bound by HBM: two passes over the data (three with a residual).  A vector of 16 bytes costs two draws of about 30 instructions
-// for bfloat16, one for float, and as many again for the elements: half of what can be issued while its bytes pass.
+// Bound by HBM: two passes over the data (three with a residual).  A draw takes some 25 instructions and an element five, which is
+// most of what can be issued while its bytes pass; so a warp takes several rows for one search of their worker and one key, and
+// places within a row are counted in 32 bits.
 #include "host_common.h"
 #include "step_common.cuh"
 
@@ -24,7 +25,9 @@ struct Dropout {
     uint64_t first;                              // the generator's state behind the seed
     uint32_t round, site, worker0, threshold;    // threshold << 16 of the bits; none_left: nothing is kept
     float scale;
-    int N, none_left, lanes, pieces;             // lanes for a row, pieces of a row (a warp's units are 32 / lanes rows by one piece)
+    int N, none_left, lanes, rounds;             // lanes for a row; rounds of loads that they need for it
+    int lots, width;                             // draws of a row; 16 bytes (or four elements) of it
+    long long share;                             // rounds of a warp
 };
 
 __host__ __device__ __forceinline__ uint64_t splitmix_step(uint64_t z) {
@@ -34,104 +37,167 @@ __host__ __device__ __forceinline__ uint64_t splitmix_step(uint64_t z) {
     return z ^ (z >> 31);
 }
 
-// The worker that row m belongs to, or -1.
-__device__ __forceinline__ int owner(const int64_t* begin, int N, long long m) {
-    if (!begin) return 0;
-    int lo = 0, hi = N;                          // the last w with begin[w] <= m
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__ldg(reinterpret_cast<const long long*>(begin) + mid) <= m) lo = mid;
-        else hi = mid - 1;
+// Rows of one worker: first and end; the key of its draws.  A row of no worker is in a range without a key.
+struct Owner {
+    long long first, end;
+    uint64_t key;
+    bool some;
+};
+// The whole warp asks for rows m of its lanes, the first lane's being the least: 32 borders at a time lead to that lane's worker,
+// and lanes beyond it go on by halves.
+__device__ __forceinline__ Owner owner_of(const Dropout& p, long long m) {
+    Owner o;
+    int w = 0;
+    o.first = 0;
+    o.end = p.M;
+    o.some = true;
+    if (p.begin) {
+        const long long* begin = reinterpret_cast<const long long*>(p.begin);
+        const long long m0 = __shfl_sync(0xffffffffu, m, 0);
+        int lo = -1, hi = p.N;                   // the last w with begin[w] <= m; -1: none
+        while (lo < hi) {
+            const int step = (hi - lo + 31) / 32, at = lo + 1 + (threadIdx.x & 31) * step;
+            const unsigned below = __ballot_sync(0xffffffffu, at <= hi && __ldg(begin + min(at, p.N)) <= m0);
+            if (below == 0u) break;
+            const int k = 31 - __clz(below);
+            hi = min(hi, lo + (k + 1) * step);
+            lo = lo + 1 + k * step;
+        }
+        hi = p.N;
+        if (lo < p.N && __ldg(begin + lo + 1) > m) hi = lo;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (__ldg(begin + mid) <= m) lo = mid;
+            else hi = mid - 1;
+        }
+        w = lo;
+        o.some = lo >= 0 && lo < p.N;
+        if (o.some) o.first = __ldg(begin + lo);
+        if (lo < p.N) o.end = __ldg(begin + lo + 1);
     }
-    return lo < N && __ldg(reinterpret_cast<const long long*>(begin) + lo) <= m ? lo : -1;
+    o.key = splitmix_step(splitmix_step(p.first ^ ((uint64_t)p.round << 32 | (uint32_t)(p.worker0 + w))) ^ (0x8000000000000000ull | p.site));
+    return o;
 }
 
-constexpr int kThreads = 256, kUnroll = 4;
+constexpr int kThreads = 256, kCtas = 4;     // CTAs on an SM
+// Loads under way of a lane: with a residual twice as many bytes to a load.  Measured (4 / 2): 15001 x 4096 bfloat16 49 / 55 us
+// (5.0 TB/s), with a residual 35395 x 1024 44 / 41 (5.3 TB/s).
+__host__ __device__ constexpr int unroll(bool res) { return res ? 2 : 4; }
+
+// Keeps and drops the elements of a lot of V from draw `place` on; f becomes residual + kept.
+template <int V, bool RES> __device__ __forceinline__ void drop(float (&f)[V], const float (&g)[V], const Dropout& p, uint64_t key, uint64_t place) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) {
+        const combo_step::f32x2 t = combo_step::mul2(combo_step::pair(f[e], f[e + 1]), combo_step::pair(p.scale, p.scale));
+        f[e] = combo_step::lo_of(t);
+        f[e + 1] = combo_step::hi_of(t);
+    }
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+        const uint64_t z = splitmix_step(key ^ (place + h));
+        const uint32_t half[2] = {(uint32_t)z, (uint32_t)(z >> 32)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = e & 1 ? half[e >> 1] : half[e >> 1] << 16;      // the element's 16 bits in front
+            const float t = bits >= p.threshold && !p.none_left ? f[h * 4 + e] : 0.0f;
+            f[h * 4 + e] = RES ? t + g[h * 4 + e] : t;
+        }
+    }
+}
 
 // EB bytes an element.  VEC: a lane's lot is 16 aligned bytes; else four elements, one at a time.
-template <int EB, bool VEC, bool RES> __global__ void __launch_bounds__(kThreads) k_dropout(const Dropout p) {
-    constexpr int V = VEC ? 16 / EB : 4, H = V / 4;
+template <int EB, bool VEC, bool RES> __global__ void __launch_bounds__(kThreads, kCtas) k_dropout(const Dropout p) {
+    constexpr int V = VEC ? 16 / EB : 4, H = V / 4, U = unroll(RES);
     combo_step::pdl_release();
-    const int lane = threadIdx.x & 31;
-    const long long lots = (p.n + 3) / 4, width = (p.n + V - 1) / V;       // draws and lots of a row
-    const int per_warp = 32 / p.lanes;
-    const long long units = (p.M + per_warp - 1) / per_warp * p.pieces;
+    const int lane = threadIdx.x & 31, side = 32 / p.lanes;      // rows side by side in a warp
+    // a warp's rounds: several rows' or a part of one's
+    const long long all = (p.M + side - 1) / side * p.rounds, from = ((long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * p.share;
+    const long long to = min(from + p.share, all);
     combo_step::pdl_wait();
-    for (long long u = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * (kThreads / 32)) {
-        const long long rows = p.pieces == 1 ? u : u / p.pieces;
-        const long long m = rows * per_warp + lane / p.lanes, v0 = (u - rows * p.pieces) * (kUnroll * 32) + lane % p.lanes;
-        if (m >= p.M) continue;
+    if (from >= to) return;
+    long long m = from / p.rounds * side + lane / p.lanes;
+    int round = (int)(from % p.rounds);
+    Owner o = {0, -1, 0, false};
+    for (long long t = from; t < to; ++t) {
         const unsigned char* x = p.x + m * p.x_pitch * EB;
         const unsigned char* r = RES ? p.residual + m * p.r_pitch * EB : nullptr;
         unsigned char* y = p.y + m * p.y_pitch * EB;
-        const int w = owner(p.begin, p.N, m);
-        if (w < 0) continue;
-        const uint64_t key = splitmix_step(splitmix_step(p.first ^ ((uint64_t)p.round << 32 | (uint32_t)(p.worker0 + w))) ^
-                                           (0x8000000000000000ull | p.site));
-        const uint64_t place = (uint64_t)(m - (p.begin ? __ldg(reinterpret_cast<const long long*>(p.begin) + w) : 0)) * lots;
-        uint4 a[kUnroll], b[kUnroll];
-        if (VEC) {
+        const int v0 = round * U * p.lanes + lane % p.lanes;
+        uint4 a[U], b[U];
+        const bool whole = VEC && m < p.M && (long long)(v0 + (U - 1) * p.lanes + 1) * V <= p.n;
+        if (whole) {
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                const long long v = v0 + k * p.lanes;
-                if ((v + 1) * V <= p.n) {
-                    a[k] = *reinterpret_cast<const uint4*>(x + v * 16);
-                    if (RES) b[k] = *reinterpret_cast<const uint4*>(r + v * 16);
+            for (int k = 0; k < U; ++k) {
+                a[k] = *reinterpret_cast<const uint4*>(x + (uint32_t)(v0 + k * p.lanes) * 16ull);
+                if (RES) b[k] = *reinterpret_cast<const uint4*>(r + (uint32_t)(v0 + k * p.lanes) * 16ull);
+            }
+        }
+        // the loads are under way while the worker is looked for
+        if (__any_sync(0xffffffffu, m >= o.end && m < p.M)) o = owner_of(p, m);
+        if (o.some && m < p.M) {
+            const uint64_t place = (uint64_t)(m - o.first) * (uint32_t)p.lots;
+            if (whole) {
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    if constexpr (VEC) {
+                        float f[V], g[V];
+                        Elem<EB>::unpack(a[k], f);
+                        if (RES) Elem<EB>::unpack(b[k], g);
+                        drop<V, RES>(f, g, p, o.key, place + (uint32_t)(v0 + k * p.lanes) * H);
+                        *reinterpret_cast<uint4*>(y + (uint32_t)(v0 + k * p.lanes) * 16ull) = Elem<EB>::pack(f);
+                    }
+                }
+            } else {
+                // the end of a row, or rows off 16-byte boundaries
+                for (int k = 0; k < U; ++k) {
+                    const int v = v0 + k * p.lanes;
+                    if (v >= p.width) break;
+                    const long long at = (long long)v * V;
+                    const int some = (int)min(p.n - at, (long long)V);
+                    float f[V], g[V];
+                    if (VEC && some == V) {
+                        if constexpr (VEC) {
+                            Elem<EB>::unpack(*reinterpret_cast<const uint4*>(x + at * EB), f);
+                            if (RES) Elem<EB>::unpack(*reinterpret_cast<const uint4*>(r + at * EB), g);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            f[e] = e < some ? Elem<EB>::get(x + (at + e) * EB) : 0.0f;
+                            g[e] = RES && e < some ? Elem<EB>::get(r + (at + e) * EB) : 0.0f;
+                        }
+                    }
+                    drop<V, RES>(f, g, p, o.key, place + (uint32_t)v * H);
+                    if (VEC && some == V) {
+                        if constexpr (VEC) *reinterpret_cast<uint4*>(y + at * EB) = Elem<EB>::pack(f);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            if (e < some) Elem<EB>::put(y + (at + e) * EB, f[e]);
+                    }
                 }
             }
         }
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const long long v = v0 + k * p.lanes;
-            if (v >= width) break;
-            const bool whole = VEC && (v + 1) * V <= p.n;
-            const int some = (int)min(p.n - v * V, (long long)V);
-            float f[V], g[V];
-            if (whole) {
-                if constexpr (VEC) {
-                    Elem<EB>::unpack(a[k], f);
-                    if (RES) Elem<EB>::unpack(b[k], g);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    f[e] = e < some ? Elem<EB>::get(x + (v * V + e) * EB) : 0.0f;
-                    if (RES) g[e] = e < some ? Elem<EB>::get(r + (v * V + e) * EB) : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < H; ++h) {
-                const uint64_t z = splitmix_step(key ^ (place + v * H + h));
-                const uint32_t half[2] = {(uint32_t)z, (uint32_t)(z >> 32)};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t bits = e & 1 ? half[e >> 1] : half[e >> 1] << 16;      // the element's 16 bits in front
-                    const float t = bits >= p.threshold && !p.none_left ? f[h * 4 + e] * p.scale : 0.0f;
-                    f[h * 4 + e] = RES ? t + g[h * 4 + e] : t;
-                }
-            }
-            if (whole) {
-                if constexpr (VEC) *reinterpret_cast<uint4*>(y + v * 16) = Elem<EB>::pack(f);
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (e < some) Elem<EB>::put(y + (v * V + e) * EB, f[e]);
-            }
+        if (++round == p.rounds) {
+            round = 0;
+            m += side;
         }
     }
 }
 
 template <int EB> cudaError_t launch(Dropout p, int sms, bool vec, cudaStream_t st) {
     const int V = vec ? 16 / EB : 4;
-    const long long width = (p.n + V - 1) / V;
-    // Lanes to a row: the fewest that take it in one piece.
+    p.lots = (int)((p.n + 3) / 4);
+    p.width = (int)((p.n + V - 1) / V);
+    const int U = unroll(p.residual != nullptr);
+    // Lanes to a row: the fewest that take it in one round of loads.  The rounds are shared out evenly to as many warps as are
+    // on the device at once.
     p.lanes = 1;
-    while (p.lanes < 32 && p.lanes * kUnroll < width) p.lanes *= 2;
-    p.pieces = (int)((width + p.lanes * kUnroll - 1) / (p.lanes * kUnroll));
-    const long long per_warp = 32 / p.lanes, units = (p.M + per_warp - 1) / per_warp * p.pieces;
-    long long grid = (units + kThreads / 32 - 1) / (kThreads / 32);
-    if (grid > (1 << 30)) grid = 1 << 30;
-    (void)sms;
+    while (p.lanes < 32 && p.lanes * U < p.width) p.lanes *= 2;
+    p.rounds = (p.width + p.lanes * U - 1) / (p.lanes * U);
+    const long long side = 32 / p.lanes, all = (p.M + side - 1) / side * p.rounds, warps = (long long)sms * kCtas * (kThreads / 32);
+    p.share = (all + warps - 1) / warps;
+    const long long grid = ((all + p.share - 1) / p.share + kThreads / 32 - 1) / (kThreads / 32);
     const dim3 g((unsigned)grid), b(kThreads);
     if (p.residual) return vec ? combo_host::launch_after(k_dropout<EB, true, true>, g, b, 0, st, p) : combo_host::launch_after(k_dropout<EB, false, true>, g, b, 0, st, p);
     return vec ? combo_host::launch_after(k_dropout<EB, true, false>, g, b, 0, st, p) : combo_host::launch_after(k_dropout<EB, false, false>, g, b, 0, st, p);
