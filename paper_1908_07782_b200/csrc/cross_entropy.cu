@@ -61,8 +61,10 @@ template <int EB, bool VEC> __device__ __forceinline__ void load_share(const uns
     constexpr int E = Elem<EB>::V;
     if (VEC) {
         const int k = (c * 32 + lane) * E;
-        if (k + E <= K) {
-            Elem<EB>::unpack(*reinterpret_cast<const uint4*>(line + (long long)k * EB), v);
+        if (K % E == 0 || k + E <= K) {
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (k < K) q = *reinterpret_cast<const uint4*>(line + (long long)k * EB);
+            Elem<EB>::unpack(q, v);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) v[e] = k + e < K ? Elem<EB>::get(line + (long long)(k + e) * EB) : 0.0f;
@@ -134,6 +136,8 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
 template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_loss(const Loss p) {
     int w;
     long long i0, i1;
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
     if (!find_rows(p, blockIdx.x, w, i0, i1)) return;
     const int rows = (int)min(i1 - i0, (long long)kR), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = lane % kR;
     const unsigned char *x0 = p.x + i0 * p.x_pitch * EB, *w0 = p.w + w * p.w_stride * EB;
@@ -196,6 +200,8 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_ba
     constexpr int E = Elem<EB>::V;
     int w;
     long long i0, i1;
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
     if (!find_rows(p, blockIdx.x, w, i0, i1)) return;
     const int rows = (int)min(i1 - i0, (long long)kR), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = lane % kR;
     const unsigned char *x0 = p.x + i0 * p.x_pitch * EB, *w0 = p.w + w * p.w_stride * EB;
@@ -252,6 +258,8 @@ template <int EB, int OB, bool VEC> __global__ void __launch_bounds__(kThreads) 
     const int w = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x;
     long long i0, i1;
+    combo_step::pdl_release();
+    combo_step::pdl_wait();
     rows_of(p, w, i0, i1);
     for (int v0 = blockIdx.y * kR; v0 < p.V; v0 += gridDim.y * kR) {
         float acc[kR][E];
@@ -259,17 +267,21 @@ template <int EB, int OB, bool VEC> __global__ void __launch_bounds__(kThreads) 
         for (int r = 0; r < kR; ++r)
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[r][e] = 0.0f;
+        // several rows' loads at once; a row without a label may hold anything (its d is 0)
+#pragma unroll 4
         for (long long i = i0 + warp; i < i1; i += kWarps) {
             const int64_t label = p.labels[i];
-            if (label < 0 || label >= p.V) continue;
-            float xv[E];
+            const bool has = label >= 0 && label < p.V;
+            float xv[E], f[kR];
             load_share<EB, VEC>(p.x + i * p.x_pitch * EB, c, lane, p.K, xv);
 #pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                const float f = p.d[i * p.V + min(v0 + r, p.V - 1)];
+            for (int r = 0; r < kR; ++r) f[r] = p.d[i * p.V + min(v0 + r, p.V - 1)];
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(f, xv[e], acc[r][e]);
-            }
+            for (int e = 0; e < E; ++e) xv[e] = has ? xv[e] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < kR; ++r)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(f[r], xv[e], acc[r][e]);
         }
         join_warps<EB, VEC>(acc, c, lane, warp, [&](int r, int k, float sum) {
             if (v0 + r < p.V && k < p.K) Elem<OB>::put(p.dw + (w * p.dw_stride + (v0 + r) * p.dw_pitch + k) * OB, sum);
@@ -280,16 +292,14 @@ template <int EB, int OB, bool VEC> __global__ void __launch_bounds__(kThreads) 
 template <int EB, bool VEC> cudaError_t launch_few(const Loss& p, int grad_bytes, cudaStream_t st) {
     const long long lots = p.M / kR + (p.N < p.M ? p.N : p.M);
     const unsigned grid = (unsigned)(lots < 1 ? 1 : lots);
-    if (!grad_bytes) {
-        if (p.M > 0) k_few_loss<EB, VEC><<<grid, kThreads, 0, st>>>(p);
-        return cudaGetLastError();
-    }
-    if (p.M > 0) k_few_back<EB, VEC><<<grid, kThreads, 0, st>>>(p);
+    if (!grad_bytes) return combo_host::launch_after(k_few_loss<EB, VEC>, dim3(grid), dim3(kThreads), 0, st, p);
+    cudaError_t e = cudaSuccess;
+    if (p.M > 0) e = combo_host::launch_after(k_few_back<EB, VEC>, dim3(grid), dim3(kThreads), 0, st, p);
+    if (e != cudaSuccess) return e;
     const unsigned classes = (unsigned)((p.V + kR - 1) / kR);
     const dim3 g((unsigned)((p.K + 32 * Elem<EB>::V - 1) / (32 * Elem<EB>::V)), classes < 65535 ? classes : 65535, (unsigned)p.N);
-    if (grad_bytes == 4) k_few_weights<EB, 4, VEC><<<g, kThreads, 0, st>>>(p);
-    else k_few_weights<EB, 2, VEC><<<g, kThreads, 0, st>>>(p);
-    return cudaGetLastError();
+    return grad_bytes == 4 ? combo_host::launch_after(k_few_weights<EB, 4, VEC>, g, dim3(kThreads), 0, st, p)
+                           : combo_host::launch_after(k_few_weights<EB, 2, VEC>, g, dim3(kThreads), 0, st, p);
 }
 
 // ---------------------------------------------------------------- packing of rows and weights for the tensor cores
@@ -610,12 +620,17 @@ size_t piece_bytes(const Plan& a, int N, size_t classes, bool back, bool direct)
 Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_bytes) {
     Plan a = {};
     const bool back = grad_bytes != 0;
-    a.few = M == 0 || (V * K <= (1 << 17) && M * V <= (1 << 24));
+    // Few multiply-adds: one launch, or two, against four and seven.  Measured, 8 workers, few / tensor cores: loss of 1336 rows, 256 ->
+    // 64, floats 11.9 / 23.9 us, 512 -> 256 54 / 41; bfloat16 11.3 / 17.0, 47 / 20; gradients 28.6 / 53.5, 147 / 82 and 36 / 38,
+    // 160 / 45; of 8000 rows, 256 -> 10, 86 / 84 and 113 / 46.
+    a.few = M == 0 || (M <= 2048 && V * K <= (elem_bytes == 4 ? 1 << 15 : 1 << 14));
     if (a.few) {
         a.total = 256 + (back ? (size_t)M * V * 4 : 0);
         return a;
     }
-    a.cg = M / N > 128 ? 2 : 1;
+    // Pairs of CTAs halve what a product takes from L2, single ones waste less of ragged rows.  Measured (pairs / single), gradients:
+    // 8 x 250 rows, 256 -> 1000, floats 91 / 74 us, bfloat16 46 / 43; 512 -> 16000 853 / 928 and 189 / 203.
+    a.cg = M / N > 128 && V * K > (1 << 19) ? 2 : 1;
     a.planes = elem_bytes == 4 ? 3 : 1;
     a.d_planes = elem_bytes == 4 ? 3 : grad_bytes == 4 ? 2 : 1;
     a.kp = (int)up(K, 64);
@@ -764,7 +779,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.dw = p.dw;
     q.dw_pitch = p.dw_pitch;
     q.dw_stride = p.dw_stride;
-    q.part_steps = EB == 4 ? 1 : 16;
+    q.part_steps = EB == 4 ? 2 : 16;
     q.dx_pitch = dx_pitch;
     q.split_steps = (int)(piece < up(p.V, 64) ? piece : up(p.V, 64)) / kStep;
     const long long row_tiles = p.M / s.height + (p.N < p.M ? p.N : p.M);          // at most

@@ -11,7 +11,7 @@
 //
 // A lane of TMEM is a row of results, so the softmax needs no exchange between threads: a thread holds 128 logits of one row.
 // Floats are products of planes: x0 w0 + (x0 w1 + x1 w0) + (x0 w2 + x1 w1 + x2 w0); what is left out is below 2^-24 of a product.
-// The tensor cores truncate at every addition of 16 products, so only `part_steps` stages of 64 are summed there (floats: one, with the
+// The tensor cores truncate at every addition of 16 products, so only `part_steps` stages of 64 are summed there (floats: two, with the
 // small products first), and the parts are added with rounding in the registers of the warps that take the results.
 #pragma once
 #include "tensor_core.cuh"
