@@ -4,12 +4,13 @@ synchronization round mixes the models (segmented gossip).
 All workers' parameters are one flat [N][P] array, their gradients another; every layer is a view into it.  One
 round is
 
-    products grouped by worker -> group norm with SiLU -> products -> loss      forward
+    products grouped by worker -> group norm with SiLU -> dropout                forward
+    combo_grouped_cross_entropy   the classifier and its loss, the logits never kept
     the same backwards, gradients written into the flat gradient array
     combo_grad_clip            every worker's gradient clipped by its norm over all its tensors
     combo_segment_aggregate_sgd  the SGD step and the segment-wise aggregation with R peers in one pass
 
-    python examples/local_step.py [--workers 8] [--rounds 30] [--dtype bf16]
+    python examples/local_step.py [--workers 8] [--rounds 30] [--dtype bf16] [--dropout 0.1]
 """
 from __future__ import annotations
 
@@ -26,9 +27,10 @@ import paper_1908_07782_b200 as combo  # noqa: E402
 class Workers:
     """N copies of a two-layer classifier (n_in -> width, group norm, SiLU, width -> classes), each on its own samples."""
 
-    def __init__(self, counts, n_in, width, classes, groups, dtype=torch.float32, device="cuda", seed=0):
+    def __init__(self, counts, n_in, width, classes, groups, dtype=torch.float32, device="cuda", seed=0,
+                 dropout=0.0):
         self.N, self.n_in, self.width, self.classes, self.groups = len(counts), n_in, width, classes, groups
-        self.dtype, self.device = dtype, torch.device(device)
+        self.dtype, self.device, self.dropout, self.seed = dtype, torch.device(device), dropout, seed
         shapes = {"w1": (width, n_in), "gamma": (width,), "beta": (width,), "w2": (classes, width)}
         self.places, at = {}, 0
         for name, shape in shapes.items():
@@ -54,10 +56,13 @@ class Workers:
             return torch.empty(M, n, dtype=t, device=self.device)
 
         self.h, self.a, self.da, self.dh = rows(width), rows(width), rows(width), rows(width)
-        self.logits, self.dlogits = rows(classes), rows(classes)
+        self.loss, self.lse = torch.empty(M, device=self.device), torch.empty(M, device=self.device)
         self.mean, self.rstd = rows(groups, torch.float32), rows(groups, torch.float32)
         self.scratch = torch.empty(combo.combo_group_norm_scratch_bytes(M, 1, width, groups), dtype=torch.uint8,
                                    device=self.device)
+        size = 4 if dtype == torch.float32 else 2
+        need = max(combo.combo_grouped_cross_entropy_scratch_bytes(self.N, M, width, classes, size, grad) for grad in (0, 4))
+        self.loss_scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
         # one entry for each layer of each worker; both arrays keep their places from step to step
         offsets = torch.tensor([w * self.P + a for w in range(self.N) for a, _, _ in self.places.values()]) * 4
         lengths = [n for _ in range(self.N) for _, n, _ in self.places.values()]
@@ -75,34 +80,39 @@ class Workers:
         part = flat[:, at:at + n]
         return part if len(shape) == 1 else part.unflatten(1, shape)
 
-    def forward(self, x, flat):
+    def drop(self, t, rnd):
+        """Dropout in place: of the activations, and, with the same mask, of their gradient."""
+        if self.dropout:
+            combo.combo_dropout(t, None, t, self.begin, self.dropout, self.seed, rnd)
+
+    def forward(self, x, flat, rnd=0):
+        """What the classifier sees of every sample."""
         one = lambda t: t.view(self.M, 1, self.width)  # noqa: E731  a sample is one position
         combo.combo_grouped_linear(x, self.view(flat, "w1"), self.h, self.begin)
         combo.combo_group_norm(one(self.h), one(self.a), self.view(flat, "gamma"), self.view(flat, "beta"), self.begin,
                                self.groups, 1e-5, combo.ACT_SILU, self.mean, self.rstd, self.scratch)
-        combo.combo_grouped_linear(self.a, self.view(flat, "w2"), self.logits, self.begin)
-        return self.logits
+        self.drop(self.a, rnd)
+        return self.a
 
-    def backward(self, x, labels, flat):
-        """Gradients of every worker's mean cross-entropy, into the flat gradient array."""
+    def backward(self, x, labels, flat, rnd=0):
+        """Every sample's loss, and gradients of every worker's mean into the flat gradient array."""
         one = lambda t: t.view(self.M, 1, self.width)  # noqa: E731
-        d = torch.softmax(self.logits.float(), 1)
-        d[torch.arange(self.M, device=self.device), labels] -= 1.0
-        owner = torch.searchsorted(self.begin, torch.arange(self.M, device=self.device), right=True) - 1
-        self.dlogits.copy_(d / self.sizes[owner, None])
-        combo.combo_grouped_linear_grad_weight(self.dlogits, self.a, self.view(self.grads, "w2"), self.begin)
-        combo.combo_grouped_linear_grad_input(self.dlogits, self.view(flat, "w2"), self.da, self.begin)
+        w2 = self.view(flat, "w2")
+        combo.combo_grouped_cross_entropy(self.a, w2, labels, self.loss, self.lse, self.begin, self.loss_scratch)
+        combo.combo_grouped_cross_entropy_backward(self.a, w2, labels, self.lse, None, self.da, self.view(self.grads, "w2"), self.begin,
+                                                   self.loss_scratch)
+        self.drop(self.da, rnd)
         combo.combo_group_norm_backward(one(self.da), one(self.h), one(self.dh), self.view(flat, "gamma"), self.view(flat, "beta"),
                                         self.begin, self.groups, combo.ACT_SILU, self.mean, self.rstd,
                                         self.view(self.grads, "gamma"), self.view(self.grads, "beta"), self.scratch)
         combo.combo_grouped_linear_grad_weight(self.dh, x, self.view(self.grads, "w1"), self.begin)
+        return self.loss
 
     def step(self, x, labels, lr, max_norm, rnd, segments, replicas, seed=1):
         """One round: local step of every worker, then the gossip round.  Returns the loss over all samples."""
         flat = self.params if self.dtype == torch.float32 else self.params.to(self.dtype)
-        self.forward(x, flat)
-        loss = torch.nn.functional.cross_entropy(self.logits.float(), labels)
-        self.backward(x, labels, flat)
+        self.forward(x, flat, rnd)
+        loss = self.backward(x, labels, flat, rnd).mean()
         combo.combo_grad_clip(self.tensors, self.outs, self.starts, self.first, len(self.tensors), self.N, self.total, 4,
                               max_norm, self.norm, self.coef, self.clip_scratch)
         idx = torch.empty((self.N, segments, replicas), dtype=torch.int32, device=self.device)
@@ -133,11 +143,12 @@ def main(argv=None):
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="f32")
     ap.add_argument("--lr", type=float, default=0.5)
     ap.add_argument("--max-norm", type=float, default=1.0)
+    ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args(argv)
     counts = [100 + (37 * w) % 150 for w in range(a.workers)]
     dtype = torch.float32 if a.dtype == "f32" else torch.bfloat16
     x, y = samples(counts, 64, 10)
-    w = Workers(counts, 64, 256, 10, 8, dtype)
+    w = Workers(counts, 64, 256, 10, 8, dtype, dropout=a.dropout)
     losses = []
     for r in range(a.rounds):
         loss = w.step(x.to(dtype), y, a.lr, a.max_norm, r, segments=4, replicas=min(2, a.workers - 1))

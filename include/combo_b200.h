@@ -481,8 +481,23 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  * other in a wider array).  A NaN or infinity reaches the results that its row and its
  * worker's weights enter, no others.  Results do not change from run to run.
  *
+ * Arithmetic: logits, exponentials and sums in binary32, relative to the row's largest
+ * logit; an exponential below 2^-126 counts as 0.  A class at -inf has probability 0
+ * (bfloat16; an infinite float may make its logits NaN).  The classes are taken a piece at a time,
+ * in backward with d in scratch between the products that form it and those that use it.
+ * bfloat16: exact products, summed as in combo_grouped_linear, in parts of 1024 added with
+ * rounding.  d is rounded to bfloat16 once for dx and for a bfloat16 dW (what that leaves
+ * of the label's d, most of a row's gradient, is added to dx in binary32), and kept to 16
+ * bits for a float dW (off by 3e-6 of its size); with row_grad NULL the mean's factor is
+ * applied behind the products.  float: products of parts of 22 bits (forward; 2^-39 of
+ * the row's or class's largest value where that is more) and 24 bits (backward), relative
+ * errors of some 1e-7 to 5e-7 of the sums' magnitudes; small problems by multiply-adds.
+ * bfloat16 weights whose base, pitch and stride are multiples of 16 bytes are read where they
+ * lie; others, and floats, are brought into scratch a piece at a time.
+ *
  * scratch: device memory of at least combo_grouped_cross_entropy_scratch_bytes bytes
- * (grad_bytes 0 for the forward call), 256-byte aligned, contents undefined afterwards.
+ * (grad_bytes 0 for the forward call), 256-byte aligned, contents undefined afterwards;
+ * about a gigabyte where d or the weights' parts of all classes are larger than that.
  */
 size_t combo_grouped_cross_entropy_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes,
                                                  int grad_bytes);
@@ -539,10 +554,11 @@ combo_status combo_device_status(void);
  * CTA (short inputs). */
 int combo_last_kernel_path(void);
 
-/* Which kernels the last combo_grouped_linear* or combo_group_norm* call on this
- * thread launched: 0 none; products: 1 multiply-adds (float), 2 tensor cores, one
- * CTA a tile, 3 tensor cores, a pair of CTAs a tile, 4 tensor cores, operands brought
- * by threads (bases, pitches or strides off 16 bytes); group norm: 5 slabs resident in
+/* Which kernels the last combo_grouped_linear*, combo_grouped_cross_entropy* or
+ * combo_group_norm* call on this thread launched: 0 none; products and cross entropy:
+ * 1 multiply-adds (products of floats, small cross entropies), 2 tensor cores, one CTA
+ * a tile, 3 tensor cores, a pair of CTAs a tile, 4 tensor cores, operands brought by
+ * threads (bases, pitches or strides off 16 bytes); group norm: 5 slabs resident in
  * shared memory, 6 streamed in two passes. */
 int combo_last_step_path(void);
 

@@ -2,6 +2,7 @@
 //
 //   z_mv = x_m . W_w,v      lse_m = log sum_v exp z_mv      loss_m = lse_m - z_m,label        m in worker w's rows, v a class
 //   d_mv = (exp(z_mv - lse_m) - [v = label_m]) g_m          dx_m = sum_v d_mv W_w,v           dW_w,v = sum_m d_mv x_m
+#include <cuda_fp16.h>
 #include <string.h>
 
 #include "host_common.h"
@@ -309,6 +310,8 @@ using namespace combo_loss;
 struct Packed {
     int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 1]; [cap]: forward the row, backward the worker; [cap]
     float *lse, *g, *own;                                      // [cap]
+    unsigned short *xh, *wh;                                   // forward, floats: planes of float16, as x and w
+    float *x_unit, *w_unit;                                    // [cap], [N][piece]: what their numbers count in
     unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][piece][kp]; of [piece / 8][cap][8]
     float2* part;
     float* dx;
@@ -408,6 +411,57 @@ template <int PLANES> __device__ __forceinline__ void store_planes(unsigned shor
     }
 }
 
+// Two planes of float16 of v in units of `unit`.
+__device__ __forceinline__ void store_halves(unsigned short* to, long long plane, const float (&v)[8], float per_unit) {
+    uint32_t o[2][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 f = make_float2(v[2 * e] * per_unit, v[2 * e + 1] * per_unit);
+        const __half2 hi = __floats2half2_rn(f.x, f.y);
+        const __half2 lo = __floats2half2_rn(f.x - __low2float(hi), f.y - __high2float(hi));
+        o[0][e] = *reinterpret_cast<const uint32_t*>(&hi);
+        o[1][e] = *reinterpret_cast<const uint32_t*>(&lo);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(to + k * plane) = make_uint4(o[k][0], o[k][1], o[k][2], o[k][3]);
+}
+// The power of two that takes the largest of a warp's finite magnitudes to 2^14 .. 2^15, and its inverse.
+__device__ __forceinline__ float unit_of(float most, float& per_unit) {
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 16));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 8));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 4));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    const int e = most > 0.0f ? max((int)(__float_as_uint(most) >> 23) - 127, -100) : 14;
+    per_unit = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+    return __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+}
+__device__ __forceinline__ float most_of(const float (&v)[8]) {
+    float most = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]) <= 3.4028235e38f ? fabsf(v[e]) : 0.0f);
+    return most;
+}
+// A line of K floats by a warp, kp values and zeros: as halves (what they count in is returned), or as three planes of bfloat16.
+__device__ __forceinline__ float store_line(const unsigned char* line, int K, int kp, int vec, int lane, bool halves, unsigned short* to, long long plane) {
+    float most = 0.0f, per_unit = 1.0f, unit = 1.0f;
+    if (halves) {
+        for (int k = lane * 8; k < K; k += 256) {
+            float v[8];
+            load8<4>(line + (long long)k * 4, K - k, vec, v);
+            most = fmaxf(most, most_of(v));
+        }
+        unit = unit_of(most, per_unit);
+    }
+    for (int k = lane * 8; k < kp; k += 256) {
+        float v[8];
+        load8<4>(line + (long long)k * 4, K - k, vec, v);
+        if (halves) store_halves(to + k, plane, v, per_unit);
+        else store_planes<3>(to + k, plane, v);
+    }
+    return unit;
+}
+
 constexpr int kPackRows = 16;
 
 // Packs the labelled rows, kPackRows to a CTA; the first CTA leaves the tables of where the workers' rows lie.
@@ -466,27 +520,40 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
                 s.g[j] = p.row_grad ? p.row_grad[from] : 1.0f / (float)count;
             }
         }
-        unsigned short* to = s.x + (long long)j * s.kp;
-        for (int k = lane * 8; k < s.kp; k += 256) {
-            float v[8];
-            load8<EB>(p.x + (from * p.x_pitch + k) * EB, from >= 0 ? p.K - k : 0, vec, v);
-            store_planes<EB == 4 ? 3 : 1>(to + k, s.cap * s.kp, v);
+        if (EB == 4) {
+            const float unit = store_line(p.x + from * p.x_pitch * EB, from >= 0 ? p.K : 0, s.kp, vec, lane, p.loss != nullptr,
+                                          (p.loss ? s.xh : s.x) + (long long)j * s.kp, s.cap * s.kp);
+            if (lane == 0) s.x_unit[j] = unit;
+        } else {
+            unsigned short* to = s.x + (long long)j * s.kp;
+            for (int k = lane * 8; k < s.kp; k += 256) {
+                float v[8];
+                load8<EB>(p.x + (from * p.x_pitch + k) * EB, from >= 0 ? p.K - k : 0, vec, v);
+                store_planes<1>(to + k, 0, v);
+            }
         }
     }
 }
 
-// The weights of `classes` classes from v0 on as planes, zeros where there are none.
-template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Loss p, unsigned short* out, int v0, int classes, int kp, int vec) {
+// The weights of `classes` classes from v0 on as planes, zeros where there are none; a warp takes a class.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Loss p, const Packed s, int v0, int classes, int vec) {
     combo_step::pdl_release();
     combo_step::pdl_wait();
-    const int lots = kp / 8;
-    const long long all = (long long)p.N * classes * lots;
-    for (long long o = blockIdx.x * (long long)kThreads + threadIdx.x; o < all; o += (long long)gridDim.x * kThreads) {
-        const long long line = o / lots;
-        const int k = (int)(o - line * lots) * 8, w = (int)(line / classes), v = v0 + (int)(line - (long long)w * classes);
-        float f[8];
-        load8<EB>(p.w + (w * p.w_stride + v * p.w_pitch + k) * EB, v < p.V ? p.K - k : 0, vec, f);
-        store_planes<EB == 4 ? 3 : 1>(out + o * 8, all * 8, f);
+    const int lane = threadIdx.x & 31;
+    const long long all = (long long)p.N * classes, plane = all * s.kp;
+    for (long long line = blockIdx.x * (long long)kWarps + (threadIdx.x >> 5); line < all; line += (long long)gridDim.x * kWarps) {
+        const int w = (int)(line / classes), v = v0 + (int)(line - (long long)w * classes);
+        const unsigned char* from = p.w + (w * p.w_stride + v * p.w_pitch) * EB;
+        if (EB == 4) {
+            const float unit = store_line(from, v < p.V ? p.K : 0, s.kp, vec, lane, p.loss != nullptr, (p.loss ? s.wh : s.w) + line * s.kp, plane);
+            if (p.loss && lane == 0) s.w_unit[line] = unit;
+        } else {
+            for (int k = lane * 8; k < s.kp; k += 256) {
+                float f[8];
+                load8<EB>(from + (long long)k * EB, v < p.V ? p.K - k : 0, vec, f);
+                store_planes<1>(s.w + line * s.kp + k, 0, f);
+            }
+        }
     }
 }
 
@@ -590,15 +657,14 @@ bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int
 }
 
 constexpr int kSms = 148;
-#ifndef KPIECE
-#define KPIECE 1024
-#endif
-constexpr size_t kPieceBytes = (size_t)KPIECE << 20;       // aimed at for a piece of classes: d, and the weights' planes
+// Aimed at for a piece of classes: d, and the weights' planes.  Pieces that stay in L2 cost more by their launches and by adding
+// to dx than reading d from memory does: gradients of 8 x 326 rows, 1024 -> 30001 1006 us (160 MB), 727 (512 MB), 610 (1.2 GB).
+constexpr size_t kPieceBytes = (size_t)1 << 30;
 
 // How a call is computed, by its sizes alone.
 struct Plan {
     bool few;
-    int cg, planes, d_planes, kp;                // of x and w; of d
+    int cg, halves, planes, d_planes, kp;        // planes of x and w, float16 and bfloat16; of d
     int v_width, k_width, unit;                  // tiles along the classes, along the inputs; pieces are multiples of `unit`
     long long cap;
     long long dx_rows;                           // of the sums for dx, all splits
@@ -614,7 +680,7 @@ int even_width(int64_t n, int most, int unit) {
 
 // Bytes of a piece of so many classes.
 size_t piece_bytes(const Plan& a, int N, size_t classes, bool back, bool direct) {
-    return (back ? up(classes * a.cap * a.d_planes * 2, 256) : 0) + (direct ? 0 : up(classes * N * a.kp * a.planes * 2, 256));
+    return (back ? up(classes * a.cap * a.d_planes * 2, 256) : 0) + (direct ? 0 : up(classes * N * a.kp * (a.planes + a.halves) * 2 + classes * N * 4, 256));
 }
 
 Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_bytes) {
@@ -631,19 +697,20 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     // Pairs of CTAs halve what a product takes from L2, single ones waste less of ragged rows.  Measured (pairs / single), gradients:
     // 8 x 250 rows, 256 -> 1000, floats 91 / 74 us, bfloat16 46 / 43; 512 -> 16000 853 / 928 and 189 / 203.
     a.cg = M / N > 128 && V * K > (1 << 19) ? 2 : 1;
-    a.planes = elem_bytes == 4 ? 3 : 1;
+    a.halves = elem_bytes == 4 && !back ? 2 : 0;
+    a.planes = elem_bytes == 2 ? 1 : back ? 3 : 0;
     a.d_planes = elem_bytes == 4 ? 3 : grad_bytes == 4 ? 2 : 1;
     a.kp = (int)up(K, 64);
-    const int most = a.planes == 3 && a.cg == 1 ? 128 : 256;
+    const int most = elem_bytes == 4 && back && a.cg == 1 ? 128 : 256;       // two stages in shared memory
     a.v_width = even_width(V, most, 128);
     a.k_width = even_width(K, most, 128);
     if (V > 1024) a.v_width = most;
     a.unit = a.v_width;
     a.cap = (long long)up(M + 63 * (N < M ? N : M), 64);
     const size_t cap = (size_t)a.cap;
-    size_t at = up((size_t)N * 4, 256) + 2 * up((size_t)M * 4, 256) + 2 * up((size_t)(N + 1) * 4, 256) + 5 * up(cap * 4, 256);
+    size_t at = up((size_t)N * 4, 256) + 2 * up((size_t)M * 4, 256) + 2 * up((size_t)(N + 1) * 4, 256) + 6 * up(cap * 4, 256);
     a.x = at;
-    at += up(cap * a.kp * a.planes * 2, 256);
+    at += up(cap * a.kp * (a.planes + a.halves) * 2, 256);
     a.part = at;
     if (!back) {
         at += up(2 * up(V, a.v_width) / a.v_width * cap * 8, 256);
@@ -697,8 +764,8 @@ template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass
 
 // EB: bytes of the inputs; GB: of dW (0: forward).
 template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Loss& p, unsigned char* scratch, int sms, int smem_optin, cudaStream_t st) {
-    constexpr int P = EB == 4 ? 3 : 1, D = EB == 4 ? 3 : GB == 4 ? 2 : 1;
     constexpr bool kBack = GB != 0;
+    constexpr int P = EB == 4 ? 3 : 1, L = EB == 2 ? 1 : kBack ? 3 : 2, D = EB == 4 ? 3 : GB == 4 ? 2 : 1;      // planes: of the gradients' products, of the logits', of d
     const auto vec_ok = [](const void* b, long long pitch, long long stride, int eb) {
         return combo_host::aligned_to(b, 16) && pitch * eb % 16 == 0 && stride * eb % 16 == 0;
     };
@@ -719,7 +786,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     s.lse = reinterpret_cast<float*>(take(cap * 4));
     s.g = reinterpret_cast<float*>(take(cap * 4));
     s.own = reinterpret_cast<float*>(take(cap * 4));
-    s.x = reinterpret_cast<unsigned short*>(scratch + a.x);
+    s.x_unit = reinterpret_cast<float*>(take(cap * 4));
+    s.xh = reinterpret_cast<unsigned short*>(scratch + a.x);
+    s.x = s.xh + cap * a.kp * a.halves;
     s.part = reinterpret_cast<float2*>(scratch + a.part);
     s.dx = reinterpret_cast<float*>(scratch + a.dx);
 
@@ -729,7 +798,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     for (int n = 2; piece > a.unit && !(direct && !kBack) && piece_bytes(a, p.N, piece, kBack, direct) > a.room; ++n)
         piece = (int)up((p.V + n - 1) / n, a.unit);
     s.d = reinterpret_cast<unsigned short*>(scratch + a.region);
-    s.w = s.d + (kBack ? up((size_t)piece * cap * D * 2, 256) / 2 : 0);
+    s.w_unit = reinterpret_cast<float*>(s.d + (kBack ? up((size_t)piece * cap * D * 2, 256) / 2 : 0));
+    s.wh = reinterpret_cast<unsigned short*>(s.w_unit + (a.halves ? (size_t)piece * p.N : 0));
+    s.w = s.wh + (size_t)piece * p.N * a.kp * a.halves;
 
     cudaError_t e = combo_host::launch_after(k_count, dim3(p.N), dim3(kCountThreads), 0, st, p, s);
     if (e != cudaSuccess) return e;
@@ -741,15 +812,17 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     const bool dw_vec = kBack && vec_ok(p.dw, p.dw_pitch, p.dw_stride, kBack ? GB : 4) && p.dw_pitch < (1LL << 36) && p.dw_stride < (1LL << 36);
     const int kt = (p.K + a.k_width - 1) / a.k_width;
     const long long dx_pitch = kt * a.k_width;
-    CUtensorMap mx, mw, md = {}, mdw = {}, out_dx = {}, out_dw = {};
-    const long long xd[3] = {a.kp, a.cap, P}, xs[2] = {a.kp, a.cap * a.kp};
-    const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : piece, p.N, direct ? 1 : P};
-    const long long lines = (long long)piece * a.kp;
+    CUtensorMap mx = {}, mw = {}, mxh = {}, mwh = {}, md = {}, mdw = {}, out_dx = {}, out_dw = {};
+    const long long lines = (long long)piece * a.kp, flat = a.cap * a.kp;
+    const long long xd[3] = {a.kp, a.cap, P}, hd[3] = {a.kp, a.cap, L}, xs[2] = {a.kp, flat};
+    const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : piece, p.N, direct ? 1 : P}, vd[4] = {a.kp, piece, p.N, L};
     const long long ws[3] = {direct ? p.w_pitch : a.kp, direct ? (p.N > 1 ? p.w_stride : 8) : lines, direct ? 8 : lines * p.N};
     // d: eight classes of a row in 16 bytes, rows side by side, so that a warp that writes and a box that is read run along memory;
     // in 64-bit units, of which a box may have 256
     const long long dd[3] = {2 * a.cap, piece / 8, D}, ds[2] = {a.cap * 2, a.cap * 2 * (piece / 8)};
-    bool fine = map_of(&mx, s.x, 2, 3, xd, xs, 64) && map_of(&mw, direct ? const_cast<unsigned char*>(p.w) : reinterpret_cast<unsigned char*>(s.w), 2, 4, wd, ws, 64);
+    bool fine = (EB == 4 && !kBack) || (map_of(&mx, s.x, 2, 3, xd, xs, 64) &&
+                                        map_of(&mw, direct ? const_cast<unsigned char*>(p.w) : reinterpret_cast<unsigned char*>(s.w), 2, 4, wd, ws, 64));
+    if (L == 2 && fine) fine = map_of(&mxh, s.xh, 2, 3, hd, xs, 64) && map_of(&mwh, s.wh, 2, 4, vd, ws, 64);
     if (kBack && fine) {
         const long long rd[3] = {dx_pitch, a.dx_rows, 1}, rs[2] = {dx_pitch, 8};
         const long long gd[3] = {p.K, p.V, p.N}, gs[2] = {p.dw_pitch, p.N > 1 ? p.dw_stride : 8};
@@ -767,6 +840,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.clusters = kSms / CG;
     q.row_cap = a.cap;
     q.count = s.count;
+    q.x_unit = s.x_unit;
+    q.w_unit = s.w_unit;
+    q.piece = piece;
     q.d = reinterpret_cast<unsigned char*>(s.d);
     q.d_blocks = piece / 8;
     q.scaled = p.row_grad != nullptr;
@@ -786,8 +862,8 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     for (int v0 = 0; v0 < p.V; v0 += piece) {
         const int classes = p.V - v0 < piece ? p.V - v0 : piece;
         if (!direct) {
-            const long long lots = (long long)p.N * piece * a.kp / 8, grid = (lots + kThreads - 1) / kThreads;
-            e = combo_host::launch_after(k_planes<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s.w, v0, piece, a.kp, (int)w_vec);
+            const long long grid = ((long long)p.N * piece + kWarps - 1) / kWarps;
+            e = combo_host::launch_after(k_planes<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s, v0, piece, (int)w_vec);
             if (e != cudaSuccess) return e;
         }
         q.v0 = v0;
@@ -796,9 +872,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.width = a.v_width;
         q.wt = (classes + a.v_width - 1) / a.v_width;
         q.steps = a.kp / kStep;
-        const Maps logits_of = {mx, mw, mw};
-        e = kBack ? launch_loss<CG, kGrad, P, P, D>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
-                  : launch_loss<CG, kStats, P, P, 1>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
+        const Maps logits_of = L == 2 ? Maps{mxh, mwh, mwh} : Maps{mx, mw, mw};
+        if constexpr (kBack) e = launch_loss<CG, kGrad, L, L, D>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
+        else e = launch_loss<CG, kStats, L, L, 1>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
         if (e != cudaSuccess) return e;
         if constexpr (kBack) {
             q.width = a.k_width;
@@ -877,6 +953,7 @@ combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in,
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     const Plan plan = plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes);
+    combo_host::set_step_path(plan.few ? combo_host::kPathMultiplyAdd : plan.cg == 2 ? combo_host::kPathTensorPairs : combo_host::kPathTensor);
     if (!plan.few) {
         e = plan.cg == 2 ? launch_tensor<2>(plan, p, elem_bytes, grad_bytes, scratch, sms, smem, st)
                          : launch_tensor<1>(plan, p, elem_bytes, grad_bytes, scratch, sms, smem, st);

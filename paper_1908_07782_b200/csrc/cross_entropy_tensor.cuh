@@ -1,7 +1,9 @@
 // The cross entropy's products on the tensor cores.
 //
-// Labelled rows are first packed: worker after worker, each from a multiple of 64 on, as bfloat16 planes (floats: three, which hold
-// all 24 bits: x = x0 + x1 + x2), zeros behind a worker's last.  Then, for a piece of the classes at a time,
+// Labelled rows are first packed: worker after worker, each from a multiple of 64 on, zeros behind a worker's last.  bfloat16 as
+// it is; floats as planes that add up to them: forward two of float16, scaled by a power of two to each row's and class's largest
+// (22 bits, or 2^-39 of the largest if that is more), backward three of bfloat16 (24 bits, whatever the range: d reaches over many
+// orders, and planes of both kinds for the logits and for the gradients cost more than they save).  Then, for a piece of the classes at a time,
 //
 //                height (128 a CTA)      width                  summed r          results
 //   logits       rows                    classes                inputs            forward: (max, sum of exponentials) of a row's 128
@@ -10,7 +12,8 @@
 //   weights'     classes                 inputs                 rows              dW
 //
 // A lane of TMEM is a row of results, so the softmax needs no exchange between threads: a thread holds 128 logits of one row.
-// Floats are products of planes: x0 w0 + (x0 w1 + x1 w0) + (x0 w2 + x1 w1 + x2 w0); what is left out is below 2^-24 of a product.
+// Floats are products of planes: x0 w0 + (x0 w1 + x1 w0), and for three x0 w2 + x1 w1 + x2 w0; what is left out of a product is
+// 2^-24 of it on average, or below that.  (Forward by three planes: 254 against 185 us for 32 x 1056 rows, 512 -> 1000.)
 // The tensor cores truncate at every addition of 16 products, so only `part_steps` stages of 64 are summed there (floats: two, with the
 // small products first), and the parts are added with rounding in the registers of the warps that take the results.
 #pragma once
@@ -65,6 +68,8 @@ struct Pass {
     const int* label;                        // of packed rows; -1 behind a worker's last
     const float *lse, *g;
     const int* count;                        // labelled rows of a worker
+    const float *x_unit, *w_unit;            // forward, floats: what a packed row's, and a class's of the piece, numbers count in
+    int piece;                               // classes of a piece
     float2* part;                            // [2 tiles of classes][row_cap]
     float* own;                              // a row's logit of its label; kGrad: what the first plane of d leaves of its d
     float* dx;                               // [splits][rows][dx_pitch]
@@ -206,6 +211,7 @@ template <int CG, int MODE, int PA, int PB, int OB>
 __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __grid_constant__ Maps maps) {
     constexpr bool A_R = MODE != kWeights, B_R = MODE == kStats || MODE == kGrad;
     constexpr int kPlanes = PA > PB ? PA : PB;
+    constexpr bool kHalf = MODE == kStats && PA == 2;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 4];
     __shared__ uint32_t tmem_at;
@@ -305,7 +311,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
             Walk<CG, MODE> walk(q, first, stride);
             uint32_t done = 0, turn = 0;     // stages; parts, which take the two accumulators in turn
             bool ok = true;
-            const uint32_t kind = product_kind(128 * CG, q.width, A_R, B_R);
+            const uint32_t kind = kHalf ? product_kind_half(128 * CG, q.width, A_R, B_R) : product_kind(128 * CG, q.width, A_R, B_R);
             while (walk.next(x)) {
                 const int parts = (x.steps + q.part_steps - 1) / q.part_steps;
                 if (elect()) {
@@ -421,6 +427,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                 }
             } else {
                 if (!mine) continue;
+                if constexpr (kHalf) {
+                    const float unit = q.x_unit[j];
+                    const float4* units = reinterpret_cast<const float4*>(q.w_unit + (long long)x.w * q.piece + col);
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 32) {
+                        if (c < columns) {
+#pragma unroll
+                            for (int e = c; e < c + 32; e += 4) {
+                                const float4 u = units[e / 4];
+                                acc[e / 2] = mul2(mul2(acc[e / 2], pair(unit, unit)), pair(u.x, u.y));
+                                acc[e / 2 + 1] = mul2(mul2(acc[e / 2 + 1], pair(unit, unit)), pair(u.z, u.w));
+                            }
+                        }
+                    }
+                }
                 if constexpr (MODE == kStats) {
                     // classes that are not there
                     const int left = q.V - (q.v0 + col);

@@ -214,6 +214,8 @@ __device__ __forceinline__ uint32_t product_kind(int m, int n, bool a_along_r, b
     return 1u << 4 | 1u << 7 | 1u << 10 | (a_along_r ? 0u : 1u << 15) | (b_along_r ? 0u : 1u << 16) | (uint32_t)(n >> 3) << 17 |
            (uint32_t)(m >> 4) << 24;
 }
+// the same for float16
+__device__ __forceinline__ uint32_t product_kind_half(int m, int n, bool a_along_r, bool b_along_r) { return product_kind(m, n, a_along_r, b_along_r) & ~(1u << 7 | 1u << 10); }
 template <int CG> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
     if constexpr (CG == 1)
         asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a),

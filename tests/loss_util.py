@@ -112,7 +112,8 @@ class Case:
                 p = torch.exp(z - lse[rows].double()[:, None])
                 hot = torch.zeros_like(p).scatter_(1, self.labels[rows, None], 1.0)
                 d = (p - hot) * g[:, None]
-                dd = g.abs()[:, None] * (p * (dz + (60 + 4 * (z.abs() + lse[rows].double().abs()[:, None])) * U) + 2 * U * (p + hot))
+                # an exponential below binary32's normal range is 0: off by less than 2^-126, whatever it is
+                dd = g.abs()[:, None] * (p * (dz + (60 + 4 * (z.abs() + lse[rows].double().abs()[:, None])) * U) + 2 * U * (p + hot) + 2.0 ** -126)
                 want_dx[rows] = d @ wt
                 tol_dx[rows] = (dd + half_dx * d.abs()) @ wt.abs() + 2 * (self.V + 4) * U * (d.abs() @ wt.abs())
                 want, tol = d.T @ x, (dd + half_dw * d.abs()).T @ x.abs() + 2 * (n + 4) * U * (d.abs().T @ x.abs())
