@@ -31,7 +31,7 @@ __device__ __forceinline__ void rows_of(const Loss& p, int w, long long& r0, lon
 }
 
 // ---------------------------------------------------------------- few multiply-adds: a CTA takes eight rows of a worker
-constexpr int kThreads = 256, kWarps = kThreads / 32, kR = 8, kU = 4;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kR = 8, kU = 4, kFewClasses = 256;
 
 // The worker and first row of lot `block` of kR rows, workers counted through kThreads at a time; false behind the last.
 __device__ __forceinline__ bool find_rows(const Loss& p, long long block, int& w, long long& i0, long long& i1) {
@@ -175,10 +175,11 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_lo
 }
 
 // What the warps hold for `lines` x (32 E) results, acc[line][e] a lane, added up in the warps' order and given to put(line, k, sum).
+constexpr int kSumWarps = 16;
 template <int EB, bool VEC, typename F>
 __device__ __forceinline__ void join_warps(const float (&acc)[kR][Elem<EB>::V], int c, int lane, int warp, F put) {
     constexpr int E = Elem<EB>::V;
-    __shared__ float sm[kWarps][2][32 * E + 1];
+    __shared__ float sm[kSumWarps][2][32 * E + 1];
 #pragma unroll
     for (int h = 0; h < kR; h += 2) {
         __syncthreads();
@@ -187,18 +188,17 @@ __device__ __forceinline__ void join_warps(const float (&acc)[kR][Elem<EB>::V], 
 #pragma unroll
             for (int e = 0; e < E; ++e) sm[warp][l][e * 32 + lane] = acc[h + l][e];
         __syncthreads();
-        for (int o = threadIdx.x; o < 2 * 32 * E; o += kThreads) {
+        for (int o = threadIdx.x; o < 2 * 32 * E; o += kSumWarps * 32) {
             const int l = o / (32 * E), at = o % (32 * E);
             float sum = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) sum += sm[k][l][VEC ? at % E * 32 + at / E : at];
+            for (int k = 0; k < kSumWarps; ++k) sum += sm[k][l][VEC ? at % E * 32 + at / E : at];
             put(h + l, c * 32 * E + at, sum);
         }
     }
 }
 
 template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_back(const Loss p) {
-    constexpr int E = Elem<EB>::V;
     int w;
     long long i0, i1;
     combo_step::pdl_release();
@@ -221,40 +221,57 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_ba
         if (has) g = 1.0f / (float)count;
     }
     const float lse = has ? p.lse_in[i0 + row] : 0.0f;
+    __shared__ __align__(16) float d[kFewClasses][kR];
     for (int v0 = warp * kU; v0 < p.V; v0 += kWarps * kU) {
         const float z = logits<EB, VEC>(p, x0, rows, w0, v0, lane);
         const int v = v0 + lane / kR;
-        if (v < p.V && row < rows) p.d[(i0 + row) * p.V + v] = has ? (expf(z - lse) - (v == label ? 1.0f : 0.0f)) * g : 0.0f;
+        if (v < p.V) {
+            const float f = has ? (expf(z - lse) - (v == label ? 1.0f : 0.0f)) * g : 0.0f;
+            d[v][row] = f;
+            if (row < rows) p.d[(i0 + row) * p.V + v] = f;
+        }
     }
     __syncthreads();
-    const float* d = p.d + i0 * p.V;
-    const unsigned some = __ballot_sync(0xffffffffu, has && lane < kR);
-    for (int c = 0; c * 32 * E < p.K; ++c) {
-        float acc[kR][E];
+    const unsigned some = __ballot_sync(0xffffffffu, has && lane < kR);          // rows with a label
+    // dx: threads side by side along the inputs, as many groups over the classes as there is room for, joined in their order
+    __shared__ float part[kThreads][kR + 1];
+    int side = 32;
+    while (side < kThreads && side < p.K) side *= 2;
+    const int group = threadIdx.x / side, groups = kThreads / side;
+    for (int k0 = 0; k0 < p.K; k0 += side) {
+        const int k = k0 + threadIdx.x % side;
+        float acc[kR];
 #pragma unroll
-        for (int r = 0; r < kR; ++r)
+        for (int r = 0; r < kR; ++r) acc[r] = 0.0f;
+        if (k < p.K) {
+#pragma unroll 8
+            for (int v = group; v < p.V; v += groups) {
+                const float wv = Elem<EB>::get(w0 + ((long long)v * p.w_pitch + k) * EB);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[r][e] = 0.0f;
-        for (int v = warp; v < p.V; v += kWarps) {
-            float wv[E];
-            load_share<EB, VEC>(w0 + (long long)v * p.w_pitch * EB, c, lane, p.K, wv);
-#pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                if (some >> r & 1u) {
-                    const float f = d[(long long)r * p.V + v];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) acc[r][e] = fmaf(f, wv[e], acc[r][e]);
-                }
+                for (int r = 0; r < kR; ++r) acc[r] = fmaf(d[v][r], wv, acc[r]);
             }
         }
-        join_warps<EB, VEC>(acc, c, lane, warp, [&](int r, int k, float sum) {
-            if (r < rows && k < p.K) Elem<EB>::put(p.dx + ((i0 + r) * p.dx_pitch + k) * EB, sum);
-        });
+        if (groups > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < kR; ++r) part[threadIdx.x][r] = acc[r];
+            __syncthreads();
+            if (group == 0) {
+                for (int g2 = 1; g2 < groups; ++g2)
+#pragma unroll
+                    for (int r = 0; r < kR; ++r) acc[r] += part[threadIdx.x + g2 * side][r];
+            }
+        }
+        if (group == 0 && k < p.K) {
+#pragma unroll
+            for (int r = 0; r < kR; ++r)
+                if (r < rows) Elem<EB>::put(p.dx + ((i0 + r) * p.dx_pitch + k) * EB, some >> r & 1u ? acc[r] : 0.0f);
+        }
     }
 }
 
 // Eight classes' gradients of one worker by 32 E columns; warps share out the rows.
-template <int EB, int OB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_weights(const Loss p) {
+template <int EB, int OB, bool VEC> __global__ void __launch_bounds__(kSumWarps * 32) k_few_weights(const Loss p) {
     constexpr int E = Elem<EB>::V;
     const int w = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x;
@@ -270,7 +287,7 @@ template <int EB, int OB, bool VEC> __global__ void __launch_bounds__(kThreads) 
             for (int e = 0; e < E; ++e) acc[r][e] = 0.0f;
         // several rows' loads at once; a row without a label may hold anything (its d is 0)
 #pragma unroll 4
-        for (long long i = i0 + warp; i < i1; i += kWarps) {
+        for (long long i = i0 + warp; i < i1; i += kSumWarps) {
             const int64_t label = p.labels[i];
             const bool has = label >= 0 && label < p.V;
             float xv[E], f[kR];
@@ -299,8 +316,8 @@ template <int EB, bool VEC> cudaError_t launch_few(const Loss& p, int grad_bytes
     if (e != cudaSuccess) return e;
     const unsigned classes = (unsigned)((p.V + kR - 1) / kR);
     const dim3 g((unsigned)((p.K + 32 * Elem<EB>::V - 1) / (32 * Elem<EB>::V)), classes < 65535 ? classes : 65535, (unsigned)p.N);
-    return grad_bytes == 4 ? combo_host::launch_after(k_few_weights<EB, 4, VEC>, g, dim3(kThreads), 0, st, p)
-                           : combo_host::launch_after(k_few_weights<EB, 2, VEC>, g, dim3(kThreads), 0, st, p);
+    return grad_bytes == 4 ? combo_host::launch_after(k_few_weights<EB, 4, VEC>, g, dim3(kSumWarps * 32), 0, st, p)
+                           : combo_host::launch_after(k_few_weights<EB, 2, VEC>, g, dim3(kSumWarps * 32), 0, st, p);
 }
 
 // ---------------------------------------------------------------- packing of rows and weights for the tensor cores
@@ -688,8 +705,8 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     const bool back = grad_bytes != 0;
     // Few multiply-adds: one launch, or two, against four and seven.  Measured, 8 workers, few / tensor cores: loss of 1336 rows, 256 ->
     // 64, floats 11.9 / 23.9 us, 512 -> 256 54 / 41; bfloat16 11.3 / 17.0, 47 / 20; gradients 28.6 / 53.5, 147 / 82 and 36 / 38,
-    // 160 / 45; of 8000 rows, 256 -> 10, 86 / 84 and 113 / 46.
-    a.few = M == 0 || (M <= 2048 && V * K <= (elem_bytes == 4 ? 1 << 15 : 1 << 14));
+    // 160 / 45; of 8000 rows, 256 -> 10, 86 / 84 and 113 / 46; many classes of few inputs take a warp many turns (16 -> 1000: 75 to 300).
+    a.few = M == 0 || (M <= 2048 && V <= kFewClasses && V * K <= (elem_bytes == 4 ? 1 << 15 : 1 << 14));
     if (a.few) {
         a.total = 256 + (back ? (size_t)M * V * 4 : 0);
         return a;
