@@ -392,21 +392,44 @@ __global__ void __launch_bounds__(kCountThreads) k_count(const Loss p, const Pac
     if (t == 0) s.count[w] = before;
 }
 
-// Eight neighbours of a line of `left` elements, zeros behind.
+// Eight neighbours of a line of `left` elements, zeros behind.  Off 16-byte boundaries the aligned 16 bytes that hold some of them
+// are read whole and shifted.
 template <int EB> __device__ __forceinline__ void load8(const unsigned char* q, int left, bool vec, float (&v)[8]) {
+    constexpr int W = 2 * EB;                    // words of eight elements
+    uint32_t w[W + 4];
+    const int some = min(max(left, 0), 8);
     if (vec && left >= 8) {
-        if constexpr (EB == 2) {
-            Elem<2>::unpack(*reinterpret_cast<const uint4*>(q), v);
-        } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float4 f = *reinterpret_cast<const float4*>(q + h * 16);
-                v[4 * h] = f.x; v[4 * h + 1] = f.y; v[4 * h + 2] = f.z; v[4 * h + 3] = f.w;
-            }
+        for (int h = 0; h < EB / 2; ++h) {
+            const uint4 f = reinterpret_cast<const uint4*>(q)[h];
+            w[4 * h] = f.x; w[4 * h + 1] = f.y; w[4 * h + 2] = f.z; w[4 * h + 3] = f.w;
         }
     } else {
+        const int off = (int)(reinterpret_cast<uintptr_t>(q) & 15u);
+        const uint4* from = reinterpret_cast<const uint4*>(q - off);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < left ? Elem<EB>::get(q + e * EB) : 0.0f;
+        for (int h = 0; h <= EB / 2; ++h) {
+            uint4 f = make_uint4(0, 0, 0, 0);
+            if (some > 0 && h * 16 < off + some * EB) f = from[h];
+            w[4 * h] = f.x; w[4 * h + 1] = f.y; w[4 * h + 2] = f.z; w[4 * h + 3] = f.w;
+        }
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < W + 2; ++i) w[i] = w[i + 2];
+        }
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < W + 1; ++i) w[i] = w[i + 1];
+        }
+        if (EB == 2 && (off & 2)) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float f = EB == 4 ? __uint_as_float(w[e]) : e & 1 ? combo_step::widen_hi(w[e / 2]) : combo_step::widen_lo(w[e / 2]);
+        v[e] = e < some ? f : 0.0f;
     }
 }
 // Writes them as bfloat16 planes: each holds what the ones before leave, rounded; towards zero where rounding would overflow.
@@ -479,10 +502,8 @@ __device__ __forceinline__ float store_line(const unsigned char* line, int K, in
     return unit;
 }
 
-constexpr int kPackRows = 16;
-
-// Packs the labelled rows, kPackRows to a CTA; the first CTA leaves the tables of where the workers' rows lie.
-template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss p, const Packed s, int vec) {
+// Packs the labelled rows, `lot` to a warp, whose places its lanes look up at once; the first CTA leaves the tables of where the workers' rows lie.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss p, const Packed s, int vec, int lot) {
     extern __shared__ int begins[];                            // packed rows [N + 1]
     __shared__ int sums[kWarps];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -517,7 +538,10 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
         scan(s.height, s.tiles, 1);
     }
     const int total = begins[p.N];
-    for (int j = blockIdx.x * kPackRows + warp; j < min((int)(blockIdx.x + 1) * kPackRows, total); j += kWarps) {
+    const int j0 = (blockIdx.x * kWarps + warp) * lot, rows = min(lot, total - j0);
+    int place = -1;                                            // of the lane's row
+    if (lane < rows) {
+        const int j = j0 + lane;
         int lo = 0, hi = p.N - 1;                              // the last w with begins[w] <= j
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -527,22 +551,24 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
         long long r0, r1;
         rows_of(p, lo, r0, r1);
         const int rank = j - begins[lo], count = s.count[lo];
-        const int from = rank < count ? s.list[r0 + rank] : -1;
-        if (lane == 0) {
-            s.src[j] = p.loss ? from : lo;
-            s.label[j] = from >= 0 ? (int)p.labels[from] : -1;
-            if (!p.loss && from >= 0) {
-                s.pos[from] = j;
-                s.lse[j] = p.lse_in[from];
-                s.g[j] = p.row_grad ? p.row_grad[from] : 1.0f / (float)count;
-            }
+        if (rank < count) place = s.list[r0 + rank];
+        s.src[j] = p.loss ? place : lo;
+        s.label[j] = place >= 0 ? (int)p.labels[place] : -1;
+        if (!p.loss && place >= 0) {
+            s.pos[place] = j;
+            s.lse[j] = p.lse_in[place];
+            s.g[j] = p.row_grad ? p.row_grad[place] : 1.0f / (float)count;
         }
+    }
+    for (int i = 0; i < rows; ++i) {
+        const int j = j0 + i, from = __shfl_sync(0xffffffffu, place, i);
         if (EB == 4) {
             const float unit = store_line(p.x + from * p.x_pitch * EB, from >= 0 ? p.K : 0, s.kp, vec, lane, p.loss != nullptr,
                                           (p.loss ? s.xh : s.x) + (long long)j * s.kp, s.cap * s.kp);
             if (lane == 0) s.x_unit[j] = unit;
         } else {
             unsigned short* to = s.x + (long long)j * s.kp;
+#pragma unroll 4
             for (int k = lane * 8; k < s.kp; k += 256) {
                 float v[8];
                 load8<EB>(p.x + (from * p.x_pitch + k) * EB, from >= 0 ? p.K - k : 0, vec, v);
@@ -552,25 +578,30 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
     }
 }
 
-// The weights of `classes` classes from v0 on as planes, zeros where there are none; a warp takes a class.
+// The weights of `classes` classes from v0 on as planes, zeros where there are none: a warp a class where it looks for the largest
+// (forward, floats), else threads side by side along all of them.
 template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Loss p, const Packed s, int v0, int classes, int vec) {
     combo_step::pdl_release();
     combo_step::pdl_wait();
     const int lane = threadIdx.x & 31;
-    const long long all = (long long)p.N * classes, plane = all * s.kp;
-    for (long long line = blockIdx.x * (long long)kWarps + (threadIdx.x >> 5); line < all; line += (long long)gridDim.x * kWarps) {
-        const int w = (int)(line / classes), v = v0 + (int)(line - (long long)w * classes);
-        const unsigned char* from = p.w + (w * p.w_stride + v * p.w_pitch) * EB;
-        if (EB == 4) {
-            const float unit = store_line(from, v < p.V ? p.K : 0, s.kp, vec, lane, p.loss != nullptr, (p.loss ? s.wh : s.w) + line * s.kp, plane);
-            if (p.loss && lane == 0) s.w_unit[line] = unit;
-        } else {
-            for (int k = lane * 8; k < s.kp; k += 256) {
-                float f[8];
-                load8<EB>(from + (long long)k * EB, v < p.V ? p.K - k : 0, vec, f);
-                store_planes<1>(s.w + line * s.kp + k, 0, f);
-            }
+    const long long lines = (long long)p.N * classes, plane = lines * s.kp;
+    if (EB == 4 && p.loss) {
+        for (long long line = blockIdx.x * (long long)kWarps + (threadIdx.x >> 5); line < lines; line += (long long)gridDim.x * kWarps) {
+            const int w = (int)(line / classes), v = v0 + (int)(line - (long long)w * classes);
+            const float unit = store_line(p.w + (w * p.w_stride + v * p.w_pitch) * EB, v < p.V ? p.K : 0, s.kp, vec, lane, true, s.wh + line * s.kp, plane);
+            if (lane == 0) s.w_unit[line] = unit;
         }
+        return;
+    }
+    const unsigned lots = (unsigned)s.kp / 8;
+    const long long all = lines * lots;
+#pragma unroll 4
+    for (long long o = blockIdx.x * (long long)kThreads + threadIdx.x; o < all; o += (long long)gridDim.x * kThreads) {
+        const long long line = all < (1LL << 32) ? (unsigned)o / lots : o / lots;
+        const int k = (int)(o - line * lots) * 8, w = (int)((unsigned)line / (unsigned)classes), v = v0 + (int)(line - (long long)w * classes);
+        float f[8];
+        load8<EB>(p.w + (w * p.w_stride + v * p.w_pitch + k) * EB, v < p.V ? p.K - k : 0, vec, f);
+        store_planes<EB == 4 ? 3 : 1>(s.w + o * 8, plane, f);
     }
 }
 
@@ -617,51 +648,75 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, cons
     }
 }
 
-// The rows' gradients to their places: the parts of the sums added up, zeros for rows without a label.
-template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const Loss p, const Packed s, const Pass q, int vec, int w_vec) {
+// 32 bytes that this kernel does not write.
+__device__ __forceinline__ void load32(const void* from, uint32_t (&v)[8]) {
+    asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+        : "l"(from));
+}
+
+// The rows' gradients to their places, a warp `lot` rows whose places its lanes look up at once: the parts of the sums added up,
+// zeros for rows without a label.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const Loss p, const Packed s, const Pass q, int vec, int w_vec, int lot) {
     combo_step::pdl_release();
     combo_step::pdl_wait();
-    const int splits = splits_of(q), lots = s.kp / 8;
+    const int lane = threadIdx.x & 31, splits = splits_of(q);
     const long long total = q.row0[q.N], a = min(max((long long)p.begin[0], 0LL), p.M), b = min(max((long long)p.begin[p.N], a), p.M);
-    for (long long o = blockIdx.x * (long long)kThreads + threadIdx.x; o < (b - a) * lots; o += (long long)gridDim.x * kThreads) {
-        const long long row = o / lots, m = a + row;
-        const int k = (int)(o - row * lots) * 8, left = p.K - k;
-        if (left <= 0) continue;
-        const int j = s.pos[m];
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = 0.0f;
-        if (j >= 0) {
-            for (int i = 0; i < splits; ++i) {
-                uint32_t v[8];
-                load32(q.dx + (i * total + j) * q.dx_pitch + k, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(v[e]);
-            }
-            if (EB == 2) {
-                // d of a row's label is most of its gradient: what the plane's rounding left of it comes here
-                float v[8];
-                load8<EB>(p.w + (s.src[j] * p.w_stride + s.label[j] * p.w_pitch + k) * EB, left, w_vec, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = fmaf(s.own[j], v[e], f[e]);
-            }
-            if (!q.scaled) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] *= s.g[j];
-            }
+    const long long m0 = a + (blockIdx.x * (long long)kWarps + (threadIdx.x >> 5)) * lot;
+    const int rows = (int)min((long long)lot, b - m0);
+    if (rows <= 0) return;
+    // of the lane's row
+    const int place = lane < rows ? s.pos[m0 + lane] : -1;
+    float rest = 0.0f, factor = 1.0f;
+    long long weights = 0;
+    if (place >= 0) {
+        if (!q.scaled) factor = s.g[place];
+        if (EB == 2) {
+            rest = s.own[place];
+            weights = s.src[place] * p.w_stride + s.label[place] * p.w_pitch;
         }
-        unsigned char* to = p.dx + (m * p.dx_pitch + k) * EB;
-        if (vec && left >= 8) {
-            if constexpr (EB == 2) {
-                *reinterpret_cast<uint4*>(to) = Elem<2>::pack(f);
-            } else {
-                reinterpret_cast<float4*>(to)[0] = make_float4(f[0], f[1], f[2], f[3]);
-                reinterpret_cast<float4*>(to)[1] = make_float4(f[4], f[5], f[6], f[7]);
-            }
-        } else {
+    }
+    for (int i0 = 0; i0 < rows; ++i0) {
+        const long long m = m0 + i0;
+        const int j = __shfl_sync(0xffffffffu, place, i0);
+        const float own = __shfl_sync(0xffffffffu, rest, i0), g = __shfl_sync(0xffffffffu, factor, i0);
+        const unsigned char* w = p.w + __shfl_sync(0xffffffffu, weights, i0) * EB;
+#pragma unroll 1
+        for (int k = lane * 8; k < p.K; k += 256) {
+            const int left = p.K - k;
+            float f[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < left) Elem<EB>::put(to + e * EB, f[e]);
+            for (int e = 0; e < 8; ++e) f[e] = 0.0f;
+            if (j >= 0) {
+                for (int i = 0; i < splits; ++i) {
+                    uint32_t v[8];
+                    load32(q.dx + (i * total + j) * q.dx_pitch + k, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(v[e]);
+                }
+                if (EB == 2) {
+                    // d of a row's label is most of its gradient: what the plane's rounding left of it comes here
+                    float v[8];
+                    load8<EB>(w + (long long)k * EB, left, w_vec, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = fmaf(own, v[e], f[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] *= g;
+            }
+            unsigned char* to = p.dx + (m * p.dx_pitch + k) * EB;
+            if (vec && left >= 8) {
+                if constexpr (EB == 2) {
+                    *reinterpret_cast<uint4*>(to) = Elem<2>::pack(f);
+                } else {
+                    reinterpret_cast<float4*>(to)[0] = make_float4(f[0], f[1], f[2], f[3]);
+                    reinterpret_cast<float4*>(to)[1] = make_float4(f[4], f[5], f[6], f[7]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < left) Elem<EB>::put(to + e * EB, f[e]);
+            }
         }
     }
 }
@@ -682,6 +737,7 @@ constexpr size_t kPieceBytes = (size_t)1 << 30;
 struct Plan {
     bool few;
     int cg, halves, planes, d_planes, kp;        // planes of x and w, float16 and bfloat16; of d
+    int out_warps;                               // of the logits' kernels, that take results
     int v_width, k_width, unit;                  // tiles along the classes, along the inputs; pieces are multiples of `unit`
     long long cap;
     long long dx_rows;                           // of the sums for dx, all splits
@@ -711,9 +767,14 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
         a.total = 256 + (back ? (size_t)M * V * 4 : 0);
         return a;
     }
-    // Pairs of CTAs halve what a product takes from L2, single ones waste less of ragged rows.  Measured (pairs / single), gradients:
-    // 8 x 250 rows, 256 -> 1000, floats 91 / 74 us, bfloat16 46 / 43; 512 -> 16000 853 / 928 and 189 / 203.
-    a.cg = M / N > 128 && V * K > (1 << 19) ? 2 : 1;
+    // Pairs of CTAs halve what a product takes from L2, single ones waste less of ragged rows.  Measured (pairs / single): loss of 8 x
+    // 300 rows, 128 -> 8000, floats 66 / 61 us, bfloat16 36 / 33; of 8 x 817, 1024 -> 30001, 359 / 414; gradients of 8 x 250, 256 ->
+    // 1000, floats 91 / 74, bfloat16 46 / 43; of 8 x 1000, 256 -> 8000 622 / 696 and 174 / 183.
+    a.cg = M / N > 128 && (back ? V * K > (1 << 19) : K > 512) ? 2 : 1;
+    // Sixteen warps for the results hide each other's waits where a tile's products take less time than they do; eight keep more in
+    // registers.  Measured (16 / 8): loss of 8 x 1000 rows, 40 -> 20000, floats 203 / 243 us, 512 -> 8000 258 / 280, bfloat16
+    // 1024 -> 30001 373 / 359; gradients of 8 x 1000 rows, bfloat16 40 -> 20000 281 / 298, of 8 x 326, 1024 -> 30001 640 / 629.
+    a.out_warps = K <= 512 ? 16 : 8;
     a.halves = elem_bytes == 4 && !back ? 2 : 0;
     a.planes = elem_bytes == 2 ? 1 : back ? 3 : 0;
     a.d_planes = elem_bytes == 4 ? 3 : grad_bytes == 4 ? 2 : 1;
@@ -730,7 +791,7 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     at += up(cap * a.kp * (a.planes + a.halves) * 2, 256);
     a.part = at;
     if (!back) {
-        at += up(2 * up(V, a.v_width) / a.v_width * cap * 8, 256);
+        at += up(a.out_warps / 4 * up(V, a.v_width) / a.v_width * cap * 8, 256);
     } else {
         const size_t wt = up(K, a.k_width) / a.k_width, split_rows = (size_t)kMaxTurns * (kSms / a.cg) / wt * 128 * a.cg;
         a.dx = at;
@@ -754,9 +815,9 @@ bool map_of(CUtensorMap* map, void* base, int eb, int rank, const long long* dim
     return combo_host::encode_tiled(map, type, rank, base, d, s, box, ones, plain ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass q, const Maps& maps, long long tiles, int sms, int smem_optin, cudaStream_t st) {
+template <int CG, int MODE, int PA, int PB, int OB, int kOutWarps = 8> cudaError_t launch_loss(Pass q, const Maps& maps, long long tiles, int sms, int smem_optin, cudaStream_t st) {
     static uint64_t allowed;
-    auto kern = k_loss<CG, MODE, PA, PB, OB>;
+    auto kern = k_loss<CG, MODE, PA, PB, OB, kOutWarps>;
     const int turn = MODE == kWeights && !q.vec ? kOutWarps * kTurn : MODE == kRows || MODE == kWeights ? kOutWarps * kPut : 0, most = smem_optin - kStaticSmem;
     q.stage_bytes = (PA * 2 + PB * (q.width / CG / 64)) * kBlock;
     q.stages = (most - 1024 - turn) / q.stage_bytes;
@@ -765,7 +826,7 @@ template <int CG, int MODE, int PA, int PB, int OB> cudaError_t launch_loss(Pass
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles < sms / CG ? tiles : sms / CG) * CG);
-    cfg.blockDim = dim3(kTcThreads);
+    cfg.blockDim = dim3(out_threads(kOutWarps));
     cfg.dynamicSmemBytes = 1024 + (size_t)q.stages * q.stage_bytes + turn;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -821,8 +882,10 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
 
     cudaError_t e = combo_host::launch_after(k_count, dim3(p.N), dim3(kCountThreads), 0, st, p, s);
     if (e != cudaSuccess) return e;
-    e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((cap + kPackRows - 1) / kPackRows)), dim3(kThreads), (size_t)(p.N + 1) * 4, st, p, s,
-                                 (int)vec_ok(p.x, p.x_pitch, 0, EB));
+    const long long pack_per = a.cap / (sms * 32);
+    const int pack_lot = pack_per < 1 ? 1 : pack_per > 8 ? 8 : (int)pack_per;
+    e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((a.cap + pack_lot * kWarps - 1) / (pack_lot * kWarps))), dim3(kThreads), (size_t)(p.N + 1) * 4, st, p,
+                                 s, (int)vec_ok(p.x, p.x_pitch, 0, EB), pack_lot);
     if (e != cudaSuccess) return e;
 
     // bfloat16 or floats by whole boxes where 16-byte boundaries allow
@@ -890,8 +953,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.wt = (classes + a.v_width - 1) / a.v_width;
         q.steps = a.kp / kStep;
         const Maps logits_of = L == 2 ? Maps{mxh, mwh, mwh} : Maps{mx, mw, mw};
-        if constexpr (kBack) e = launch_loss<CG, kGrad, L, L, D>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
-        else e = launch_loss<CG, kStats, L, L, 1>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
+        constexpr int kMode = kBack ? kGrad : kStats, kOut = kBack ? D : 1;
+        e = a.out_warps == 16 ? launch_loss<CG, kMode, L, L, kOut, 16>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
+                              : launch_loss<CG, kMode, L, L, kOut, 8>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
         if (e != cudaSuccess) return e;
         if constexpr (kBack) {
             q.width = a.k_width;
@@ -908,14 +972,15 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         }
     }
     if (!kBack) {
-        const int pieces = 2 * ((p.V + a.v_width - 1) / a.v_width), warps = pieces >= 8 * kFinishWarps ? kFinishWarps : pieces / 8 < 4 ? 4 : pieces / 8;
+        const int pieces = a.out_warps / 4 * ((p.V + a.v_width - 1) / a.v_width), warps = pieces >= 8 * kFinishWarps ? kFinishWarps : pieces / 8 < 4 ? 4 : pieces / 8;
         return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(warps * 32), 0, st, p, s, pieces);
     }
     q.width = a.k_width;
     q.wt = kt;
-    const long long lots = (long long)p.M * a.kp / 8, grid = (lots + kThreads - 1) / kThreads;
-    return combo_host::launch_after(k_rows_out<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s, q,
-                                    (int)vec_ok(p.dx, p.dx_pitch, 0, EB), (int)w_vec);
+    const long long per = p.M / (sms * 32);
+    const int lot = per < 1 ? 1 : per > 8 ? 8 : (int)per;
+    return combo_host::launch_after(k_rows_out<EB>, dim3((unsigned)((p.M + lot * kWarps - 1) / (lot * kWarps))), dim3(kThreads), 0, st, p, s, q,
+                                    (int)vec_ok(p.dx, p.dx_pitch, 0, EB), (int)w_vec, lot);
 }
 
 template <int CG> cudaError_t launch_tensor(const Plan& a, const Loss& p, int elem_bytes, int grad_bytes, void* scratch, int sms, int smem_optin, cudaStream_t st) {

@@ -35,7 +35,8 @@ enum Mode { kStats = 0, kGrad = 1, kRows = 2, kWeights = 3 };
 
 constexpr int kStep = 64;                    // values of r in a stage
 constexpr int kBlock = 64 * kStep * 2;       // bytes of a block of 64 x 64
-constexpr int kOutWarps = 8, kFirstOutWarp = 4, kCols = 1024 / kOutWarps, kTcThreads = 32 * (kFirstOutWarp + kOutWarps);
+constexpr int kFirstOutWarp = 4;
+constexpr int out_threads(int warps) { return 32 * (kFirstOutWarp + warps); }
 constexpr int kMaxStages = 8;
 constexpr int kTurn = 32 * 33 * 4;           // weights': bytes in which a warp turns 32 x 32 results
 constexpr int kPut = 32 * 128;               // bytes that a warp hands to TMA: 32 rows of 128
@@ -70,7 +71,7 @@ struct Pass {
     const int* count;                        // labelled rows of a worker
     const float *x_unit, *w_unit;            // forward, floats: what a packed row's, and a class's of the piece, numbers count in
     int piece;                               // classes of a piece
-    float2* part;                            // [2 tiles of classes][row_cap]
+    float2* part;                            // [pieces of a thread's columns][row_cap]
     float* own;                              // a row's logit of its label; kGrad: what the first plane of d leaves of its d
     float* dx;                               // [splits][rows][dx_pitch]
     unsigned char* dw;
@@ -177,16 +178,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void load32(const void* from, uint32_t (&v)[8]) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-                 : "l"(from)
-                 : "memory");
-}
-
 // A warp's columns c .. of acc, 128 bytes of a lane's row, into shared memory in TMA's order (16 bytes of a row at their number xor
 // the row's), and on from there by `hand`, which one thread calls.
-template <int EB, typename F> __device__ __forceinline__ void put_box(uint32_t put, const f32x2 (&acc)[kCols / 2], int c, int lane, F hand) {
+template <int EB, int kCols, typename F> __device__ __forceinline__ void put_box(uint32_t put, const f32x2 (&acc)[kCols], int c, int lane, F hand) {
     if (elect()) tma_store_wait_read();
     __syncwarp();
 #pragma unroll
@@ -194,7 +188,7 @@ template <int EB, typename F> __device__ __forceinline__ void put_box(uint32_t p
         uint32_t o[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const f32x2 v = acc[(EB == 4 ? (c + k * 4 + e) / 2 : (c + k * 8) / 2 + e) % (kCols / 2)];
+            const f32x2 v = acc[(EB == 4 ? (c + k * 4 + e) / 2 : (c + k * 8) / 2 + e) % kCols];
             o[e] = EB == 4 ? __float_as_uint(e & 1 ? hi_of(v) : lo_of(v)) : combo_step::pack_bf16(lo_of(v), hi_of(v));
         }
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + lane * 128 + ((k ^ (lane & 7)) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
@@ -207,10 +201,10 @@ template <int EB, typename F> __device__ __forceinline__ void put_box(uint32_t p
 }
 
 // PA, PB: planes of the height's and the width's operand.  OB: weights': bytes of a result; kGrad: planes of d.
-template <int CG, int MODE, int PA, int PB, int OB>
-__global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __grid_constant__ Maps maps) {
+template <int CG, int MODE, int PA, int PB, int OB, int kOutWarps>
+__global__ void __launch_bounds__(out_threads(kOutWarps), 1) k_loss(const Pass q, const __grid_constant__ Maps maps) {
     constexpr bool A_R = MODE != kWeights, B_R = MODE == kStats || MODE == kGrad;
-    constexpr int kPlanes = PA > PB ? PA : PB;
+    constexpr int kPlanes = PA > PB ? PA : PB, kCols = 1024 / kOutWarps;
     constexpr bool kHalf = MODE == kStats && PA == 2;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 4];
@@ -404,7 +398,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                 if (q.vec) {
 #pragma unroll
                     for (int c = 0; c < kCols; c += 128 / OB)
-                        if (c < columns && col + c < q.K) put_box<OB>(put, acc, c, lane, [&] { tma_store_3d(&maps.out, put, col + c, v, x.w); });
+                        if (c < columns && col + c < q.K) put_box<OB, kCols / 2>(put, acc, c, lane, [&] { tma_store_3d(&maps.out, put, col + c, v, x.w); });
                 } else {
                     // off 16-byte boundaries: lots of 32 x 32 are turned and stored a line at a time
                     float* turned = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + q.stages * q.stage_bytes + (warp - kFirstOutWarp) * kTurn);
@@ -542,7 +536,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_loss(const Pass q, const __gr
                     if (!q.add || x.steps > 0) {
 #pragma unroll
                         for (int c = 0; c < kCols; c += 32)
-                            if (c < columns) put_box<4>(put, acc, c, lane, [&] { q.add ? tma_add_3d(&maps.out, put, col + c, y, 0) : tma_store_3d(&maps.out, put, col + c, y, 0); });
+                            if (c < columns) put_box<4, kCols / 2>(put, acc, c, lane, [&] { q.add ? tma_add_3d(&maps.out, put, col + c, y, 0) : tma_store_3d(&maps.out, put, col + c, y, 0); });
                     }
                 }
             }

@@ -91,7 +91,7 @@ def test_training_with_dropout_runs():
 
 def test_which_kernels_a_loss_takes():
     for counts, n_in, n_out, path in (([40, 9], 64, 20, combo.STEP_MULTIPLY_ADD), ([40, 9], 256, 3000, combo.STEP_TENSOR),
-                                      ([300, 200], 256, 3000, combo.STEP_TENSOR_PAIRS), ([1500, 900], 64, 20, combo.STEP_TENSOR)):
+                                      ([300, 200], 520, 3000, combo.STEP_TENSOR_PAIRS), ([1500, 900], 64, 20, combo.STEP_TENSOR)):
         for dtype in (torch.float32, torch.bfloat16):
             c = Case(counts, n_in, n_out, dtype)
             c.forward()
