@@ -60,6 +60,7 @@ struct Pass {
     int v0, w_row;                           // the piece's first class, and where the map of the weights has it
     int v_end;                               // weights': behind the piece's last class
     int clusters, split_steps;               // rows': that run at once; a whole piece's stages
+    float split_cost;
     int add, vec;                            // rows': whether sums are there already; weights': whether TMA may store them
     int scaled;                              // whether d holds the rows' factors g; else the weights' gradients are divided by `count`
     long long row_cap;
@@ -82,15 +83,16 @@ struct alignas(64) Maps {
 };
 
 // Into how many parts the sums over a piece's classes are cut, to have work for all CTAs where rows are few: the number with the
-// fewest turns for the whole, a turn being a part of a tile; of at least eight stages, and in four turns at most.
+// least time, in tiles of the whole sum: turns of the CTAs by parts of a tile, and what a part's sums cost in memory (written, read
+// and added up: split_cost for as many tiles as stages).
 constexpr int kMaxSplits = 16, kMaxTurns = 4;
 __device__ __forceinline__ int splits_of(const Pass& q) {
     const int total = q.tiles[q.N] * q.wt;
     int best = 1;
     float least = 1e30f;
     for (int s = 1; s <= kMaxSplits && (s == 1 || (s * 8 <= q.split_steps && total * s <= kMaxTurns * q.clusters)); ++s) {
-        const float turns = (float)((total * s + q.clusters - 1) / q.clusters) / s;
-        if (turns < 0.95f * least) { least = turns; best = s; }
+        const float time = (float)((total * s + q.clusters - 1) / q.clusters) / s + s * q.split_cost * total / q.split_steps;
+        if (time < least) { least = time; best = s; }
     }
     return best;
 }
