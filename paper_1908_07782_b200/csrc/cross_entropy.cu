@@ -325,7 +325,7 @@ using namespace combo_loss;
 
 // Where things lie in scratch.
 struct Packed {
-    int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 1]; [cap]: forward the row, backward the worker; [cap]
+    int *count, *list, *pos, *row0, *tiles, *src, *label;      // [N]; [M]; [M]; [N + 1]; [N + 2]; [cap]: forward the row, backward the worker; [cap]
     float *lse, *g, *own;                                      // [cap]
     unsigned short *xh, *wh;                                   // forward, floats: planes of float16, as x and w
     float *x_unit, *w_unit;                                    // [cap], [N][piece]: what their numbers count in
@@ -503,7 +503,7 @@ __device__ __forceinline__ float store_line(const unsigned char* line, int K, in
 }
 
 // Packs the labelled rows, `lot` to a warp, whose places its lanes look up at once; the first CTA leaves the tables of where the workers' rows lie.
-template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss p, const Packed s, int vec, int lot) {
+template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss p, const Packed s, int vec, int lot, const Splits splits) {
     extern __shared__ int begins[];                            // packed rows [N + 1]
     __shared__ int sums[kWarps];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -536,6 +536,7 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
     if (blockIdx.x == 0) {
         for (int w = t; w <= p.N; w += kThreads) s.row0[w] = begins[w];
         scan(s.height, s.tiles, 1);
+        if (t == 0) s.tiles[p.N + 1] = splits_of(splits, s.tiles[p.N]);
     }
     const int total = begins[p.N];
     const int j0 = (blockIdx.x * kWarps + warp) * lot, rows = min(lot, total - j0);
@@ -660,7 +661,7 @@ __device__ __forceinline__ void load32(const void* from, uint32_t (&v)[8]) {
 template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const Loss p, const Packed s, const Pass q, int vec, int w_vec, int lot) {
     combo_step::pdl_release();
     combo_step::pdl_wait();
-    const int lane = threadIdx.x & 31, splits = splits_of(q);
+    const int lane = threadIdx.x & 31, splits = q.tiles[q.N + 1];
     const long long total = q.row0[q.N], a = min(max((long long)p.begin[0], 0LL), p.M), b = min(max((long long)p.begin[p.N], a), p.M);
     const long long m0 = a + (blockIdx.x * (long long)kWarps + (threadIdx.x >> 5)) * lot;
     const int rows = (int)min((long long)lot, b - m0);
@@ -688,11 +689,18 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_rows_out(const L
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = 0.0f;
             if (j >= 0) {
-                for (int i = 0; i < splits; ++i) {
-                    uint32_t v[8];
-                    load32(q.dx + (i * total + j) * q.dx_pitch + k, v);
+                for (int i = 0; i < splits; i += 4) {
+                    uint32_t v[4][8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(v[e]);
+                    for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[h][e] = 0u;
+                        if (i + h < splits) load32(q.dx + ((i + h) * total + j) * q.dx_pitch + k, v[h]);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(v[h][e]);
                 }
                 if (EB == 2) {
                     // d of a row's label is most of its gradient: what the plane's rounding left of it comes here
@@ -786,7 +794,7 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     a.unit = a.v_width;
     a.cap = (long long)up(M + 63 * (N < M ? N : M), 64);
     const size_t cap = (size_t)a.cap;
-    size_t at = up((size_t)N * 4, 256) + 2 * up((size_t)M * 4, 256) + 2 * up((size_t)(N + 1) * 4, 256) + 6 * up(cap * 4, 256);
+    size_t at = up((size_t)N * 4, 256) + 2 * up((size_t)M * 4, 256) + 2 * up((size_t)(N + 2) * 4, 256) + 6 * up(cap * 4, 256);
     a.x = at;
     at += up(cap * a.kp * (a.planes + a.halves) * 2, 256);
     a.part = at;
@@ -857,8 +865,8 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     s.count = reinterpret_cast<int*>(take((size_t)p.N * 4));
     s.list = reinterpret_cast<int*>(take((size_t)p.M * 4));
     s.pos = reinterpret_cast<int*>(take((size_t)p.M * 4));
-    s.row0 = reinterpret_cast<int*>(take((size_t)(p.N + 1) * 4));
-    s.tiles = reinterpret_cast<int*>(take((size_t)(p.N + 1) * 4));
+    s.row0 = reinterpret_cast<int*>(take((size_t)(p.N + 2) * 4));
+    s.tiles = reinterpret_cast<int*>(take((size_t)(p.N + 2) * 4));
     s.src = reinterpret_cast<int*>(take(cap * 4));
     s.label = reinterpret_cast<int*>(take(cap * 4));
     s.lse = reinterpret_cast<float*>(take(cap * 4));
@@ -882,15 +890,17 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
 
     cudaError_t e = combo_host::launch_after(k_count, dim3(p.N), dim3(kCountThreads), 0, st, p, s);
     if (e != cudaSuccess) return e;
+    // a part's sums: 128 KB a CTA, at 5 TB/s each way, against 0.29 us a stage (floats six times)
+    const int kt = (p.K + a.k_width - 1) / a.k_width, whole = (int)(piece < (long long)up(p.V, 64) ? piece : up(p.V, 64)) / kStep;
+    const Splits splits = {kSms / CG, kt, whole, 0.125f * CG / (EB == 4 ? 6 : 1)};
     const long long pack_per = a.cap / (sms * 32);
     const int pack_lot = pack_per < 1 ? 1 : pack_per > 8 ? 8 : (int)pack_per;
     e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((a.cap + pack_lot * kWarps - 1) / (pack_lot * kWarps))), dim3(kThreads), (size_t)(p.N + 1) * 4, st, p,
-                                 s, (int)vec_ok(p.x, p.x_pitch, 0, EB), pack_lot);
+                                 s, (int)vec_ok(p.x, p.x_pitch, 0, EB), pack_lot, splits);
     if (e != cudaSuccess) return e;
 
     // bfloat16 or floats by whole boxes where 16-byte boundaries allow
     const bool dw_vec = kBack && vec_ok(p.dw, p.dw_pitch, p.dw_stride, kBack ? GB : 4) && p.dw_pitch < (1LL << 36) && p.dw_stride < (1LL << 36);
-    const int kt = (p.K + a.k_width - 1) / a.k_width;
     const long long dx_pitch = kt * a.k_width;
     CUtensorMap mx = {}, mw = {}, mxh = {}, mwh = {}, md = {}, mdw = {}, out_dx = {}, out_dw = {};
     const long long lines = (long long)piece * a.kp, flat = a.cap * a.kp;
@@ -917,8 +927,6 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.N = p.N;
     q.V = p.V;
     q.K = p.K;
-    q.clusters = kSms / CG;
-    q.split_cost = 0.125f * CG / (EB == 4 ? 6 : 1);      // 128 KB a CTA, at 5 TB/s each way, against 0.29 us a stage (floats six times)
     q.row_cap = a.cap;
     q.count = s.count;
     q.x_unit = s.x_unit;
@@ -938,7 +946,6 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.dw_stride = p.dw_stride;
     q.part_steps = EB == 4 ? 2 : 16;
     q.dx_pitch = dx_pitch;
-    q.split_steps = (int)(piece < up(p.V, 64) ? piece : up(p.V, 64)) / kStep;
     const long long row_tiles = p.M / s.height + (p.N < p.M ? p.N : p.M);          // at most
     for (int v0 = 0; v0 < p.V; v0 += piece) {
         const int classes = p.V - v0 < piece ? p.V - v0 : piece;

@@ -50,7 +50,8 @@ __device__ __forceinline__ bool give_up(int site) {
     return false;
 }
 
-// Where the packed rows of the workers lie: `row0` [N + 1] first packed row (multiples of 64), `tiles` [N + 1] tiles of rows before.
+// Where the packed rows of the workers lie: `row0` [N + 1] first packed row (multiples of 64), `tiles` [N + 2] tiles of rows before, and the
+// number of parts of dx's sums.
 struct Pass {
     const int *row0, *tiles;
     int N, V, K;
@@ -59,8 +60,6 @@ struct Pass {
     int stages, stage_bytes;
     int v0, w_row;                           // the piece's first class, and where the map of the weights has it
     int v_end;                               // weights': behind the piece's last class
-    int clusters, split_steps;               // rows': that run at once; a whole piece's stages
-    float split_cost;
     int add, vec;                            // rows': whether sums are there already; weights': whether TMA may store them
     int scaled;                              // whether d holds the rows' factors g; else the weights' gradients are divided by `count`
     long long row_cap;
@@ -84,15 +83,20 @@ struct alignas(64) Maps {
 
 // Into how many parts the sums over a piece's classes are cut, to have work for all CTAs where rows are few: the number with the
 // least time, in tiles of the whole sum: turns of the CTAs by parts of a tile, and what a part's sums cost in memory (written, read
-// and added up: split_cost for as many tiles as stages).
+// and added up: `cost` for as many tiles as stages).
 constexpr int kMaxSplits = 16, kMaxTurns = 4;
-__device__ __forceinline__ int splits_of(const Pass& q) {
-    const int total = q.tiles[q.N] * q.wt;
+struct Splits {
+    int clusters, wt, steps;                 // that run at once; tiles along the inputs; a whole piece's stages
+    float cost;
+};
+__device__ __forceinline__ int splits_of(const Splits& q, int tiles) {
+    const int total = tiles * q.wt;
+    const float each = q.cost * total / q.steps;
     int best = 1;
     float least = 1e30f;
-    for (int s = 1; s <= kMaxSplits && (s == 1 || (s * 8 <= q.split_steps && total * s <= kMaxTurns * q.clusters)); ++s) {
-        const float time = (float)((total * s + q.clusters - 1) / q.clusters) / s + s * q.split_cost * total / q.split_steps;
-        if (time < least) { least = time; best = s; }
+    for (int s = 1; s <= kMaxSplits && (s == 1 || (s * 8 <= q.steps && total * s <= kMaxTurns * q.clusters)); ++s) {
+        const float time = (float)((total * s + q.clusters - 1) / q.clusters) / s + s * each;
+        if (time < 0.95f * least) { least = time; best = s; }
     }
     return best;
 }
@@ -111,7 +115,7 @@ template <int CG, int MODE> struct Walk {
     int w, row, rows, code, high;            // the lane's tile; w < 0: none
     __device__ __forceinline__ Walk(const Pass& q_, int first, int stride_) : q(q_), t(first), stride(stride_) {
         lane = threadIdx.x & 31;
-        splits = MODE == kRows ? splits_of(q) : 1;
+        splits = MODE == kRows ? q.tiles[q.N + 1] : 1;
         at = 32;
     }
     __device__ __forceinline__ void find() {
