@@ -1,0 +1,64 @@
+"""The grouped cross entropy where the classes are taken in several pieces, and at the largest numbers of classes and inputs."""
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import paper_1908_07782_b200 as combo  # noqa: E402
+from loss_util import Case  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.mark.parametrize("dtype,out,counts,n_in,n_out", [(BF16, F32, [2100, 2000], 64, 66000), (F32, F32, [1200, 900], 40, 90000),
+                                                         (BF16, BF16, [3000, 70], 72, 180001)])
+def test_gradients_in_pieces(dtype, out, counts, n_in, n_out):
+    # d alone is more than a piece's gigabyte
+    planes = 3 if dtype == F32 else 2 if out == F32 else 1
+    assert sum(counts) * n_out * 2 * planes > 1 << 30
+    c = Case(counts, n_in, n_out, dtype, out)
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
+
+
+def test_loss_in_pieces():
+    """Float weights whose planes are more than a gigabyte."""
+    c = Case([1] * 64, 1000, 4500, F32)
+    assert 64 * 4500 * 1024 * 4 > 1 << 30
+    c.forward()
+    c.check_forward()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("counts,n_in,n_out", [([3], 16, 1 << 20), ([2, 1], 1 << 20, 8)])
+def test_the_most_classes_and_inputs(counts, n_in, n_out, dtype):
+    c = Case(counts, n_in, n_out, dtype)
+    c.forward()
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
+    combo.combo_device_status()
+
+
+def test_many_rows_of_few_labels():
+    c = Case([30000, 0, 9000], 40, 70, BF16, F32, keep=0.02, mean=False)
+    c.forward()
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_most_workers(dtype):
+    c = Case([k % 3 == 0 for k in range(8192)], 16, 300, dtype)
+    c.forward()
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
