@@ -898,7 +898,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     // a part's sums: 128 KB a CTA, at 5 TB/s each way, against 0.29 us a stage (floats six times)
     const int kt = (p.K + a.k_width - 1) / a.k_width, whole = (int)(piece < (long long)up(p.V, 64) ? piece : up(p.V, 64)) / kStep;
     const Splits splits = {kSms / CG, kt, whole, 0.125f * CG / (EB == 4 ? 6 : 1)};
-    const long long pack_per = a.cap / (sms * 32);
+    const long long pack_per = a.cap / (sms * 64);
     const int pack_lot = pack_per < 1 ? 1 : pack_per > 8 ? 8 : (int)pack_per;
     e = combo_host::launch_after(k_pack<EB>, dim3((unsigned)((a.cap + pack_lot * kWarps - 1) / (pack_lot * kWarps))), dim3(kThreads), (size_t)(p.N + 1) * 4, st, p,
                                  s, (int)vec_ok(p.x, p.x_pitch, 0, EB), pack_lot, splits);
@@ -992,7 +992,8 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     }
     q.width = a.k_width;
     q.wt = kt;
-    const long long per = p.M / (sms * 32);
+    // several rows to a warp where there are many: one search for all, but rows wait for one another
+    const long long per = p.M / (sms * 128);
     const int lot = per < 1 ? 1 : per > 8 ? 8 : (int)per;
     return combo_host::launch_after(k_rows_out<EB>, dim3((unsigned)((p.M + lot * kWarps - 1) / (lot * kWarps))), dim3(kThreads), 0, st, p, s, q,
                                     (int)vec_ok(p.dx, p.dx_pitch, 0, EB), (int)w_vec, lot);
