@@ -6,12 +6,12 @@
 // orders, and planes of both kinds for the logits and for the gradients cost more than they save).  Then, for a piece of the classes at a time,
 //
 //                height (128 a CTA)      width                  summed r          results
-//   logits       rows                    classes                inputs            forward: (max, sum of exponentials) of a row's 128
+//   logits       rows                    classes                inputs            forward: (max, sum of exponentials) of a row's 64 or 128
 //                                                                                 classes; backward: d, as bfloat16 planes in scratch
 //   rows'        rows                    inputs                 classes           dx, added up in scratch over the pieces
 //   weights'     classes                 inputs                 rows              dW
 //
-// A lane of TMEM is a row of results, so the softmax needs no exchange between threads: a thread holds 128 logits of one row.
+// A lane of TMEM is a row of results, so the softmax needs no exchange between threads: a thread holds 64 or 128 logits of one row.
 // Floats are products of planes: x0 w0 + (x0 w1 + x1 w0), and for three x0 w2 + x1 w1 + x2 w0; what is left out of a product is
 // 2^-24 of it on average, or below that.  (Forward by three planes: 254 against 185 us for 32 x 1056 rows, 512 -> 1000.)
 // The tensor cores truncate at every addition of 16 products, so only `part_steps` stages of 64 are summed there (floats: two, with the
@@ -108,7 +108,7 @@ struct Tile {
 };
 
 // Walks the tiles t, t + stride, ...; the whole warp.  Lanes find 32 tiles at once: the search and the divisions take more than a
-// thousand cycles, and taking them before every tile left the ring of stages short of loads (16 stages a tile: 700 cycles a stage).
+// thousand cycles, during which nothing is loaded (tiles of 16 stages: 621 cycles a stage with them before every tile, 597 so).
 template <int CG, int MODE> struct Walk {
     const Pass& q;
     int t, stride, lane, at, splits;
