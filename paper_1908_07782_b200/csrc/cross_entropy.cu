@@ -967,8 +967,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.steps = a.kp / kStep;
         const Maps logits_of = L == 2 ? Maps{mxh, mwh, mwh} : Maps{mx, mw, mw};
         constexpr int kMode = kBack ? kGrad : kStats, kOut = kBack ? D : 1;
-        e = a.out_warps == 16 ? launch_loss<CG, kMode, L, L, kOut, 16>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
-                              : launch_loss<CG, kMode, L, L, kOut, 8>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
+        constexpr int kMost = CG == 2 && !kBack ? 8 : 16;              // forward, pairs take more than 512 inputs
+        e = a.out_warps == kMost ? launch_loss<CG, kMode, L, L, kOut, kMost>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st)
+                                 : launch_loss<CG, kMode, L, L, kOut, 8>(q, logits_of, row_tiles * q.wt, sms, smem_optin, st);
         if (e != cudaSuccess) return e;
         if constexpr (kBack) {
             q.width = a.k_width;
