@@ -401,14 +401,26 @@ __global__ void __launch_bounds__(out_threads(kOutWarps), 1) k_loss(const Pass q
                 }
                 const int v = q.v0 + x.h0 + rank * 128 + quarter * 32;
                 if (v >= q.v_end) continue;
+                const int lines = min(q.v_end - v, 32);
                 if (q.vec) {
+                    // TMA writes whole 16 bytes: the box in which a line ends inside them is left to the lanes, a class each
+                    const bool whole = q.K * OB % 16 == 0;
 #pragma unroll
-                    for (int c = 0; c < kCols; c += 128 / OB)
-                        if (c < columns && col + c < q.K) put_box<OB, kCols / 2>(put, acc, c, lane, [&] { tma_store_3d(&maps.out, put, col + c, v, x.w); });
+                    for (int c = 0; c < kCols; c += 128 / OB) {
+                        if (c < columns && col + c < q.K) {
+                            if (whole || col + c + 128 / OB <= q.K) {
+                                put_box<OB, kCols / 2>(put, acc, c, lane, [&] { tma_store_3d(&maps.out, put, col + c, v, x.w); });
+                            } else if (lane < lines) {
+                                unsigned char* to = q.dw + (x.w * q.dw_stride + (v + lane) * q.dw_pitch + col + c) * OB;
+#pragma unroll
+                                for (int e = 0; e < 128 / OB; ++e)
+                                    if (col + c + e < q.K) combo_step::Elem<OB>::put(to + e * OB, e & 1 ? hi_of(acc[(c + e) / 2 % (kCols / 2)]) : lo_of(acc[(c + e) / 2 % (kCols / 2)]));
+                            }
+                        }
+                    }
                 } else {
                     // off 16-byte boundaries: lots of 32 x 32 are turned and stored a line at a time
                     float* turned = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + q.stages * q.stage_bytes + (warp - kFirstOutWarp) * kTurn);
-                    const int lines = min(q.v_end - v, 32);
 #pragma unroll
                     for (int c = 0; c < kCols; c += 32) {
                         if (c < columns) {

@@ -101,7 +101,8 @@ __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int
                      : "memory");
 }
 // A box of this CTA's shared memory to global memory; the thread that asked may wait until it has been read (the memory may be
-// used again), or is there.
+// used again), or is there.  Outside the map nothing is written, but for a line that ends inside 16 bytes: those are written whole
+// (measured: lines of 773 floats, the three behind each).
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t from, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(from), "r"(x), "r"(y), "r"(z)
                  : "memory");

@@ -199,3 +199,43 @@ def test_a_view_beside_the_input():
     wide[:, :32] = c.x
     combo.combo_grouped_cross_entropy_backward(wide[:, :32], c.w, c.labels, c.exact_lse(), None, wide[:, 32:], c.dw, c.begin, c.scratch(True))
     assert torch.equal(wide[:, 32:], want)
+
+
+# Pairs of CTAs in both directions: eight warps for the results, several tiles along the inputs, workers' ends inside a pair.
+BY_PAIRS = {
+    "dense": dict(counts=[300, 0, 200], n_in=776, n_out=1500, keep=0.6),
+    "factors": dict(counts=[300, 0, 200], n_in=776, n_out=1500, keep=0.6, mean=False),
+    "off 16 bytes": dict(counts=[300, 0, 200], n_in=776, n_out=1500, keep=0.6, xp=3, wp=1, skew=1),
+    "ends inside 16 bytes": dict(counts=[150, 290], n_in=773, n_out=1501, xp=3, wp=3, gap=8, mean=False),
+}
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("shape", BY_PAIRS)
+def test_values_and_gradients_by_pairs(shape, types):
+    c = Case(dtype=types[0], out=types[1], seed=len(shape), **BY_PAIRS[shape])
+    c.forward()
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR_PAIRS
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR_PAIRS
+    c.check_backward(lse)
+    for buf, t in ((c.dx_buf, c.dx), (c.dw_buf, c.dw)):
+        assert int((~buf.isnan()).sum()) == t.numel()
+
+
+@pytest.mark.parametrize("n_out,path", [(13, combo.STEP_MULTIPLY_ADD), (301, combo.STEP_TENSOR)])
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_widths_that_end_inside_16_bytes(types, n_out, path):
+    """Places, pitches and strides on 16 bytes, widths that are not."""
+    c = Case([129, 65, 0, 257], 77, n_out, types[0], types[1], keep=0.6, mean=False, xp=3, wp=3, gap=8)
+    c.forward()
+    assert combo.combo_last_step_path() == path
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == path
+    c.check_backward(lse)
+    for buf, t in ((c.dx_buf, c.dx), (c.dw_buf, c.dw)):
+        assert int((~buf.isnan()).sum()) == t.numel()
