@@ -239,3 +239,15 @@ def test_widths_that_end_inside_16_bytes(types, n_out, path):
     c.check_backward(lse)
     for buf, t in ((c.dx_buf, c.dx), (c.dw_buf, c.dw)):
         assert int((~buf.isnan()).sum()) == t.numel()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+def test_more_workers_than_threads_in_few_multiply_adds(types):
+    c = Case([k % 3 for k in range(700)], 32, 10, types[0], types[1], lead=1, behind=2, keep=0.8)
+    c.forward()
+    assert combo.combo_last_step_path() == combo.STEP_MULTIPLY_ADD
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == combo.STEP_MULTIPLY_ADD
+    c.check_backward(lse)

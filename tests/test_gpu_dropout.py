@@ -147,3 +147,50 @@ def test_captured_and_on_another_stream():
     combo.combo_dropout(x, None, z, None, 0.5, 3, 4, stream=s)
     torch.cuda.synchronize()
     assert torch.equal(y, z)
+
+
+def kept_rows(rows, n, p, seed, rnd, site, worker):
+    """As kept(), all rows at once."""
+    u = np.uint64
+    with np.errstate(over="ignore"):
+        z = np.arange(rows * -(-n // 4), dtype=u) ^ u(step(step(step(seed) ^ (rnd << 32 | worker)) ^ (1 << 63 | site)))
+        z = z + u(0x9E3779B97F4A7C15)
+        z = (z ^ (z >> u(30))) * u(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> u(27))) * u(0x94D049BB133111EB)
+        z = z ^ (z >> u(31))
+    return z.astype("<u8").view("<u2").reshape(rows, -(-n // 4) * 4)[:, :n] >= int(p * 65536 + 0.5)
+
+
+# 148 SMs hold 4736 warps: each takes several rounds of loads, in which rows and workers change
+ROUNDS = {
+    "several rows": dict(n=40, each=800, workers=300, extra=8), "off 16 bytes": dict(n=37, each=500, workers=300, extra=2, skew=1),
+    "parts of a row": dict(n=2500, each=50, workers=150, extra=4), "odd parts of a row": dict(n=2501, each=50, workers=150, extra=2, skew=1),
+    "one worker": dict(n=200, each=40000, workers=1, extra=0), "many workers": dict(n=16, each=40, workers=8000, extra=0),
+}
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", ROUNDS)
+def test_several_rounds_to_a_warp(shape, dtype, residual):
+    n, each, workers, extra, skew = (ROUNDS[shape].get(k, 0) for k in ("n", "each", "workers", "extra", "skew"))
+    p, seed, rnd, site = 0.2, 99, 5, 3
+    r = np.random.default_rng(n)
+    counts = r.integers(0, 2 * each, workers) * (r.random(workers) < 0.8) if workers > 1 else [each]
+    lead, behind = (3, 5) if workers > 1 else (0, 0)
+    at = lead + np.concatenate([[0], np.cumsum(counts)])
+    M = int(at[-1]) + behind
+    g = torch.Generator().manual_seed(n)
+    _, x = array(M, n, n + extra, dtype, skew, g)
+    add = array(M, n, n + extra, dtype, skew, g)[1] if residual else None
+    buf, y = array(M, n, n + extra, dtype, skew, g)
+    before = y.clone()
+    combo.combo_dropout(x, add, y, torch.tensor(at).to(DEV) if workers > 1 else None, p, seed, rnd, site)
+    keep = torch.from_numpy(np.concatenate([kept_rows(int(c), n, p, seed, rnd, site, w) for w, c in enumerate(counts)])).to(DEV)
+    inside = slice(int(at[0]), int(at[-1]))
+    want = torch.where(keep, x[inside].float() * np.float32(65536 / (65536 - int(p * 65536 + 0.5))), 0.0)
+    if residual:
+        want = want + add[inside].float()
+    assert torch.equal(y[inside], want.to(dtype))
+    assert torch.equal(y[:lead], before[:lead]) and torch.equal(y[M - behind:], before[M - behind:])
+    assert int((~buf.isnan()).sum()) == y.numel()

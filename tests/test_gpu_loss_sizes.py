@@ -62,3 +62,22 @@ def test_the_most_workers(dtype):
     lse = c.exact_lse()
     c.backward(lse)
     c.check_backward(lse)
+
+
+def test_loss_in_pieces_off_16_bytes():
+    """bfloat16 weights whose copy is more than a gigabyte."""
+    assert 8 * 70001 * 1024 * 2 > 1 << 30
+    c = Case([3, 1, 0, 2, 1, 5, 1, 1], 1000, 70001, BF16, xp=3, wp=1, skew=1)
+    c.forward()
+    c.check_forward()
+
+
+@pytest.mark.parametrize("dtype,out,counts,n_in,n_out", [(BF16, F32, [2100, 2000], 61, 66000), (F32, F32, [1200, 900], 39, 90000),
+                                                         (BF16, BF16, [3000, 70], 77, 180001)])
+def test_gradients_in_pieces_off_16_bytes(dtype, out, counts, n_in, n_out):
+    planes = 3 if dtype == F32 else 2 if out == F32 else 1
+    assert sum(counts) * n_out * 2 * planes > 1 << 30
+    c = Case(counts, n_in, n_out, dtype, out, xp=3, wp=1, skew=1, mean=False)
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
