@@ -949,7 +949,6 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.dw = p.dw;
     q.dw_pitch = p.dw_pitch;
     q.dw_stride = p.dw_stride;
-    q.part_steps = EB == 4 ? 2 : 16;
     q.dx_pitch = dx_pitch;
     const long long row_tiles = p.M / s.height + (p.N < p.M ? p.N : p.M);          // at most
     for (int v0 = 0; v0 < p.V; v0 += piece) {
@@ -965,6 +964,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.width = a.v_width;
         q.wt = (classes + a.v_width - 1) / a.v_width;
         q.steps = a.kp / kStep;
+        q.part_steps = EB == 4 ? 2 : 16;
         const Maps logits_of = L == 2 ? Maps{mxh, mwh, mwh} : Maps{mx, mw, mw};
         constexpr int kMode = kBack ? kGrad : kStats, kOut = kBack ? D : 1;
         constexpr int kMost = CG == 2 && !kBack ? 8 : 16;              // forward, pairs take more than 512 inputs
@@ -991,8 +991,6 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         const int pieces = a.out_warps / 4 * ((p.V + a.v_width - 1) / a.v_width), warps = pieces >= 8 * kFinishWarps ? kFinishWarps : pieces / 8 < 4 ? 4 : pieces / 8;
         return combo_host::launch_after(k_finish, dim3((unsigned)((cap + 31) / 32)), dim3(warps * 32), 0, st, p, s, pieces);
     }
-    q.width = a.k_width;
-    q.wt = kt;
     // several rows to a warp where there are many: one search for all, but rows wait for one another
     const long long per = p.M / (sms * 128);
     const int lot = per < 1 ? 1 : per > 8 ? 8 : (int)per;

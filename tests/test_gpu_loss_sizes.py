@@ -81,3 +81,17 @@ def test_gradients_in_pieces_off_16_bytes(dtype, out, counts, n_in, n_out):
     lse = c.exact_lse()
     c.backward(lse)
     c.check_backward(lse)
+
+
+def test_pieces_sum_alike():
+    """Classes of equal weights, one in every 256, lie at the same places of the tiles of every piece: wherever no row has them as its
+    label their gradients are equal to the last bit."""
+    counts, n_in, n_out = [2100, 2000], 520, 256 * 258
+    assert sum(counts) * n_out * 2 * 2 > 1 << 30               # d alone is more than a piece
+    c = Case(counts, n_in, n_out, BF16, F32)
+    c.w.copy_(c.w[:, :256].repeat(1, n_out // 256, 1))
+    c.labels %= 256
+    c.forward()
+    c.backward(c.lse)
+    dw = c.dw.view(2, n_out // 256, 256, n_in)
+    assert torch.equal(dw[:, 1:], dw[:, 1:2].expand(-1, n_out // 256 - 1, -1, -1))
