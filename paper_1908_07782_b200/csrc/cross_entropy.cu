@@ -173,9 +173,9 @@ template <int EB, bool VEC> __global__ void __launch_bounds__(kThreads) k_few_lo
         s = 0.0f;
         for (int k = 0; k < kWarps; ++k)
             for (int u = 0; u < kU; ++u) join(m, s, sm[0][k][u * kR + r], sm[1][k][u * kR + r]);
-        const float lse = m + logf(s);
-        p.lse[i0 + r] = where[r] >= 0 ? lse : 0.0f;
-        p.loss[i0 + r] = where[r] >= 0 ? lse - (&sm[2][0][0])[where[r]] : 0.0f;
+        const float rest = logf(s);                            // s is at least 1
+        p.lse[i0 + r] = where[r] >= 0 ? m + rest : 0.0f;
+        p.loss[i0 + r] = where[r] >= 0 ? m - (&sm[2][0][0])[where[r]] + rest : 0.0f;
     }
 }
 
@@ -631,9 +631,9 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, cons
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = fmaxf(most, v[e].x);
             const float zero = most == -INFINITY ? 0.0f : most;
-            sum *= exp2_fast(m - zero);
+            sum *= exp2_fast((m - zero) * kLog2E);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[e].y * exp2_fast(v[e].x - zero);
+            for (int e = 0; e < 8; ++e) sum += v[e].y * exp2_fast((v[e].x - zero) * kLog2E);
             m = most;
         }
     }
@@ -647,10 +647,11 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, cons
         const float zero = most == -INFINITY ? 0.0f : most;
         sum = 0.0f;
 #pragma unroll 8
-        for (int k = 0; k < warps; ++k) sum += sm[1][k][lane] * exp2_fast(sm[0][k][lane] - zero);
-        const float lse = (zero + log2f(sum)) * 0.69314718f;
-        p.lse[from] = lse;
-        p.loss[from] = lse - s.own[j];
+        for (int k = 0; k < warps; ++k) sum += sm[1][k][lane] * exp2_fast((sm[0][k][lane] - zero) * kLog2E);
+        // the sum is at least 1: a loss is not below 0, and small ones do not come out of a difference of large logits
+        const float rest = logf(sum);
+        p.lse[from] = zero + rest;
+        p.loss[from] = zero - s.own[j] + rest;
     }
 }
 

@@ -470,15 +470,15 @@ __global__ void __launch_bounds__(out_threads(kOutWarps), 1) k_loss(const Pass q
                             for (int e = 0; e < 16; ++e) most[e & 3] = fmaxf(most[e & 3], fmaxf(lo_of(acc[c / 2 + e]), hi_of(acc[c / 2 + e])));
                         }
                     }
-                    // exponents of two against the largest one as it is rounded here, so that its rounding does not enter the sum
-                    const float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * kLog2E, zero = m == -INFINITY ? 0.0f : -m;
+                    // differences to the largest first, so that a row's sum holds a 1 and no rounding of large logits
+                    const float m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), zero = m == -INFINITY ? 0.0f : -m;
                     f32x2 sum[2] = {0, 0};
 #pragma unroll
                     for (int c = 0; c < kCols; c += 32) {
                         if (c < columns) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
-                                const f32x2 x2 = fma2(acc[c / 2 + e], pair(kLog2E, kLog2E), pair(zero, zero));
+                                const f32x2 x2 = mul2(add2(acc[c / 2 + e], pair(zero, zero)), pair(kLog2E, kLog2E));
                                 sum[e & 1] = add2(sum[e & 1], pair(exp2_fast(lo_of(x2)), exp2_fast(hi_of(x2))));
                             }
                         }
