@@ -24,7 +24,6 @@ namespace combo_loss {
 using namespace combo_tc;
 using combo_step::add2;
 using combo_step::f32x2;
-using combo_step::fma2;
 using combo_step::hi_of;
 using combo_step::lo_of;
 using combo_step::mul2;
@@ -495,7 +494,7 @@ __global__ void __launch_bounds__(out_threads(kOutWarps), 1) k_loss(const Pass q
                     }
                 } else if constexpr (MODE == kGrad) {
                     const int left = q.v_end - (q.v0 + col), label = q.label[j];
-                    const float lse = label >= 0 ? -q.lse[j] * kLog2E : 0.0f;
+                    const float lse = label >= 0 ? -q.lse[j] : 0.0f;
                     const int at = label - q.v0 - col;
                     const bool here = label >= 0 && at >= 0 && at < columns;
                     const bool any = __any_sync(0xffffffffu, here), all = __all_sync(0xffffffffu, label >= 0) && left >= columns;
@@ -509,7 +508,8 @@ __global__ void __launch_bounds__(out_threads(kOutWarps), 1) k_loss(const Pass q
                         if (c < columns) {
 #pragma unroll
                             for (int e = c / 2; e < c / 2 + 16; ++e) {
-                                const f32x2 x2 = fma2(acc[e], pair(kLog2E, kLog2E), pair(lse, lse));
+                                // the difference first: a product would be rounded at the size of the logits
+                                const f32x2 x2 = mul2(add2(acc[e], pair(lse, lse)), pair(kLog2E, kLog2E));
                                 acc[e] = pair(exp2_fast(lo_of(x2)), exp2_fast(hi_of(x2)));
                             }
                             if (any) {

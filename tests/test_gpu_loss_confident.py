@@ -1,4 +1,5 @@
-"""The loss of rows whose label's class leads by far: it goes to zero and is never below, however large the logits are."""
+"""Rows whose label's class leads by far: their loss goes to zero and is never below, and so do their gradients, however large the
+logits are."""
 import os
 import sys
 
@@ -7,16 +8,16 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 import paper_1908_07782_b200 as combo  # noqa: E402
-from loss_util import DEV, U, Case  # noqa: E402
+from loss_util import DEV, HALF, U, Case  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
 
 
-def confident(counts, n_in, n_out, dtype, lead, offset):
+def confident(counts, n_in, n_out, dtype, lead, offset, **more):
     """Rows with one input of 1, so that logits are weights, which either type holds: the label's `offset`, the others' `lead` to
     `lead` + 24 below."""
-    c = Case(counts, n_in, n_out, dtype)
+    c = Case(counts, n_in, n_out, dtype, **more)
     g = torch.Generator().manual_seed(n_out)
     pick = torch.arange(c.M) % n_in
     label = (pick * 7 + 3) % n_out
@@ -81,3 +82,28 @@ def test_a_single_class_costs_nothing(dtype, n_in):
     c.forward()
     assert (c.loss == 0).all()
     c.check_forward()
+
+
+@pytest.mark.parametrize("offset,lead", [(20.0, 10.0), (250.0, 10.0), (250.0, 45.0), (-90.0, 45.0)])
+@pytest.mark.parametrize("counts,n_in,n_out,path", [([3, 1, 20], 64, 10, combo.STEP_MULTIPLY_ADD), ([40, 130], 64, 700, combo.STEP_TENSOR),
+                                                    ([40, 130], 600, 2000, combo.STEP_TENSOR), ([300, 200], 600, 1000, combo.STEP_TENSOR_PAIRS)])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (BF16, F32)], ids=["f32", "bf16", "bf16-f32"])
+def test_small_gradients_of_large_logits(types, counts, n_in, n_out, path, offset, lead):
+    c = confident(counts, n_in, n_out, types[0], lead, offset, out=types[1], mean=False)
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == path
+    for w, (a, b) in enumerate(c.spans):
+        x, wt, g, e = c.x[a:b].double(), c.w[w].double(), c.row_grad[a:b].double()[:, None], lse[a:b].double()[:, None]
+        t = x @ wt.T - e
+        hot = torch.zeros_like(t).scatter_(1, c.labels[a:b, None], 1.0)
+        d = (torch.exp(t) - hot) * g
+        # Logits are exact.  The difference to lse is rounded, and its product with log2(e); an exponential is off by 2^-22 of its
+        # value; then come the difference to 1 and the factor.
+        dd = g.abs() * (torch.exp(t) * (3 * t.abs() + 6) * U + 2.0 ** -126) + 2 * U * d.abs()
+        n = b - a
+        for got, want, tol, half in (
+                (c.dx[a:b], d @ wt, (dd + HALF[types[0]] * d.abs()) @ wt.abs() + 2 * (n_out + 4) * U * (d.abs() @ wt.abs()), HALF[types[0]]),
+                (c.dw[w], d.T @ x, (dd + (2.0 ** -16 if types[1] != types[0] else HALF[types[0]]) * d.abs()).T @ x.abs() +
+                 2 * (n + 4) * U * (d.abs().T @ x.abs()), HALF[types[1]])):
+            Case.near(got, want, tol, half, "gradients of worker %d" % w)
