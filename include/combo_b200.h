@@ -490,9 +490,8 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  * bfloat16: exact products, summed as in combo_grouped_linear, in parts of 1024 (a float
  * dW: of 256) added with rounding.  d is rounded to bfloat16 once for dx and for a
  * bfloat16 dW (what that leaves of the label's d, most of a row's gradient, is added to dx
- * in binary32), and kept to 16 bits for a float dW (off by 3e-6 of its size, 6e-7 with
- * row_grad NULL, where the mean's factor is applied behind the products and the label's d
- * stays near -1).
+ * in binary32), and kept to 24 bits for a float dW; with row_grad NULL the mean's factor is
+ * applied behind the products.
  * float: products of parts of 22 bits (forward; 2^-39 of the row's or class's largest value
  * where that is more) and 24 bits (backward), relative errors of some 1e-7 to 5e-7 of the
  * sums' magnitudes; small problems by multiply-adds.

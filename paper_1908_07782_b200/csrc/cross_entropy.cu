@@ -787,11 +787,12 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     a.cg = M / N > 128 && (back ? V * K > (1 << 19) : K > 512) ? 2 : 1;
     // Sixteen warps for the results hide each other's waits where a tile's products take less time than they do; eight keep more in
     // registers.  Measured (16 / 8): loss of 8 x 1000 rows, 40 -> 20000, floats 203 / 243 us, 512 -> 8000 258 / 280, bfloat16
-    // 1024 -> 30001 373 / 359; gradients of 8 x 1000 rows, bfloat16 40 -> 20000 281 / 298, of 8 x 326, 1024 -> 30001 640 / 629.
-    a.out_warps = K <= 512 ? 16 : 8;
+    // 1024 -> 30001 373 / 359; gradients of 8 x 1000 rows, bfloat16 40 -> 20000 281 / 298, of 8 x 326, 1024 -> 30001 640 / 629; with
+    // three planes of d to write, 4 x 1995 rows, 768 -> 32000 1777 / 1887, 5 x 1000, 1216 -> 9213 529 / 525.
+    a.out_warps = K <= (elem_bytes == 2 && grad_bytes == 4 ? 1024 : 512) ? 16 : 8;
     a.halves = elem_bytes == 4 && !back ? 2 : 0;
     a.planes = elem_bytes == 2 ? 1 : back ? 3 : 0;
-    a.d_planes = elem_bytes == 4 ? 3 : grad_bytes == 4 ? 2 : 1;
+    a.d_planes = grad_bytes == 4 ? 3 : 1;
     a.kp = (int)up(K, 64);
     const int most = elem_bytes == 4 && back && a.cg == 1 ? 128 : 256;       // two stages in shared memory
     a.v_width = even_width(V, most, 128);
@@ -857,7 +858,7 @@ template <int CG, int MODE, int PA, int PB, int OB, int kOutWarps = 8> cudaError
 // EB: bytes of the inputs; GB: of dW (0: forward).
 template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Loss& p, unsigned char* scratch, int sms, int smem_optin, cudaStream_t st) {
     constexpr bool kBack = GB != 0;
-    constexpr int P = EB == 4 ? 3 : 1, L = EB == 2 ? 1 : kBack ? 3 : 2, D = EB == 4 ? 3 : GB == 4 ? 2 : 1;      // planes: of the gradients' products, of the logits', of d
+    constexpr int P = EB == 4 ? 3 : 1, L = EB == 2 ? 1 : kBack ? 3 : 2, D = GB == 4 ? 3 : 1;      // planes: of the gradients' products, of the logits', of d
     const auto vec_ok = [](const void* b, long long pitch, long long stride, int eb) {
         return combo_host::aligned_to(b, 16) && pitch * eb % 16 == 0 && stride * eb % 16 == 0;
     };
@@ -981,8 +982,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
             e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw, out_dx}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
             if (e != cudaSuccess) return e;
             q.ht = (classes + s.height - 1) / s.height;
-            // Floats summed in shorter parts: off by 6e-7 of their size instead of 2e-6 (4 x 1995 rows), for a twentieth of the time.
-            if (D == 2) q.part_steps = 4;
+            // Floats of bfloat16 take d to 24 bits, in three planes, and are summed in shorter parts: off by 6e-7 of their size (4 x
+            // 1995 rows; 1.1e-6 in parts of 512, for a hundredth of the time; 2.5e-6 with two planes, for a quarter).
+            if (EB == 2 && GB == 4) q.part_steps = 4;
             q.vec = dw_vec;
             e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{mdw, mx, out_dw}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
             if (e != cudaSuccess) return e;

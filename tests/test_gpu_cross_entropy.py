@@ -251,3 +251,23 @@ def test_more_workers_than_threads_in_few_multiply_adds(types):
     c.backward(lse)
     assert combo.combo_last_step_path() == combo.STEP_MULTIPLY_ADD
     c.check_backward(lse)
+
+
+@pytest.mark.parametrize("mean", [True, False])
+@pytest.mark.parametrize("counts,n_in,n_out", [([40, 1, 9], 48, 400), ([60, 33], 32, 600), ([64] * 40, 64, 20)])
+def test_float_gradients_of_bfloat16_rows_have_float_precision(counts, n_in, n_out, mean):
+    """Seen over a worker's gradients as a whole: d enters a float dW to 24 bits."""
+    c = Case(counts, n_in, n_out, BF16, F32, mean=mean)
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR
+    for w in range(c.N):
+        rows, x, wt, z, dz = c.logits(w)
+        g = torch.full((len(rows), 1), 1.0 / len(rows), dtype=torch.float64, device=DEV) if mean else c.row_grad[rows].double()[:, None]
+        p = torch.exp(z - lse[rows].double()[:, None])
+        hot = torch.zeros_like(p).scatter_(1, c.labels[rows, None], 1.0)
+        want = ((p - hot) * g).T @ x
+        error = float((c.dw[w].double() - want).norm() / want.norm())
+        # the tensor cores truncate when they add 16 products: logits, of 1.5 on average, by n_in / 16 units of 2 U, the sums over the
+        # rows by as many as there are sixteens; an exponential is off by 4 U, d by 3 more, what its three planes leave by one
+        assert error <= (1.5 * 2 * (n_in / 16 + 1) + 8 + 2 * (len(rows) / 16 + 1)) * U, error / U
