@@ -479,7 +479,7 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  *
  * Outputs must not overlap inputs, scratch or one another (x and dx may lie beside each
  * other in a wider array).  A NaN or infinity reaches the results that its row and its
- * worker's weights enter, no others.  Results do not change from run to run.
+ * worker's weights enter, no others.  Results do not change from run to run (with as much scratch).
  *
  * Arithmetic: logits, exponentials and sums in binary32, relative to the row's largest
  * logit; an exponential below 2^-126 counts as 0.  A loss is formed from differences of
@@ -498,12 +498,25 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  * bfloat16 weights whose base, pitch and stride are multiples of 16 bytes are read where
  * they lie; others, and floats, are brought into scratch a piece at a time.
  *
- * scratch: device memory of at least combo_grouped_cross_entropy_scratch_bytes bytes
- * (grad_bytes 0 for the forward call), 256-byte aligned, contents undefined afterwards;
- * about a gigabyte where d or the weights' parts of all classes are larger than that.
+ * scratch: device memory, 256-byte aligned, contents undefined afterwards, of
+ * combo_grouped_cross_entropy_scratch_bytes bytes (grad_bytes 0 for the forward call), or
+ * of less, down to combo_grouped_cross_entropy_least_scratch_bytes: the classes are then
+ * taken in smaller pieces, at the price of time and, in backward, of another order in
+ * which dx is added up.  With R = M + 63 min(N, M) (every worker's rows are rounded up to
+ * 64, labelled or not), K = n_in up to a multiple of 128 and V = n_out it holds, in bytes,
+ *   packed rows           2 R K (bfloat16), 4 R K (floats, forward), 6 R K (backward)
+ *   forward               R V / 16 to R V / 4 of pieces' maxima and sums
+ *   backward              4 R K of dx's sums, more where they are cut into parts
+ *   a piece of C classes  2 R C of d (bfloat16 dW), 6 R C (float dW), and the weights' parts:
+ *                         2 N C K (bfloat16 off 16 bytes), 4 N C K (floats, forward), 6 N C K
+ * with C from 128 or 256, or all there are if that is less, up to what a gigabyte holds.
+ * A forward call on bfloat16 weights on 16 bytes has no pieces: it is as fast with the
+ * least.  Few rows and classes (multiply-adds): 4 M n_out bytes in backward.
  */
 size_t combo_grouped_cross_entropy_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes,
                                                  int grad_bytes);
+size_t combo_grouped_cross_entropy_least_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes,
+                                                       int grad_bytes);
 combo_status combo_grouped_cross_entropy(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch,
                                          int64_t w_stride, int elem_bytes, const int64_t* d_labels,
                                          const int64_t* d_begin, int N, int64_t M, int64_t n_in, int64_t n_out,

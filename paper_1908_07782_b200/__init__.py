@@ -17,4 +17,5 @@ from .binding import (ComboError, combo_aggregation_divergence, combo_aggregatio
                       STEP_TENSOR_THREADS, STEP_RESIDENT, STEP_STREAMED,
                       combo_grouped_linear, combo_grouped_linear_grad_input, combo_grouped_linear_grad_weight,
                       combo_grouped_cross_entropy, combo_grouped_cross_entropy_backward,
-                      combo_grouped_cross_entropy_scratch_bytes, combo_dropout)
+                      combo_grouped_cross_entropy_scratch_bytes, combo_grouped_cross_entropy_least_scratch_bytes,
+                      combo_dropout)

@@ -87,8 +87,9 @@ def load():
     lib.combo_grad_scratch_bytes.restype = ctypes.c_size_t
     lib.combo_group_norm_scratch_bytes.argtypes = [i64, i64, i64, i32]
     lib.combo_group_norm_scratch_bytes.restype = ctypes.c_size_t
-    lib.combo_grouped_cross_entropy_scratch_bytes.argtypes = [i32, i64, i64, i64, i32, i32]
-    lib.combo_grouped_cross_entropy_scratch_bytes.restype = ctypes.c_size_t
+    for name in ("combo_grouped_cross_entropy_scratch_bytes", "combo_grouped_cross_entropy_least_scratch_bytes"):
+        getattr(lib, name).argtypes = [i32, i64, i64, i64, i32, i32]
+        getattr(lib, name).restype = ctypes.c_size_t
     lib.combo_set_kernel_path.argtypes = [i32]
     lib.combo_set_kernel_path.restype = None
     lib.combo_set_tuning.argtypes = [i32, i32]
@@ -499,6 +500,11 @@ def _loss_args(name, x, w, labels, floats, begin):
 def combo_grouped_cross_entropy_scratch_bytes(N: int, M: int, n_in: int, n_out: int, elem_bytes: int, grad_bytes: int = 0) -> int:
     """Scratch of combo_grouped_cross_entropy, or, with the size of dw's elements, of its backward call."""
     return int(load().combo_grouped_cross_entropy_scratch_bytes(N, M, n_in, n_out, elem_bytes, grad_bytes))
+
+
+def combo_grouped_cross_entropy_least_scratch_bytes(N: int, M: int, n_in: int, n_out: int, elem_bytes: int, grad_bytes: int = 0) -> int:
+    """The least scratch that those calls take: the classes in smaller pieces, for more time (none for bfloat16 forward on 16 bytes)."""
+    return int(load().combo_grouped_cross_entropy_least_scratch_bytes(N, M, n_in, n_out, elem_bytes, grad_bytes))
 
 
 def combo_grouped_cross_entropy(x, w, labels, loss, lse, begin, scratch, stream=None):

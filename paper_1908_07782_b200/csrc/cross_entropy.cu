@@ -334,7 +334,7 @@ struct Packed {
     float *lse, *g, *own;                                      // [cap]
     unsigned short *xh, *wh;                                   // forward, floats: planes of float16, as x and w
     float *x_unit, *w_unit;                                    // [cap], [N][piece]: what their numbers count in
-    unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][piece][kp]; of [piece / 8][cap][8]
+    unsigned short *x, *w, *d;                                 // planes of [cap][kp]; of [N][classes there are][kp]; of [piece / 8][cap][8]
     float2* part;
     float* dx;
     long long cap;
@@ -585,8 +585,8 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_pack(const Loss 
 }
 
 // The weights of `classes` classes from v0 on as planes, zeros where there are none: a warp a class where it looks for the largest
-// (forward, floats), else threads side by side along all of them.
-template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Loss p, const Packed s, int v0, int classes, int vec) {
+// (forward, floats; a piece's units lie `piece` apart), else threads side by side along all of them.
+template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Loss p, const Packed s, int v0, int classes, int piece, int vec) {
     combo_step::pdl_release();
     combo_step::pdl_wait();
     const int lane = threadIdx.x & 31;
@@ -595,7 +595,7 @@ template <int EB> __global__ void __launch_bounds__(kThreads) k_planes(const Los
         for (long long line = blockIdx.x * (long long)kWarps + (threadIdx.x >> 5); line < lines; line += (long long)gridDim.x * kWarps) {
             const int w = (int)(line / classes), v = v0 + (int)(line - (long long)w * classes);
             const float unit = store_line(p.w + (w * p.w_stride + v * p.w_pitch) * EB, v < p.V ? p.K : 0, s.kp, vec, lane, true, s.wh + line * s.kp, plane);
-            if (lane == 0) s.w_unit[line] = unit;
+            if (lane == 0) s.w_unit[(long long)w * piece + (v - v0)] = unit;
         }
         return;
     }
@@ -744,8 +744,12 @@ bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int
 
 constexpr int kSms = 148;
 // Aimed at for a piece of classes: d, and the weights' planes.  Pieces that stay in L2 cost more by their launches and by adding
-// to dx than reading d from memory does: gradients of 8 x 326 rows, 1024 -> 30001 1006 us (160 MB), 727 (512 MB), 610 (1.2 GB).
+// to dx than reading d from memory does: gradients of 8 x 326 rows, 1024 -> 30001 791 us (256 MB), 685 (512 MB), 607 (1 GB), of 4 x
+// 1995, 768 -> 32000 2236, 1856, 1829.  A caller who would rather have the memory gives less.
 constexpr size_t kPieceBytes = (size_t)1 << 30;
+// Asked for of that for copies of bfloat16 weights, which calls on 16-byte boundaries do not make: forward 8 x 1000 rows, 1023 ->
+// 30001 722 us (128 MB), 641 (256 MB), 601 (all, 491 MB).
+constexpr size_t kCopyBytes = (size_t)1 << 28;
 
 // How a call is computed, by its sizes alone.
 struct Plan {
@@ -755,7 +759,8 @@ struct Plan {
     int v_width, k_width, unit;                  // tiles along the classes, along the inputs; pieces are multiples of `unit`
     long long cap;
     long long dx_rows;                           // of the sums for dx, all splits
-    size_t x, part, dx, region, room, total;     // places in scratch; bytes of the region for pieces
+    size_t x, part, dx, region;                  // places in scratch
+    size_t room, least, total;                   // bytes of the region for pieces; of scratch, at least and as it pays
 };
 
 size_t up(size_t n, size_t unit) { return (n + unit - 1) / unit * unit; }
@@ -765,9 +770,16 @@ int even_width(int64_t n, int most, int unit) {
     return (int)up((size_t)((n + tiles - 1) / tiles), unit);
 }
 
-// Bytes of a piece of so many classes.
-size_t piece_bytes(const Plan& a, int N, size_t classes, bool back, bool direct) {
-    return (back ? up(classes * a.cap * a.d_planes * 2, 256) : 0) + (direct ? 0 : up(classes * N * a.kp * (a.planes + a.halves) * 2 + classes * N * 4, 256));
+// Classes whose weights a piece has planes of.
+size_t lines_of(size_t piece, size_t V) { return piece < up(V, 8) ? piece : up(V, 8); }
+
+// Bytes of a piece of so many classes: of d, and of the weights' planes.
+size_t d_bytes(const Plan& a, size_t piece) { return up(piece * a.cap * a.d_planes * 2, 256); }
+size_t planes_bytes(const Plan& a, int N, size_t V, size_t piece) {
+    return up((size_t)N * (lines_of(piece, V) * a.kp * (a.planes + a.halves) * 2 + (a.halves ? piece * 4 : 0)), 256);
+}
+size_t piece_bytes(const Plan& a, int N, size_t V, size_t piece, bool back, bool direct) {
+    return (back ? d_bytes(a, piece) : 0) + (direct ? 0 : planes_bytes(a, N, V, piece));
 }
 
 Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_bytes) {
@@ -778,7 +790,7 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     // 160 / 45; of 8000 rows, 256 -> 10, 86 / 84 and 113 / 46; many classes of few inputs take a warp many turns (16 -> 1000: 75 to 300).
     a.few = M == 0 || (M <= 2048 && V <= kFewClasses && V * K <= (elem_bytes == 4 ? 1 << 15 : 1 << 14));
     if (a.few) {
-        a.total = 256 + (back ? (size_t)M * V * 4 : 0);
+        a.total = a.least = 256 + (back ? (size_t)M * V * 4 : 0);
         return a;
     }
     // Pairs of CTAs halve what a product takes from L2, single ones waste less of ragged rows.  Measured (pairs / single): loss of 8 x
@@ -814,9 +826,12 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
         at += up((size_t)a.dx_rows * wt * a.k_width * 4, 256);
     }
     a.region = at;
-    const size_t whole = piece_bytes(a, N, up(V, a.unit), back, false), least = piece_bytes(a, N, a.unit, back, false);
-    a.room = whole < kPieceBytes ? whole : least > kPieceBytes ? least : kPieceBytes;
+    const size_t all = up(V, a.unit), copy = planes_bytes(a, N, V, all), least = piece_bytes(a, N, V, a.unit, back, false);
+    a.room = (back ? d_bytes(a, all) : 0) + (elem_bytes == 4 || copy < kCopyBytes ? copy : kCopyBytes);
+    if (a.room > kPieceBytes) a.room = kPieceBytes;
+    if (a.room < least) a.room = least;
     a.total = at + a.room;
+    a.least = at + least;
     return a;
 }
 
@@ -888,12 +903,13 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     // bfloat16 weights on 16-byte boundaries are read where they lie
     const bool w_vec = vec_ok(p.w, p.w_pitch, p.w_stride, EB), direct = EB == 2 && w_vec && p.w_pitch < (1LL << 36) && p.w_stride < (1LL << 36);
     int piece = (int)up(p.V, a.unit);
-    for (int n = 2; piece > a.unit && !(direct && !kBack) && piece_bytes(a, p.N, piece, kBack, direct) > a.room; ++n)
+    for (int n = 2; piece > a.unit && !(direct && !kBack) && piece_bytes(a, p.N, p.V, piece, kBack, direct) > a.room; ++n)
         piece = (int)up((p.V + n - 1) / n, a.unit);
+    const int there = (int)lines_of(piece, p.V);               // classes whose weights have planes
     s.d = reinterpret_cast<unsigned short*>(scratch + a.region);
-    s.w_unit = reinterpret_cast<float*>(s.d + (kBack ? up((size_t)piece * cap * D * 2, 256) / 2 : 0));
+    s.w_unit = reinterpret_cast<float*>(s.d + (kBack ? d_bytes(a, piece) / 2 : 0));
     s.wh = reinterpret_cast<unsigned short*>(s.w_unit + (a.halves ? (size_t)piece * p.N : 0));
-    s.w = s.wh + (size_t)piece * p.N * a.kp * a.halves;
+    s.w = s.wh + (size_t)there * p.N * a.kp * a.halves;
 
     cudaError_t e = combo_host::launch_after(k_count, dim3(p.N), dim3(kCountThreads), 0, st, p, s);
     if (e != cudaSuccess) return e;
@@ -910,9 +926,9 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     const bool dw_vec = kBack && vec_ok(p.dw, p.dw_pitch, p.dw_stride, kBack ? GB : 4) && p.dw_pitch < (1LL << 36) && p.dw_stride < (1LL << 36);
     const long long dx_pitch = kt * a.k_width;
     CUtensorMap mx = {}, mw = {}, mxh = {}, mwh = {}, md = {}, mdw = {}, out_dx = {}, out_dw = {};
-    const long long lines = (long long)piece * a.kp, flat = a.cap * a.kp;
+    const long long lines = (long long)there * a.kp, flat = a.cap * a.kp;
     const long long xd[3] = {a.kp, a.cap, P}, hd[3] = {a.kp, a.cap, L}, xs[2] = {a.kp, flat};
-    const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : piece, p.N, direct ? 1 : P}, vd[4] = {a.kp, piece, p.N, L};
+    const long long wd[4] = {direct ? p.K : a.kp, direct ? p.V : there, p.N, direct ? 1 : P}, vd[4] = {a.kp, there, p.N, L};
     const long long ws[3] = {direct ? p.w_pitch : a.kp, direct ? (p.N > 1 ? p.w_stride : 8) : lines, direct ? 8 : lines * p.N};
     // d: eight classes of a row in 16 bytes, rows side by side, so that a warp that writes and a box that is read run along memory;
     // in 64-bit units, of which a box may have 256
@@ -956,8 +972,8 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     for (int v0 = 0; v0 < p.V; v0 += piece) {
         const int classes = p.V - v0 < piece ? p.V - v0 : piece;
         if (!direct) {
-            const long long grid = ((long long)p.N * piece + kWarps - 1) / kWarps;
-            e = combo_host::launch_after(k_planes<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s, v0, piece, (int)w_vec);
+            const long long grid = ((long long)p.N * there + kWarps - 1) / kWarps;
+            e = combo_host::launch_after(k_planes<EB>, dim3((unsigned)(grid < sms * 16 ? grid : sms * 16)), dim3(kThreads), 0, st, p, s, v0, there, piece, (int)w_vec);
             if (e != cudaSuccess) return e;
         }
         q.v0 = v0;
@@ -1012,7 +1028,7 @@ combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in,
     if (!sizes_ok(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes)) return COMBO_ERR_INVALID_ARG;
     const bool back = grad_bytes != 0;
     if (!p.begin || !combo_host::aligned_to(p.begin, 8)) return COMBO_ERR_INVALID_ARG;
-    if (!scratch || !combo_host::aligned_to(scratch, 256) || scratch_bytes < plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes).total)
+    if (!scratch || !combo_host::aligned_to(scratch, 256) || scratch_bytes < plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes).least)
         return COMBO_ERR_INVALID_ARG;
     if (p.M > 0) {
         if (!p.x || !p.labels || p.x_pitch < n_in || p.x_pitch > (1LL << 40) / p.M) return COMBO_ERR_INVALID_ARG;
@@ -1052,7 +1068,10 @@ combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in,
     p.V = (int)n_out;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    const Plan plan = plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes);
+    Plan plan = plan_of(p.N, p.M, n_in, n_out, elem_bytes, grad_bytes);
+    // what there is, up to what pays
+    const size_t given = scratch_bytes - plan.region, pays = plan.room > kPieceBytes ? plan.room : kPieceBytes;
+    plan.room = given < pays ? given : pays;
     combo_host::set_step_path(plan.few ? combo_host::kPathMultiplyAdd : plan.cg == 2 ? combo_host::kPathTensorPairs : combo_host::kPathTensor);
     if (!plan.few) {
         e = plan.cg == 2 ? launch_tensor<2>(plan, p, elem_bytes, grad_bytes, scratch, sms, smem, st)
@@ -1086,6 +1105,10 @@ extern "C" {
 
 size_t combo_grouped_cross_entropy_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int grad_bytes) {
     return sizes_ok(N, M, n_in, n_out, elem_bytes, grad_bytes) ? plan_of(N, M, n_in, n_out, elem_bytes, grad_bytes).total : 0;
+}
+
+size_t combo_grouped_cross_entropy_least_scratch_bytes(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int grad_bytes) {
+    return sizes_ok(N, M, n_in, n_out, elem_bytes, grad_bytes) ? plan_of(N, M, n_in, n_out, elem_bytes, grad_bytes).least : 0;
 }
 
 combo_status combo_grouped_cross_entropy(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch, int64_t w_stride, int elem_bytes,

@@ -95,3 +95,38 @@ def test_pieces_sum_alike():
     c.backward(c.lse)
     dw = c.dw.view(2, n_out // 256, 256, n_in)
     assert torch.equal(dw[:, 1:], dw[:, 1:2].expand(-1, n_out // 256 - 1, -1, -1))
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (BF16, F32)], ids=["f32", "bf16", "bf16-f32"])
+@pytest.mark.parametrize("odd", [0, 1])
+@pytest.mark.parametrize("counts,n_in,n_out", [([129, 65, 0, 257], 200, 1500), ([40, 3], 136, 2057), ([300, 200], 776, 1301), ([700] * 3, 520, 20)])
+def test_the_least_scratch(counts, n_in, n_out, odd, types):
+    """Pieces of one tile of classes; the same values from any amount of scratch, rows' gradients up to the order of their sums."""
+    c = Case(counts, n_in, n_out, types[0], types[1], keep=0.8, mean=False, xp=3 * odd, wp=odd, skew=odd)
+    size = {F32: 4, BF16: 2}
+    least = [combo.combo_grouped_cross_entropy_least_scratch_bytes(c.N, c.M, n_in, n_out, size[types[0]], g) for g in (0, size[types[1]])]
+    lse = c.exact_lse()
+    want = []
+    for more in (0, 1 << 20, 1 << 30):
+        # nothing behind what was given is touched
+        f, b = (torch.full((n + more + 4096,), 0xff, dtype=torch.uint8, device="cuda:0") for n in least)
+        c.forward(f[:least[0] + more])
+        c.check_forward()
+        c.backward(lse, b[:least[1] + more])
+        c.check_backward(lse)
+        assert (f[least[0] + more:] == 0xff).all() and (b[least[1] + more:] == 0xff).all()
+        want.append([t.clone() for t in (c.loss, c.lse, c.dw)])
+    for got in want[1:]:
+        assert all(torch.equal(a, k) for a, k in zip(got, want[0]))
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (BF16, F32)], ids=["f32", "bf16", "bf16-f32"])
+def test_many_workers_of_few_classes(types):
+    """Planes of the classes there are: 20 and not a tile's 128."""
+    c = Case([k % 5 for k in range(1200)], 136, 20, types[0], types[1], keep=0.8, xp=3, wp=1, skew=1)
+    c.forward()
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)

@@ -111,3 +111,22 @@ def test_python_side_checks_name_what_is_wrong():
             combo.combo_dropout(**dict(dict(x=x, residual=None, y=x.clone(), begin=begin, p=0.5, seed=1, rnd=0), **kw))
     with pytest.raises(ValueError, match=HOST):
         combo.combo_dropout(x, None, x.clone(), begin, 0.5, 1, 0)
+
+
+def test_least_scratch(place):
+    """Less scratch than asked for is taken, down to the least; it is far less than all rows' logits where those are large."""
+    least = combo.combo_grouped_cross_entropy_least_scratch_bytes
+    assert least(2, 4, 8, 8, 4, 2) == 0 and least(2, -1, 8, 8, 4, 0) == 0
+    for elem, grad in ((4, 0), (4, 4), (2, 0), (2, 2), (2, 4)):
+        for N, M, k, v in ((2, 4, 8, 8), (8, 6536, 1024, 30001), (64, 64, 1000, 4500), (1024, 4096, 512, 10), (1, 1 << 22, 64, 1 << 20)):
+            assert 0 < least(N, M, k, v, elem, grad) <= scratch(N, M, k, v, elem, grad)
+        # the weights, the rows and an eighth of their logits
+        assert least(8, 6536, 1024, 30001, elem, grad) < 6536 * 30001 * 4 // 4
+    # a copy of bfloat16 weights, which a call on 16-byte boundaries does not make, takes a quarter of a gigabyte at most
+    assert scratch(16, 16, 1024, 32000, 2, 0) < 300 << 20 and least(16, 16, 1024, 32000, 2, 0) < 16 << 20
+    # few classes: the weights' three planes, not those of a tile's 128 classes
+    assert scratch(1024, 1024, 4096, 10, 4, 4) < 6 * (1024 * 16 + 1024 * 64 + 128) * 4096 + 4 * 1024 * 64 * 4096 + (64 << 20)
+    lib = combo.load()
+    at = lambda k: place + 2048 * k  # noqa: E731
+    need = least(2, 3000, 64, 1000, 2, 0)
+    assert lib.combo_grouped_cross_entropy(at(0), 64, at(1), 64, 64000, 2, at(2), at(3), 2, 3000, 64, 1000, at(4), at(5), at(10), need - 1, None) == INVALID
