@@ -550,7 +550,7 @@ combo_status combo_grouped_cross_entropy_backward(const void* x, int64_t x_pitch
  * holds it; `site` tells apart the dropouts of one step.  p in 0 .. 1; p = 1 keeps nothing.
  * Dropped elements are 0 (or the residual) whatever x holds.  binary32 product and sum, each
  * rounded; rounded once more to bfloat16.  y may be x or residual (same pitch); other
- * overlaps with y are refused.  n <= 2^32, M * n <= 2^40, first_worker + N <=
+ * overlaps with y, d_begin's too, are refused.  n <= 2^32, M * n <= 2^40, first_worker + N <=
  * COMBO_MAX_WORKERS.
  */
 combo_status combo_dropout(const void* x, int64_t x_pitch, const void* residual, int64_t residual_pitch, void* y,

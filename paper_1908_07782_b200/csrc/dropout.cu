@@ -221,6 +221,7 @@ extern "C" combo_status combo_dropout(const void* x, int64_t x_pitch, const void
         const combo_host::Rows rr = {residual, M, (size_t)n * eb, (size_t)residual_pitch * eb};
         if (!(x == y && (x_pitch == y_pitch || M == 1)) && combo_host::overlap(rx, ry)) return COMBO_ERR_ALIAS;
         if (residual && !(residual == y && (residual_pitch == y_pitch || M == 1)) && combo_host::overlap(rr, ry)) return COMBO_ERR_ALIAS;
+        if (d_begin && combo_host::overlap(y, ry.extent(), d_begin, ((size_t)N + 1) * 8)) return COMBO_ERR_ALIAS;
     }
     int sms = 0, smem = 0;
     const combo_status rc = combo_host::device(&sms, &smem);

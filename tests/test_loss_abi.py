@@ -130,3 +130,10 @@ def test_least_scratch(place):
     at = lambda k: place + 2048 * k  # noqa: E731
     need = least(2, 3000, 64, 1000, 2, 0)
     assert lib.combo_grouped_cross_entropy(at(0), 64, at(1), 64, 64000, 2, at(2), at(3), 2, 3000, 64, 1000, at(4), at(5), at(10), need - 1, None) == INVALID
+
+
+def test_dropout_refuses_to_write_over_its_table(place):
+    lib = combo.load()
+    for begin in (place + 4096, place + 4096 + 8 * 3, place + 4096 - 16, place + 4096 + 120):
+        # y: four rows of eight floats, 128 bytes from place + 4096 on; begin: 24 bytes
+        assert lib.combo_dropout(place, 8, None, 0, place + 4096, 8, 4, begin, 2, 4, 8, 0.5, 1, 2, 3, 0, None) == ALIAS, begin - place
