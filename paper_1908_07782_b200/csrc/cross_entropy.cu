@@ -655,11 +655,13 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const Loss p, cons
     }
 }
 
-// 32 bytes that this kernel does not write.
+// 32 bytes.  An ordinary load that stays behind the wait for the preceding kernel: it may still be writing them while this one starts,
+// which the read-only path does not allow for.
 __device__ __forceinline__ void load32(const void* from, uint32_t (&v)[8]) {
-    asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-        : "l"(from));
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "l"(from)
+                 : "memory");
 }
 
 // The rows' gradients to their places, a warp `lot` rows whose places its lanes look up at once: the parts of the sums added up,

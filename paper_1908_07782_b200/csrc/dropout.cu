@@ -52,28 +52,29 @@ __device__ __forceinline__ Owner owner_of(const Dropout& p, long long m) {
     o.end = p.M;
     o.some = true;
     if (p.begin) {
+        // (ordinary loads: a preceding kernel may have written the table while this one started)
         const long long* begin = reinterpret_cast<const long long*>(p.begin);
         const long long m0 = __shfl_sync(0xffffffffu, m, 0);
         int lo = -1, hi = p.N;                   // the last w with begin[w] <= m; -1: none
         while (lo < hi) {
             const int step = (hi - lo + 31) / 32, at = lo + 1 + (threadIdx.x & 31) * step;
-            const unsigned below = __ballot_sync(0xffffffffu, at <= hi && __ldg(begin + min(at, p.N)) <= m0);
+            const unsigned below = __ballot_sync(0xffffffffu, at <= hi && begin[min(at, p.N)] <= m0);
             if (below == 0u) break;
             const int k = 31 - __clz(below);
             hi = min(hi, lo + (k + 1) * step);
             lo = lo + 1 + k * step;
         }
         hi = p.N;
-        if (lo < p.N && __ldg(begin + lo + 1) > m) hi = lo;
+        if (lo < p.N && begin[lo + 1] > m) hi = lo;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (__ldg(begin + mid) <= m) lo = mid;
+            if (begin[mid] <= m) lo = mid;
             else hi = mid - 1;
         }
         w = lo;
         o.some = lo >= 0 && lo < p.N;
-        if (o.some) o.first = __ldg(begin + lo);
-        if (lo < p.N) o.end = __ldg(begin + lo + 1);
+        if (o.some) o.first = begin[lo];
+        if (lo < p.N) o.end = begin[lo + 1];
     }
     o.key = splitmix_step(splitmix_step(p.first ^ ((uint64_t)p.round << 32 | (uint32_t)(p.worker0 + w))) ^ (0x8000000000000000ull | p.site));
     return o;
