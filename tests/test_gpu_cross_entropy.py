@@ -271,3 +271,45 @@ def test_float_gradients_of_bfloat16_rows_have_float_precision(counts, n_in, n_o
         # the tensor cores truncate when they add 16 products: logits, of 1.5 on average, by n_in / 16 units of 2 U, the sums over the
         # rows by as many as there are sixteens; an exponential is off by 4 U, d by 3 more, what its three planes leave by one
         assert error <= (1.5 * 2 * (n_in / 16 + 1) + 8 + 2 * (len(rows) / 16 + 1)) * U, error / U
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("counts,n_in,n_out", [([300, 200], 5000, 120), ([300, 1], 4500, 250), ([600], 530, 1024)])
+def test_pairs_with_few_classes(counts, n_in, n_out, types):
+    """One or two tiles along the classes, less than a pair's height of them."""
+    c = Case(counts, n_in, n_out, types[0], types[1], keep=0.9, mean=False)
+    c.forward()
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR_PAIRS
+    c.check_backward(lse)
+
+
+@pytest.mark.parametrize("large", [2.0 ** 12, 2.0 ** 20, 2.0 ** 30])
+@pytest.mark.parametrize("counts,n_in,n_out", [([6, 9], 24, 11), ([40, 130], 96, 520), ([300, 200], 600, 700)])
+def test_one_input_far_larger_than_the_others(counts, n_in, n_out, large):
+    """Floats: an input that is large where its weights are nothing or small, and a class with one large weight."""
+    c = Case(counts, n_in, n_out, F32, mean=False, keep=0.8)
+    c.x[:, 5] *= large
+    c.w[:, :, 5] = 0.0
+    c.w[0, 3, 7] *= large
+    c.x[:, 7] /= large
+    c.w[:, 4, 5] = 0.5 / large
+    c.forward()
+    few = combo.combo_last_step_path() == combo.STEP_MULTIPLY_ADD
+    for w in range(c.N):
+        rows, x, wt, z, dz = c.logits(w)
+        # two planes of float16 keep 22 bits of a value, or 2^-39 of the largest of its row or class if that is more: an error of half
+        # of float16's least number, 2^-25, in units that take the largest to at least 2^14
+        if not few:
+            dz = dz + 2.0 ** -39 * (x.abs().amax(1)[:, None] * wt.abs().sum(1) + x.abs().sum(1)[:, None] * wt.abs().amax(1)) + \
+                c.K * 2.0 ** -78 * x.abs().amax(1)[:, None] * wt.abs().amax(1)
+        lse, own = torch.logsumexp(z, 1), z.gather(1, c.labels[rows, None])[:, 0]
+        tol = dz.max(1).values + (200 + c.V / 8) * U + 4 * U * (lse.abs() + z.max(1).values.abs())
+        assert ((c.lse[rows].double() - lse).abs() <= tol).all()
+        assert ((c.loss[rows].double() - (lse - own)).abs() <= tol + dz.max(1).values + 2 * U * own.abs()).all()
+    # backward keeps 24 bits of every value
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
