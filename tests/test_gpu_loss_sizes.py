@@ -130,3 +130,15 @@ def test_many_workers_of_few_classes(types):
     lse = c.exact_lse()
     c.backward(lse)
     c.check_backward(lse)
+
+
+def test_the_most_rows():
+    """Scratch of more than a gigabyte for one tile of classes."""
+    c = Case([1 << 21, 0, (1 << 21) - 7, 2], 24, 70, BF16, F32, keep=0.6, mean=False, lead=2, behind=3)
+    assert c.M == 1 << 22
+    c.forward()
+    c.check_forward()
+    lse = c.exact_lse()
+    c.backward(lse)
+    c.check_backward(lse)
+    combo.combo_device_status()
