@@ -509,7 +509,7 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  *   backward              4 R K of dx's sums, more where they are cut into parts
  *   a piece of C classes  2 R C of d (bfloat16 dW), 6 R C (float dW), and the weights' parts:
  *                         2 N C K (bfloat16 off 16 bytes), 4 N C K (floats, forward), 6 N C K
- * with C from 128 or 256, or all there are if that is less, up to what a gigabyte holds.
+ * with C from 128 or 256, or all there are if that is less, up to what 640 MB hold.
  * A forward call on bfloat16 weights on 16 bytes has no pieces: it is as fast with the
  * least.  Few rows and classes (multiply-adds): 4 M n_out bytes in backward.
  */
