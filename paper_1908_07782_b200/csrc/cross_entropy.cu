@@ -765,9 +765,10 @@ bool sizes_ok(int N, int64_t M, int64_t n_in, int64_t n_out, int elem_bytes, int
 
 constexpr int kSms = 148;
 // Aimed at for a piece of classes: d, and the weights' planes.  Pieces that stay in L2 cost more by their launches and by adding
-// to dx than reading d from memory does; beyond some 600 MB nothing is gained.  Measured with 128 / 256 / 512 / 640 MB / 1 GB: gradients of
-// 8 x 326 of 2186 rows, 1024 -> 30001 917 / 721 / 681 / 598 / 599 us, of 4 x 1995, 768 -> 32000 2608 / 1950 / 1868 / 1868 / 1932, of 8 x
-// 1000 floats, 256 -> 20000 1803 / 1536 / 1350 / 1350 / 1456.  A caller who would rather have the memory gives less.
+// to dx than reading d from memory does; beyond some 600 MB little is gained.  Measured with 128 / 256 / 384 / 512 MB / 1 GB more than the
+// least: gradients of 8 x 326 of 2186 rows, 1024 -> 30001 917 / 721 / 681 / 598 / 599 us, of 4 x 1995, 768 -> 32000 2608 / 1950 / 1867 /
+// 1868 / 1932, of 8 x 1000 floats, 256 -> 20000 1803 / 1536 / 1527 / 1350 / 1456; of 2 x 2000, 512 -> 60000 into floats 1401 (640 MB) and
+// 1222 (1 GB).  A caller who would rather have the memory gives less.
 constexpr size_t kPieceBytes = (size_t)640 << 20;
 // Asked for of that for copies of bfloat16 weights, which calls on 16-byte boundaries do not make: forward 8 x 1000 rows, 1023 ->
 // 30001 722 us (128 MB), 641 (256 MB), 601 (all, 491 MB).
