@@ -482,8 +482,9 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  * worker's weights enter, no others.  Results do not change from run to run (with as much scratch).
  *
  * Arithmetic: logits, exponentials and sums in binary32, relative to the row's largest
- * logit; an exponential below 2^-126 counts as 0.  A loss is formed from differences of
- * logits, so that it is exact to some 1e-6 however large they are, and not below 0.  A class at -inf has probability 0
+ * logit; an exponential below 2^-126 counts as 0.  Losses and d are formed from
+ * differences of logits: what that adds to the logits' own errors does not grow with their
+ * size, and no loss is below 0.  A class at -inf has probability 0
  * (bfloat16; an infinite float may make its logits NaN).  The classes are taken a piece
  * at a time, in backward with d in scratch between the products that form it and those
  * that use it.
