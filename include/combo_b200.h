@@ -489,7 +489,7 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  * at a time, in backward with d in scratch between the products that form it and those
  * that use it.
  * bfloat16: exact products, summed as in combo_grouped_linear, in parts of 1024 (a float
- * dW: of 256) added with rounding.  d is rounded to bfloat16 once for dx and for a
+ * dW: of 256; up to 256 classes of 128, its logits of 256) added with rounding.  d is rounded to bfloat16 once for dx and for a
  * bfloat16 dW (what that leaves of the label's d, most of a row's gradient, is added to dx
  * in binary32), and kept to 24 bits for a float dW; with row_grad NULL the mean's factor is
  * applied behind the products.

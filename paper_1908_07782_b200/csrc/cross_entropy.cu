@@ -991,6 +991,11 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
     q.dw_pitch = p.dw_pitch;
     q.dw_stride = p.dw_stride;
     q.dx_pitch = dx_pitch;
+    // Where classes are few, exponentials near 1 hand the logits' errors on, and shorter parts cost little, the classes' tile being one.
+    // Gradients of the weights off by, and time (shorter / as of more classes): floats, 13 x 1800 rows, 128 -> 18, 2.5e-7, 98 us /
+    // 1.4e-6, 91; floats of bfloat16, 3 x 1200, 1408 -> 14, 5.6e-7, 111 / 1.7e-6, 109.  Of many classes: floats, 8 x 250, 512 -> 10000,
+    // 539 / 498 us, floats of bfloat16, 4 x 1995, 768 -> 32000, 2092 / 1770, both off by less than 1e-6 as they are.
+    const bool few_classes = p.V <= kFewClasses;
     const long long row_tiles = p.M / s.height + (p.N < p.M ? p.N : p.M);          // at most
     for (int v0 = 0; v0 < p.V; v0 += piece) {
         const int classes = p.V - v0 < piece ? p.V - v0 : piece;
@@ -1005,7 +1010,7 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
         q.width = a.v_width;
         q.wt = (classes + a.v_width - 1) / a.v_width;
         q.steps = a.kp / kStep;
-        q.part_steps = EB == 4 ? 2 : 16;
+        q.part_steps = EB == 4 ? kBack && few_classes ? 1 : 2 : GB == 4 && few_classes ? 4 : 16;
         const Maps logits_of = L == 2 ? Maps{mxh, mwh, mwh} : Maps{mx, mw, mw};
         constexpr int kMode = kBack ? kGrad : kStats, kOut = kBack ? D : 1;
         constexpr int kMost = CG == 2 && !kBack ? 8 : 16;              // forward, pairs take more than 512 inputs
@@ -1017,13 +1022,14 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
             q.wt = kt;
             q.steps = (classes + kStep - 1) / kStep;
             q.add = v0 > 0;
+            if (EB == 2) q.part_steps = 16;
             // bfloat16 rows take the first plane of d: the others are below their rounding
             e = launch_loss<CG, kRows, EB == 4 ? 3 : 1, P, 1>(q, Maps{md, mw, out_dx}, row_tiles * kt * kMaxSplits, sms, smem_optin, st);
             if (e != cudaSuccess) return e;
             q.ht = (classes + s.height - 1) / s.height;
             // Floats of bfloat16 take d to 24 bits, in three planes, and are summed in shorter parts: off by 6e-7 of their size (4 x
             // 1995 rows; 1.1e-6 in parts of 512, for a hundredth of the time; 2.5e-6 with two planes, for a quarter).
-            if (EB == 2 && GB == 4) q.part_steps = 4;
+            if (EB == 2 && GB == 4) q.part_steps = few_classes ? 2 : 4;
             q.vec = dw_vec;
             e = launch_loss<CG, kWeights, D, P, GB>(q, Maps{mdw, mx, out_dw}, (long long)p.N * kt * q.ht, sms, smem_optin, st);
             if (e != cudaSuccess) return e;

@@ -313,3 +313,25 @@ def test_one_input_far_larger_than_the_others(counts, n_in, n_out, large):
     lse = c.exact_lse()
     c.backward(lse)
     c.check_backward(lse)
+
+
+@pytest.mark.parametrize("dtype,counts,n_in,n_out,mean", [(F32, [1800, 1750, 1790], 128, 18, False), (F32, [700, 800, 650], 120, 8, True),
+                                                          (BF16, [1200, 300, 900], 1408, 14, True), (BF16, [2, 5, 3], 1304, 65, True)])
+def test_gradients_of_few_classes_are_as_exact_as_32_bit_arithmetic(dtype, counts, n_in, n_out, mean):
+    """Errors over all of a float gradient: within 1.5 times those of the same formula in 32-bit torch arithmetic, or 16 units."""
+    c = Case(counts, n_in, n_out, dtype, F32, mean=mean)
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR
+    got, want, plain = [], [], []
+    for w, (a, b) in enumerate(c.spans):
+        for t, to in ((torch.float64, want), (torch.float32, plain)):
+            x, wt = c.x[a:b].to(t), c.w[w].to(t)
+            g = torch.full((b - a, 1), 1.0 / (b - a), dtype=t, device=DEV) if mean else c.row_grad[a:b, None].to(t)
+            d = torch.exp(x @ wt.T - lse[a:b, None].to(t))
+            d.scatter_add_(1, c.labels[a:b, None], torch.full((b - a, 1), -1.0, dtype=t, device=DEV))
+            to.append((d * g).T @ x)
+        got.append(c.dw[w])
+    got, want, plain = (torch.stack(t).double() for t in (got, want, plain))
+    error, allowed = float((got - want).norm() / want.norm()), float((plain - want).norm() / want.norm())
+    assert error <= max(16 * U, 1.5 * allowed), (error, allowed)
