@@ -489,10 +489,11 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  * at a time, in backward with d in scratch between the products that form it and those
  * that use it.
  * bfloat16: exact products, summed as in combo_grouped_linear, in parts of 1024 (a float
- * dW: of 256; up to 256 classes of 128, its logits of 256) added with rounding.  d is rounded to bfloat16 once for dx and for a
- * bfloat16 dW (what that leaves of the label's d, most of a row's gradient, is added to dx
- * in binary32), and kept to 24 bits for a float dW; with row_grad NULL the mean's factor is
- * applied behind the products.
+ * dW: of 256; up to 256 classes of 128, its logits of 256) added with rounding.  d is rounded to bfloat16 once for dx (what
+ * that leaves of the label's d, most of a row's gradient, is added in binary32) and for a
+ * bfloat16 dW of more than 128 rows a worker on average; a bfloat16 dW of fewer takes 16
+ * bits of it, a float dW 24.  With row_grad NULL the mean's factor is applied behind the
+ * products.
  * float: products of parts of 22 bits (forward; 2^-39 of the row's or class's largest value
  * where that is more) and 24 bits (backward), relative errors of some 1e-7 to 5e-7 of the
  * sums' magnitudes; small problems by multiply-adds.
@@ -508,7 +509,7 @@ combo_status combo_grouped_linear_grad_weight(const void* dy, int64_t dy_pitch, 
  *   packed rows           2 R K (bfloat16), 4 R K (floats, forward), 6 R K (backward)
  *   forward               R V / 16 to R V / 4 of pieces' maxima and sums
  *   backward              4 R K of dx's sums, more where they are cut into parts
- *   a piece of C classes  2 R C of d (bfloat16 dW), 6 R C (float dW), and the weights' parts:
+ *   a piece of C classes  2 R C or 4 R C of d (bfloat16 dW), 6 R C (float), and the weights' parts:
  *                         2 N C K (bfloat16 off 16 bytes), 4 N C K (floats, forward), 6 N C K
  * with C from 128 or 256, or all there are if that is less, up to what 640 MB hold.
  * A forward call on bfloat16 weights on 16 bytes has no pieces: it is as fast with the

@@ -827,7 +827,10 @@ Plan plan_of(int N, int64_t M, int64_t K, int64_t V, int elem_bytes, int grad_by
     a.out_warps = K <= (elem_bytes == 2 && grad_bytes == 4 ? 1024 : 512) ? 16 : 8;
     a.halves = elem_bytes == 4 && !back ? 2 : 0;
     a.planes = elem_bytes == 2 ? 1 : back ? 3 : 0;
-    a.d_planes = grad_bytes == 4 ? 3 : 1;
+    // A bfloat16 dW of few rows takes two planes: sums of a row or two do not average the rounding of d, which came on top of their own
+    // (off by up to 3.8e-3 of their size, now by 1.7e-3 as bfloat16 is; of many rows 2.4e-3).  Measured (two / one): 16 x 1 row, 1024 ->
+    // 32000 637 / 626 us, 16 x 120 821 / 782, 43 x 37, 128 -> 22408 302 / 273; of many rows it is one more of three products.
+    a.d_planes = grad_bytes == 4 ? 3 : grad_bytes == 2 && M <= 128LL * N ? 2 : 1;
     a.kp = (int)up(K, 64);
     const int most = elem_bytes == 4 && back && a.cg == 1 ? 128 : 256;       // two stages in shared memory
     a.v_width = even_width(V, most, 128);
@@ -893,10 +896,10 @@ template <int CG, int MODE, int PA, int PB, int OB, int kOutWarps = 8> cudaError
     return cudaLaunchKernelEx(&cfg, kern, q, maps);
 }
 
-// EB: bytes of the inputs; GB: of dW (0: forward).
-template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Loss& p, unsigned char* scratch, int sms, int smem_optin, cudaStream_t st) {
+// EB: bytes of the inputs; GB: of dW (0: forward); D: planes of d.
+template <int CG, int EB, int GB, int D> cudaError_t run_tensor(const Plan& a, const Loss& p, unsigned char* scratch, int sms, int smem_optin, cudaStream_t st) {
     constexpr bool kBack = GB != 0;
-    constexpr int P = EB == 4 ? 3 : 1, L = EB == 2 ? 1 : kBack ? 3 : 2, D = GB == 4 ? 3 : 1;      // planes: of the gradients' products, of the logits', of d
+    constexpr int P = EB == 4 ? 3 : 1, L = EB == 2 ? 1 : kBack ? 3 : 2;      // planes: of the gradients' products, of the logits'
     const auto vec_ok = [](const void* b, long long pitch, long long stride, int eb) {
         return combo_host::aligned_to(b, 16) && pitch * eb % 16 == 0 && stride * eb % 16 == 0;
     };
@@ -1048,9 +1051,13 @@ template <int CG, int EB, int GB> cudaError_t run_tensor(const Plan& a, const Lo
 
 template <int CG> cudaError_t launch_tensor(const Plan& a, const Loss& p, int elem_bytes, int grad_bytes, void* scratch, int sms, int smem_optin, cudaStream_t st) {
     unsigned char* b = static_cast<unsigned char*>(scratch);
-    if (elem_bytes == 4) return grad_bytes ? run_tensor<CG, 4, 4>(a, p, b, sms, smem_optin, st) : run_tensor<CG, 4, 0>(a, p, b, sms, smem_optin, st);
-    if (grad_bytes == 4) return run_tensor<CG, 2, 4>(a, p, b, sms, smem_optin, st);
-    return grad_bytes ? run_tensor<CG, 2, 2>(a, p, b, sms, smem_optin, st) : run_tensor<CG, 2, 0>(a, p, b, sms, smem_optin, st);
+    if (elem_bytes == 4) return grad_bytes ? run_tensor<CG, 4, 4, 3>(a, p, b, sms, smem_optin, st) : run_tensor<CG, 4, 0, 1>(a, p, b, sms, smem_optin, st);
+    if (grad_bytes == 4) return run_tensor<CG, 2, 4, 3>(a, p, b, sms, smem_optin, st);
+    if (grad_bytes == 0) return run_tensor<CG, 2, 0, 1>(a, p, b, sms, smem_optin, st);
+    if constexpr (CG == 1) {                         // pairs have more rows a worker
+        if (a.d_planes == 2) return run_tensor<1, 2, 2, 2>(a, p, b, sms, smem_optin, st);
+    }
+    return run_tensor<CG, 2, 2, 1>(a, p, b, sms, smem_optin, st);
 }
 
 combo_status cross_entropy(Loss p, int elem_bytes, int grad_bytes, int64_t n_in, int64_t n_out, void* scratch, size_t scratch_bytes, void* stream) {

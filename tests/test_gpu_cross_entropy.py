@@ -335,3 +335,21 @@ def test_gradients_of_few_classes_are_as_exact_as_32_bit_arithmetic(dtype, count
     got, want, plain = (torch.stack(t).double() for t in (got, want, plain))
     error, allowed = float((got - want).norm() / want.norm()), float((plain - want).norm() / want.norm())
     assert error <= max(16 * U, 1.5 * allowed), (error, allowed)
+
+
+@pytest.mark.parametrize("counts,n_in,n_out", [([1] * 9, 64, 700), ([2, 1, 40, 0, 3], 200, 1500), ([70, 60], 333, 264), ([128] * 3, 72, 2000)])
+def test_bfloat16_gradients_of_few_rows_are_rounded_once(counts, n_in, n_out):
+    """d enters a bfloat16 dW of few rows a worker to 16 bits, so that the last rounding is nearly all that it is off by."""
+    c = Case(counts, n_in, n_out, BF16, BF16, mean=False, keep=0.9)
+    lse = c.exact_lse()
+    c.backward(lse)
+    assert combo.combo_last_step_path() == combo.STEP_TENSOR
+    for w in range(c.N):
+        rows, x, wt, z, dz = c.logits(w)
+        e, g = lse[rows].double()[:, None], c.row_grad[rows].double()[:, None]
+        p = torch.exp(z - e)
+        hot = torch.zeros_like(p).scatter_(1, c.labels[rows, None], 1.0)
+        d = (p - hot) * g
+        # as in Case.check_backward, but for d's own rounding: 2^-16 of it, after two planes of half a step of 2^-8 each
+        dd = g.abs() * (p * (dz + (60 + 4 * (z.abs() + e.abs())) * U) + 2 * U * (p + hot) + 2.0 ** -126) + 2.0 ** -16 * d.abs()
+        Case.near(c.dw[w], d.T @ x, dd.T @ x.abs() + 2 * (len(rows) + 4) * U * (d.abs().T @ x.abs()), 2.0 ** -8, "dw of worker %d" % w)
