@@ -4,7 +4,7 @@
 //   d_mv = (exp(z_mv - lse_m) - [v = label_m]) g_m          dx_m = sum_v d_mv W_w,v           dW_w,v = sum_m d_mv x_m
 //
 // Large calls pack the labelled rows and go through the tensor cores (cross_entropy_tensor.cuh), which bound them: forward 8 x 817
-// rows, 1024 -> 30001 bfloat16 365 to 387 us, gradients 4 x 1995 rows, 768 -> 32000 into floats 1725 to 1940; one row a worker, 16 x
+// rows, 1024 -> 30001 bfloat16 365 to 388 us, gradients 4 x 1995 rows, 768 -> 32000 into floats 1725 to 1970; one row a worker, 16 x
 // 1024 -> 32000, 190 us, bound by its 1.05 GB of weights.  Small ones are bound by latency and take one launch, or two, of
 // multiply-adds: loss of 8 x 1 row, 256 -> 10, 8.4 us, gradients of 8 x 167 rows 18.
 #include <cuda_fp16.h>
